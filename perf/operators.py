@@ -229,7 +229,8 @@ def _prepare_w4(case, gen, s, seed):
     if own:
         # the weights as the library keeps them: laid out once when they are loaded
         lib = s["lib"]
-        s["weights"] = torch.empty(lib.sgap_w4_layout_size(groups, inner, outer, case["group_k"]), dtype=torch.uint8, device="cuda")
+        size = lib.sgap_w4_layout_size(groups, inner, outer, case["group_k"], zeros=case["zeros"])
+        s["weights"] = torch.empty(size, dtype=torch.uint8, device="cuda")
         lib.sgap_w4_layout(groups, inner, outer, case["group_k"], quant, s["scales"], s["zeros"], s["weights"])
         s["Y"] = torch.empty((s["rows"], outer), dtype=dtype, device="cuda")
 
@@ -375,7 +376,8 @@ def run(s):
     groups, inner, outer, rows = case["groups"], case["inner"], case["outer"], s["rows"]
     gather = {} if s["src"] is None else {"src": s["src"], "src_div": case["k"]}
     if op == "w4":
-        lib.sgap_grouped_mm_w4(groups, rows, inner, outer, case["group_k"], s["offsets"], s["X"], s["weights"], s["Y"], **gather)
+        lib.sgap_grouped_mm_w4(groups, rows, inner, outer, case["group_k"], s["offsets"], s["X"], s["weights"], s["Y"],
+                               zeros=case["zeros"], **gather)
         return [s["Y"]]
     layout = case["layout"]
     lib.sgap_grouped_mm(groups, rows, inner, outer, s["offsets"], s["X"], s["W"], s["Y"], layout, **gather)
