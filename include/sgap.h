@@ -706,6 +706,124 @@ int sgap_reorder_rows_csr(int64_t M, int64_t K, const int32_t* rowptr, const int
                           int order, int32_t* perm, int32_t* rowptr_out, int32_t* colidx_out, float* vals_out,
                           void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Mixtures of experts.  A router gives each of T tokens k of E experts: a
+ * sparse T x E matrix with k stored entries a row.  These calls make that
+ * matrix and its transpose (the pairs grouped by expert), multiply the rows of
+ * each group by its expert's weights, and sum the results up by token.  All of
+ * them follow the conventions at the top of this file: device pointers, nothing
+ * allocated, work enqueued on `stream` (and so fit for a HIP graph), results
+ * overwritten, SGAP_ERR_INVALID_ARG found before anything is launched.  They
+ * use no atomics: two calls on the same inputs give the same bits.
+ *
+ * Element types: an array typed `void` holds elements of the call's `dtype`.
+ * Sums, softmax statistics and gates are 32-bit floats; a result is rounded to
+ * its type once, when it is stored.
+ */
+typedef enum { SGAP_F32 = 0, SGAP_F16 = 1, SGAP_BF16 = 2 } sgap_dtype;
+#define SGAP_MAX_EXPERTS 1024
+#define SGAP_MAX_CHOSEN 16
+
+/*
+ * The k largest of E logits for each token, their gates, and the pairs grouped
+ * by expert.  Pair t * k + j is token t's choice j; choices are sorted by
+ * logit, the largest first, equal ones by their expert.
+ *   logits      T x E, rows ld_logits apart; read only.  -infinity marks an
+ *               expert that the token may not have: it is never chosen, and a
+ *               token with fewer than k others left has fewer choices (expert
+ *               and slot -1, gate 0).  NaN counts as larger than every number,
+ *               and makes the token's gates NaN; so does +infinity.
+ *   renormalise 0: gate = softmax over all E logits; 1: over the chosen ones
+ *   gates       T x k floats
+ *   experts     T x k: the chosen experts
+ *   slot        T x k: the place of each pair in `order`
+ *   order       T * k: the pairs by expert, and by number within one; behind
+ *               them (missing choices) -1
+ *   offsets     E + 1: expert e has places offsets[e] .. offsets[e+1]
+ *   workspace   sgap_route_topk_workspace_size(T, E, k) bytes (0 up to 64
+ *               tokens: may be null then), 16-byte aligned, caller-owned;
+ *               contents meaningless before and after
+ * 1 <= k <= SGAP_MAX_CHOSEN, k <= E <= SGAP_MAX_EXPERTS, T * k < 2^31 - 1.
+ */
+int64_t sgap_route_topk_workspace_size(int64_t T, int64_t E, int64_t k);
+int sgap_route_topk(int64_t T, int64_t E, int64_t k, int dtype, const void* logits, int64_t ld_logits, int renormalise,
+                    float* gates, int32_t* experts, int32_t* slot, int32_t* order, int32_t* offsets, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+/* The gradient of the logits (T x E, every element written) from that of the
+ * gates; logits, gates and experts as sgap_route_topk had and left them.  The
+ * choice itself counts as constant. */
+int sgap_route_topk_grad(int64_t T, int64_t E, int64_t k, int dtype, const void* logits, int64_t ld_logits, int renormalise,
+                         const float* gates, const int32_t* experts, const float* dgates, void* dlogits, int64_t ld_dlogits,
+                         void* stream);
+
+/*
+ * out[t, :] = sum over j of gates[t, j] * Z[slot[t, j], :]; a slot of -1 adds
+ * nothing, and a token of which nothing is left becomes +0.  gates null: all 1
+ * (what the gradient of gathered rows needs).
+ *   Z     T * k rows of D, contiguous;  out  T x D, contiguous
+ */
+int sgap_route_combine(int64_t T, int64_t k, int64_t D, int dtype, const void* Z, const int32_t* slot, const float* gates,
+                       void* out, void* stream);
+/* dZ[slot[t, j], :] = gates[t, j] * dout[t, :] (rows that no pair has, by
+ * `order`, become +0) and dgates[t, j] = <Z[slot[t, j], :], dout[t, :]> (0 for
+ * a slot of -1). */
+int sgap_route_combine_grad(int64_t T, int64_t k, int64_t D, int dtype, const void* Z, const int32_t* slot,
+                            const int32_t* order, const float* gates, const void* dout, void* dZ, float* dgates, void* stream);
+
+/*
+ * Products over ragged groups of rows: group g has rows offsets[g] ..
+ * offsets[g+1] of R, and
+ *   Y[r, :] = X[src(r), :] * op(W[g])          r in group g
+ * Rows behind offsets[G] become +0.
+ *   offsets  G + 1, from 0, non-decreasing, offsets[G] <= R (not checked on
+ *            the device, but nothing outside 0 .. R is touched whatever they
+ *            hold); null: one group of all rows, G = 1
+ *   X        x_rows rows of K elements, ldx apart
+ *   src      null: src(r) = r; else R entries, and row r takes row
+ *            src[r] / src_div of X: with sgap_route_topk's order and its k that
+ *            is the token of each pair.  A row outside X counts as zeros.
+ *   W        G matrices, contiguous: SGAP_WEIGHTS_NK N x K (Y = X W^T), or
+ *            SGAP_WEIGHTS_KN K x N (Y = X W)
+ *   Y        R x N, rows ldy apart
+ * The gradient of the rows that come in is the same call on dY with the other
+ * layout's name: K and N change places, and W stays where it is.  K = 0 gives
+ * zeros.  Any sizes, strides and element-aligned addresses; multiples of 16
+ * bytes are faster.  Y must not overlap X or W.
+ */
+typedef enum { SGAP_WEIGHTS_NK = 0, SGAP_WEIGHTS_KN = 1 } sgap_weight_layout;
+int sgap_grouped_mm(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, const int32_t* offsets, const void* X, int64_t ldx,
+                    int64_t x_rows, const int32_t* src, int64_t src_div, const void* W, int layout, void* Y, int64_t ldy,
+                    void* stream);
+/* dW[g] = sum over the rows r of group g of dY[r, :] (x) X[src(r), :], in the
+ * weights' layout; a group without rows gets +0. */
+int sgap_grouped_mm_wgrad(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, const int32_t* offsets, const void* X,
+                          int64_t ldx, int64_t x_rows, const int32_t* src, int64_t src_div, const void* dY, int64_t lddy,
+                          void* dW, int layout, void* stream);
+
+/*
+ * The same product with weights of 4 bits,
+ *   W[g][n, k] = (code[g][n, k] - zero[g][n, k / group_k]) * scale[g][n, k / group_k],
+ * for few rows a group: the weights pass once for every 16 (few rows) or 48
+ * rows.  No weight is rounded on the way.  sgap_w4_layout puts codes, scales
+ * and zero points into the order in which the product reads them; a program
+ * does that once, when it loads its weights, and may free them afterwards.
+ *   codes    G x N x K/2 bytes, the code of an even k in the low half
+ *   scales   G x N x K/group_k elements of 16 bits, of the type that the
+ *            products are asked for
+ *   zeros    G x N x K/group_k bytes; null: all 8
+ *   weights  sgap_w4_layout_size bytes, 16-byte aligned
+ * group_k is 32, 64 or a multiple of 128, and divides K; dtype SGAP_F16 or
+ * SGAP_BF16; everything else as for sgap_grouped_mm.  `zeros` of the size and
+ * the product: whether there were zero points.
+ */
+int64_t sgap_w4_layout_size(int64_t G, int64_t K, int64_t N, int64_t group_k, int zeros);
+int sgap_w4_layout(int64_t G, int64_t K, int64_t N, int64_t group_k, const uint8_t* codes, const void* scales,
+                   const uint8_t* zeros, void* weights, int64_t weights_bytes, void* stream);
+int sgap_grouped_mm_w4(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, int64_t group_k, int zeros, const int32_t* offsets,
+                       const void* X, int64_t ldx, int64_t x_rows, const int32_t* src, int64_t src_div, const void* weights,
+                       int64_t weights_bytes, void* Y, int64_t ldy, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,7 +1,7 @@
 """Binding of libsgap.so: argument marshalling only.
 
-sgap_spmm_csr_ex, sgap_spmm_csr_cfg, sgap_sddmm_csr, sgap_sddmm_csr_windows, sgap_ttm_csf and sgap_mttkrp_csf_ex go
-through a small native module (csrc/sgap_python.cpp), which reads the tensors and calls the library in a few hundred
+sgap_spmm_csr_ex, sgap_spmm_csr_cfg, sgap_sddmm_csr, sgap_sddmm_csr_windows, sgap_ttm_csf, sgap_mttkrp_csf_ex and the
+calls of a mixture of experts (sgap_route_*, sgap_grouped_*) go through a small native module (csrc/sgap_python.cpp), which reads the tensors and calls the library in a few hundred
 nanoseconds; what it does not take (another type, a wrong length, a number that is no int) goes through ctypes and the
 checks below, which say what is wrong.  The other calls, and all of them where that module has not been built, go
 through ctypes: about 8 us of host time each.
@@ -59,6 +59,16 @@ EXPORTS = {
     "sgap_ttm_csf": (_int, [_i64, _i64, _i64, _p, _p, _p, _p, _p, _int, _int, _int, _i64, _p]),
     "sgap_mttkrp_csf": (_int, [_i64, _i64, _i64, _i64, _p, _p, _p, _p, _p, _p, _p, _p, _int, _int, _p]),
     "sgap_mttkrp_csf_ex": (_int, [_i64, _i64, _i64, _i64, _p, _p, _p, _p, _p, _p, _p, _p, _int, _int, _int, _i64, _p]),
+    "sgap_route_topk_workspace_size": (_i64, [_i64, _i64, _i64]),
+    "sgap_route_topk": (_int, [_i64, _i64, _i64, _int, _p, _i64, _int, _p, _p, _p, _p, _p, _p, _i64, _p]),
+    "sgap_route_topk_grad": (_int, [_i64, _i64, _i64, _int, _p, _i64, _int, _p, _p, _p, _p, _i64, _p]),
+    "sgap_route_combine": (_int, [_i64, _i64, _i64, _int, _p, _p, _p, _p, _p]),
+    "sgap_route_combine_grad": (_int, [_i64, _i64, _i64, _int, _p, _p, _p, _p, _p, _p, _p, _p]),
+    "sgap_grouped_mm": (_int, [_i64, _i64, _i64, _i64, _int, _p, _p, _i64, _i64, _p, _i64, _p, _int, _p, _i64, _p]),
+    "sgap_grouped_mm_wgrad": (_int, [_i64, _i64, _i64, _i64, _int, _p, _p, _i64, _i64, _p, _i64, _p, _i64, _p, _int, _p]),
+    "sgap_w4_layout_size": (_i64, [_i64, _i64, _i64, _i64, _int]),
+    "sgap_w4_layout": (_int, [_i64, _i64, _i64, _i64, _p, _p, _p, _p, _i64, _p]),
+    "sgap_grouped_mm_w4": (_int, [_i64, _i64, _i64, _i64, _int, _i64, _int, _p, _p, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p]),
     "sgap_status_string": (ctypes.c_char_p, [_int]),
     "sgap_last_error": (ctypes.c_char_p, []),
     "sgap_version": (_int, []),
@@ -574,3 +584,199 @@ def sgap_stream_f32(src, dst, n, mode, stream=None) -> None:
 
     _check(load().sgap_stream_f32(_dev_ptr(src, torch.float32, "src") if src is not None else None,
                                   _dev_ptr(dst, torch.float32, "dst"), int(n), int(mode), _stream_ptr(stream)))
+
+
+# --------------------------------------------------------------------------
+# mixtures of experts
+# --------------------------------------------------------------------------
+
+SGAP_F32, SGAP_F16, SGAP_BF16 = 0, 1, 2
+SGAP_MAX_EXPERTS, SGAP_MAX_CHOSEN = 1024, 16
+WEIGHT_LAYOUTS = {"nk": 0, "kn": 1}
+
+
+def _element_type(t, name):
+    import torch
+
+    types = {torch.float32: SGAP_F32, torch.float16: SGAP_F16, torch.bfloat16: SGAP_BF16}
+    if not isinstance(t, torch.Tensor) or t.dtype not in types:
+        raise TypeError(f"{name} must be a float32, float16 or bfloat16 tensor")
+    return types[t.dtype]
+
+
+def _flat(t, dtype, count, name):
+    """Device pointer of a contiguous tensor of `count` elements."""
+    ptr = _dev_ptr(t, dtype, name)
+    if t.numel() != count:
+        raise ValueError(f"{name} must have {count} elements, got {t.numel()}")
+    return ptr
+
+
+def _rows(t, dtype, rows, columns, name):
+    """(device pointer, elements from row to row) of a matrix whose rows are contiguous."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (device memory)")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or t.shape[1] != columns:
+        raise ValueError(f"{name} must be {'any number of' if rows is None else rows} rows of {columns}, got {tuple(t.shape)}")
+    if (columns > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < columns):
+        raise ValueError(f"the rows of {name} must be contiguous and must not overlap")
+    return (t.data_ptr() if t.numel() else None), (t.stride(0) if t.shape[0] > 1 else columns)
+
+
+def sgap_route_topk_workspace_size(T, E, k) -> int:
+    size = load().sgap_route_topk_workspace_size(int(T), int(E), int(k))
+    if size < 0:
+        raise SgapError(SGAP_ERR_INVALID_ARG, load().sgap_last_error().decode())
+    return size
+
+
+def sgap_route_topk(T, E, k, logits, gates, experts, slot, order, offsets, renormalise=True, workspace=None, stream=None) -> None:
+    """The k largest of E logits for each of T tokens, their gates, and the pairs (token, expert) grouped by expert (see
+    include/sgap.h).  `workspace`: a CUDA uint8 tensor of sgap_route_topk_workspace_size bytes, None where that is 0."""
+    renormalise = int(bool(renormalise))
+    st = (_native or _load_native()).route_topk(T, E, k, logits, gates, experts, slot, order, offsets, renormalise, workspace, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(logits, "logits")
+    ptr, ld = _rows(logits, logits.dtype, T, E, "logits")
+    ws, ws_bytes = _workspace_args(workspace)
+    _check(load().sgap_route_topk(
+        T, E, k, dtype, ptr, ld, renormalise, _flat(gates, torch.float32, T * k, "gates"),
+        _flat(experts, torch.int32, T * k, "experts"), _flat(slot, torch.int32, T * k, "slot"),
+        _flat(order, torch.int32, T * k, "order"), _flat(offsets, torch.int32, E + 1, "offsets"), ws, ws_bytes, _stream_ptr(stream)))
+
+
+def sgap_route_topk_grad(T, E, k, logits, gates, experts, dgates, dlogits, renormalise=True, stream=None) -> None:
+    """dlogits from the gradient of the gates that sgap_route_topk gave (see include/sgap.h)."""
+    renormalise = int(bool(renormalise))
+    st = (_native or _load_native()).route_topk_grad(T, E, k, logits, gates, experts, dgates, dlogits, renormalise, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(logits, "logits")
+    ptr, ld = _rows(logits, logits.dtype, T, E, "logits")
+    dptr, ldd = _rows(dlogits, logits.dtype, T, E, "dlogits")
+    _check(load().sgap_route_topk_grad(
+        T, E, k, dtype, ptr, ld, renormalise, _flat(gates, torch.float32, T * k, "gates"),
+        _flat(experts, torch.int32, T * k, "experts"), _flat(dgates, torch.float32, T * k, "dgates"), dptr, ldd,
+        _stream_ptr(stream)))
+
+
+def sgap_route_combine(T, k, D, Z, slot, gates, out, stream=None) -> None:
+    """out[t] = sum over j of gates[t, j] * Z[slot[t, j]]; gates None: all 1 (see include/sgap.h)."""
+    st = (_native or _load_native()).route_combine(T, k, D, Z, slot, gates, out, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(Z, "Z")
+    _check(load().sgap_route_combine(
+        T, k, D, dtype, _flat(Z, Z.dtype, T * k * D, "Z"), _flat(slot, torch.int32, T * k, "slot"),
+        None if gates is None else _flat(gates, torch.float32, T * k, "gates"), _flat(out, Z.dtype, T * D, "out"),
+        _stream_ptr(stream)))
+
+
+def sgap_route_combine_grad(T, k, D, Z, slot, order, gates, dout, dZ, dgates, stream=None) -> None:
+    """The gradients of sgap_route_combine (see include/sgap.h)."""
+    st = (_native or _load_native()).route_combine_grad(T, k, D, Z, slot, order, gates, dout, dZ, dgates, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(Z, "Z")
+    _check(load().sgap_route_combine_grad(
+        T, k, D, dtype, _flat(Z, Z.dtype, T * k * D, "Z"), _flat(slot, torch.int32, T * k, "slot"),
+        _flat(order, torch.int32, T * k, "order"), _flat(gates, torch.float32, T * k, "gates"), _flat(dout, Z.dtype, T * D, "dout"),
+        _flat(dZ, Z.dtype, T * k * D, "dZ"), _flat(dgates, torch.float32, T * k, "dgates"), _stream_ptr(stream)))
+
+
+def _grouped_args(G, R, K, offsets, X, src, src_div):
+    """(offsets, X, ldx, rows of X, src, src_div) of a product over groups."""
+    import torch
+
+    off = None if offsets is None else _flat(offsets, torch.int32, G + 1, "offsets")
+    ptr, ld = _rows(X, X.dtype, None, K, "X")
+    return off, ptr, ld, X.shape[0], None if src is None else _flat(src, torch.int32, R, "src"), int(src_div)
+
+
+def sgap_grouped_mm(G, R, K, N, offsets, X, W, Y, layout="nk", src=None, src_div=1, stream=None) -> None:
+    """Y[r] = X[src[r] // src_div] * op(W[g]) for the rows r of each group g; `layout` "nk" (W[g] is N x K) or "kn" (see
+    include/sgap.h).  offsets None: one group of all rows; src None: row r takes row r."""
+    layout = WEIGHT_LAYOUTS.get(layout, layout)
+    st = (_native or _load_native()).grouped_mm(G, R, K, N, offsets, X, W, Y, layout, src, src_div, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    dtype = _element_type(X, "X")
+    args = _grouped_args(G, R, K, offsets, X, src, src_div)
+    w = _flat(W, X.dtype, G * K * N, "W")
+    y, ldy = _rows(Y, X.dtype, R, N, "Y")
+    _check(load().sgap_grouped_mm(G, R, K, N, dtype, *args, w, int(layout), y, ldy, _stream_ptr(stream)))
+
+
+def sgap_grouped_mm_wgrad(G, R, K, N, offsets, X, dY, dW, layout="nk", src=None, src_div=1, stream=None) -> None:
+    """The gradient of sgap_grouped_mm's weights (see include/sgap.h)."""
+    layout = WEIGHT_LAYOUTS.get(layout, layout)
+    st = (_native or _load_native()).grouped_mm_wgrad(G, R, K, N, offsets, X, dY, dW, layout, src, src_div, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    dtype = _element_type(X, "X")
+    args = _grouped_args(G, R, K, offsets, X, src, src_div)
+    d, ldd = _rows(dY, X.dtype, R, N, "dY")
+    w = _flat(dW, X.dtype, G * K * N, "dW")
+    _check(load().sgap_grouped_mm_wgrad(G, R, K, N, dtype, *args, d, ldd, w, int(layout), _stream_ptr(stream)))
+
+
+def sgap_w4_layout_size(G, K, N, group_k, zeros=False) -> int:
+    size = load().sgap_w4_layout_size(int(G), int(K), int(N), int(group_k), int(bool(zeros)))
+    if size < 0:
+        raise SgapError(SGAP_ERR_INVALID_ARG, load().sgap_last_error().decode())
+    return size
+
+
+def sgap_w4_layout(G, K, N, group_k, codes, scales, zeros, weights, stream=None) -> None:
+    """4-bit weights as sgap_grouped_mm_w4 reads them, into the CUDA uint8 tensor `weights` of sgap_w4_layout_size bytes: codes
+    G x N x K/2 (uint8), scales G x N x K/group_k (float16 or bfloat16), zeros the same in uint8 or None for 8."""
+    import torch
+
+    if _element_type(scales, "scales") == SGAP_F32:
+        raise TypeError("scales must be float16 or bfloat16")
+    blocks = K // max(int(group_k), 1)
+    ws, ws_bytes = _workspace_args(weights)
+    _check(load().sgap_w4_layout(
+        G, K, N, int(group_k), _flat(codes, torch.uint8, G * N * (K // 2), "codes"), _flat(scales, scales.dtype, G * N * blocks, "scales"),
+        None if zeros is None else _flat(zeros, torch.uint8, G * N * blocks, "zeros"), ws, ws_bytes, _stream_ptr(stream)))
+
+
+def sgap_grouped_mm_w4(G, R, K, N, group_k, offsets, X, weights, Y, zeros=False, src=None, src_div=1, stream=None) -> None:
+    """sgap_grouped_mm with the weights that sgap_w4_layout left in `weights`; `zeros`: whether there were zero points.  X and Y
+    have the scales' type (see include/sgap.h)."""
+    zeros = int(bool(zeros))
+    st = (_native or _load_native()).grouped_mm_w4(G, R, K, N, group_k, offsets, X, weights, Y, zeros, src, src_div, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    dtype = _element_type(X, "X")
+    args = _grouped_args(G, R, K, offsets, X, src, src_div)
+    ws, ws_bytes = _workspace_args(weights)
+    y, ldy = _rows(Y, X.dtype, R, N, "Y")
+    _check(load().sgap_grouped_mm_w4(G, R, K, N, dtype, int(group_k), zeros, *args, ws, ws_bytes, y, ldy, _stream_ptr(stream)))

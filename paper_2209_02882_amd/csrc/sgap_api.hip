@@ -230,6 +230,15 @@ int fail(int status, const char* fmt, const char* detail = "")
     return status;
 }
 
+}  // namespace
+
+// the same for the entry points in other files
+namespace sgap {
+int fail_call(int status, const char* detail) { return fail(status, "%s", detail); }
+}  // namespace sgap
+
+namespace {
+
 bool is_pow2_group(int g) { return g >= 1 && g <= 64 && (g & (g - 1)) == 0; }
 
 int ilog2(int v)

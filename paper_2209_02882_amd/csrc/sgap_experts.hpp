@@ -1,0 +1,162 @@
+// Shared by the operators of a mixture of experts: element types, 16-byte pieces of rows, the matrix instruction, and
+// the host-side launch entry points.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sgap {
+
+typedef _Float16 half_t;
+typedef __bf16 bf16_t;
+
+// 16 bytes as the memory path takes them, asking for no more alignment than an element has: this chip reads and writes
+// such addresses in one instruction.
+template <typename T>
+struct Piece {
+    static constexpr int kCount = 16 / (int)sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+    typedef T loose __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+template <typename T>
+using piece_t = typename Piece<T>::vec;
+
+template <typename T>
+__device__ __forceinline__ piece_t<T> load_piece(const T* p)
+{
+    return *reinterpret_cast<const typename Piece<T>::loose*>(p);
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* p, piece_t<T> v)
+{
+    *reinterpret_cast<typename Piece<T>::loose*>(p) = v;
+}
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// acc += A * B on a 16 x 16 tile.  A lane has 16 bytes of one row of A (row lane % 16) and of one column of B (column
+// lane % 16), the piece lane / 16 of four: 32 values of the inner dimension with 16-bit types, 16 with floats, where one
+// instruction takes one value of each lane.  Which lane holds which value of the inner dimension does not matter as long
+// as A and B agree.  Result: lane l has rows 4 * (l / 16) + 0 .. 3 of column l % 16.
+__device__ __forceinline__ f32x4 mma16(piece_t<half_t> a, piece_t<half_t> b, f32x4 acc)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(piece_t<bf16_t> a, piece_t<bf16_t> b, f32x4 acc)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma16(piece_t<float> a, piece_t<float> b, f32x4 acc)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc, 0, 0, 0);
+    return acc;
+}
+
+// The rows that a product takes: row r is row src[r] / div of X, or row r itself without a list.
+struct RowSource {
+    const int32_t* __restrict__ src;
+    uint32_t div;
+    int64_t rows;  // rows of X; a row that lies outside counts as zeros
+    __device__ __forceinline__ int64_t row(int64_t r) const  // -1: no such row
+    {
+        if (!src) return r < rows ? r : -1;
+        const int32_t s = src[r];
+        if (s < 0) return -1;
+        const int64_t t = (uint32_t)s / div;
+        return t < rows ? t : -1;
+    }
+};
+
+// Rows first .. end of group g; nothing outside 0 .. rows whatever the offsets hold.  Without offsets: one group of all rows.
+struct GroupRows {
+    int64_t first, end;
+};
+__device__ __forceinline__ GroupRows group_rows(const int32_t* __restrict__ offsets, int64_t g, int64_t rows)
+{
+    if (!offsets) return {0, rows};
+    const int64_t a = offsets[g], b = offsets[g + 1];
+    const int64_t first = a < 0 ? 0 : a, end = b > rows ? rows : b;
+    return {first, end < first ? first : end};
+}
+
+// What a product over groups has to know.  K: inner dimension of the product, N: its columns.
+struct GroupedArgs {
+    int64_t G, R, K, N;
+    const int32_t* __restrict__ offsets;
+    RowSource from;
+    const void* __restrict__ X;
+    int64_t ldx;
+    const void* __restrict__ W;  // G matrices, N x K or K x N
+    void* __restrict__ Y;
+    int64_t ldy;
+    bool weights_kn;  // K x N
+};
+
+// dW of the same: Y holds the gradient of the product's result (read), W the gradient of the weights (written).
+struct GroupedW4Args {
+    int64_t G, R, K, N;
+    const int32_t* __restrict__ offsets;
+    RowSource from;
+    const void* __restrict__ X;
+    int64_t ldx;
+    const uint8_t* __restrict__ weights;  // as launch_w4_layout leaves them
+    int group_k;
+    bool zeros;
+    void* __restrict__ Y;
+    int64_t ldy;
+};
+
+struct RouteArgs {
+    int64_t T;
+    int E, k, dtype;
+    bool renormalise;
+    const void* __restrict__ logits;
+    int64_t ld;
+    float* __restrict__ gates;
+    int32_t *__restrict__ experts, *__restrict__ slot, *__restrict__ order, *__restrict__ offsets;
+    void* workspace;
+};
+
+struct RouteGradArgs {
+    int64_t T;
+    int E, k, dtype;
+    bool renormalise;
+    const void* __restrict__ logits;
+    int64_t ld;
+    const float* __restrict__ gates;
+    const int32_t* __restrict__ experts;
+    const float* __restrict__ dgates;
+    void* __restrict__ dlogits;
+    int64_t ldd;
+};
+
+struct CombineArgs {
+    int64_t T, D;
+    int k, dtype;
+    const void* __restrict__ Z;
+    const int32_t* __restrict__ slot;
+    const int32_t* __restrict__ order;
+    const float* __restrict__ gates;
+    const void* __restrict__ dout;
+    void* __restrict__ out;  // the sum, or the gradient of Z
+    float* __restrict__ dgates;
+};
+
+int64_t route_workspace_bytes(int64_t T, int64_t E, int64_t k);
+hipError_t launch_route(const RouteArgs& a, hipStream_t s);
+hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);
+hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
+hipError_t launch_combine_grad(const CombineArgs& a, hipStream_t s);
+// dtype as in sgap.h
+hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s);
+hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
+struct W4Sizes {
+    int64_t tiles_n, blocks_k, scales_k;   // per group: tiles of 16 columns, blocks of 128 weights, scales along K
+    int64_t scales_at, zeros_at, bytes;    // byte offsets in the laid-out weights
+};
+W4Sizes w4_sizes(int64_t G, int64_t K, int64_t N, int group_k, bool zeros);
+hipError_t launch_w4_layout(int64_t G, int64_t K, int64_t N, int group_k, const uint8_t* q, const void* scales,
+                            const uint8_t* zeros, uint8_t* out, hipStream_t s);
+hipError_t launch_grouped_w4(const GroupedW4Args& a, int dtype, hipStream_t s);
+
+}  // namespace sgap

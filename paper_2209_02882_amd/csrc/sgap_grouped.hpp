@@ -1,0 +1,63 @@
+// How the products over groups find their work: tiles of rows that never cross a group, found from the offsets on the
+// device, so that the host needs no group's size.
+#pragma once
+#include "sgap_experts.hpp"
+
+namespace sgap {
+
+// The rows of one tile: up to BM rows from `first`, of group g; g = G: rows behind the last group, whose results are zero.
+struct RowTile {
+    int64_t g, first;
+    int rows;  // 0: no such tile
+};
+
+__device__ __forceinline__ int wave_scan_int(int v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// Tile number `index` of the tiles of BM rows of all groups, in their order, and of the rows behind them.  By one
+// wavefront, whose lanes look at 64 groups at a time; every lane gets the answer.
+template <int BM>
+__device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ offsets, int64_t G, int64_t R, int64_t index)
+{
+    if (!offsets) {
+        const int64_t first = index * BM;
+        return {0, first, first < R ? (int)min((int64_t)BM, R - first) : 0};
+    }
+    const int lane = threadIdx.x & 63;
+    int64_t passed = 0;  // tiles of the groups looked at
+    for (int64_t g0 = 0; g0 < G; g0 += 64) {
+        const int64_t g = g0 + lane;
+        GroupRows rows = {0, 0};
+        if (g < G) rows = group_rows(offsets, g, R);
+        const int tiles = (int)((rows.end - rows.first + BM - 1) / BM);
+        const int upto = wave_scan_int(tiles);
+        const uint64_t behind = __ballot(passed + upto > index);
+        if (behind) {
+            const int who = __builtin_ctzll(behind);
+            const int before = __shfl(upto - tiles, who);
+            const int first = __shfl((int)rows.first, who), end = __shfl((int)rows.end, who);
+            const int64_t at = first + (index - passed - before) * BM;
+            return {g0 + who, at, (int)min((int64_t)BM, end - at)};
+        }
+        passed += __shfl(upto, 63);
+    }
+    const int64_t last = group_rows(offsets, G - 1, R).end;
+    const int64_t at = last + (index - passed) * BM;
+    return {G, at, at < R ? (int)min((int64_t)BM, R - at) : 0};
+}
+
+// tiles of BM rows at most: every group may have a last tile that is not full, and the rows behind the groups too
+inline int64_t most_row_tiles(int64_t G, int64_t R, int BM, bool offsets)
+{
+    return offsets ? (R + BM - 1) / BM + (G < R ? G : R) + 1 : (R + BM - 1) / BM;
+}
+
+}  // namespace sgap

@@ -8,6 +8,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <initializer_list>
+
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -112,6 +114,38 @@ struct Matrix {
         C = c.floats(7, M * N);
     }
 };
+
+struct Rows {
+    void* data;
+    int64_t ld;
+};
+
+// the calls' element types
+int element_type(at::ScalarType t)
+{
+    return t == at::kFloat ? SGAP_F32 : t == at::kHalf ? SGAP_F16 : t == at::kBFloat16 ? SGAP_BF16 : -1;
+}
+
+// a matrix of rows x columns whose rows lie side by side at any distance
+Rows rows_of(Call& c, int n, at::ScalarType type, int64_t rows, int64_t columns)
+{
+    const at::Tensor* t = c.tensor(n);
+    if (!t) return {nullptr, 0};
+    if (!t->is_cuda() || t->scalar_type() != type || t->dim() != 2 || t->size(0) != rows || t->size(1) != columns ||
+        (columns > 1 && t->stride(1) != 1) || (rows > 1 && t->stride(0) < columns)) {
+        c.ok = false;
+        return {nullptr, 0};
+    }
+    return {t->numel() ? t->data_ptr() : nullptr, rows > 1 ? t->stride(0) : columns};
+}
+
+at::ScalarType type_of(Call& c, int n)
+{
+    const at::Tensor* t = c.tensor(n);
+    if (!t) return at::kFloat;
+    if (element_type(t->scalar_type()) < 0) c.ok = false;
+    return t->scalar_type();
+}
 
 PyObject* status(int st) { return PyLong_FromLong(st); }
 
@@ -247,12 +281,182 @@ PyObject* mttkrp_csf_ex(PyObject*, PyObject* const* arg, Py_ssize_t n)
     });
 }
 
+bool sizes_ok(Call& c, std::initializer_list<int64_t> sizes)
+{
+    for (int64_t v : sizes)
+        if (v < 0 || v > INT32_MAX) c.ok = false;
+    return c.ok;
+}
+
+// T, E, k, logits, gates, experts, slot, order, offsets, renormalise, workspace, stream
+PyObject* route_topk(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 12) return status(kNotTaken);
+    const int64_t T = c.number(0), E = c.number(1), k = c.number(2);
+    if (!sizes_ok(c, {T, E, k})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 3);
+    const Rows logits = rows_of(c, 3, type, T, E);
+    float* gates = c.floats(4, T * k);
+    int32_t *experts = c.ints(5, T * k), *slot = c.ints(6, T * k), *order = c.ints(7, T * k), *offsets = c.ints(8, E + 1);
+    const int renormalise = c.small(9);
+    int64_t bytes = 0;
+    void* ws = c.workspace(10, &bytes);
+    void* stream = c.stream(11);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_route_topk(T, E, k, element_type(type), logits.data, logits.ld, renormalise, gates, experts, slot, order,
+                               offsets, ws, bytes, stream);
+    });
+}
+
+// T, E, k, logits, gates, experts, dgates, dlogits, renormalise, stream
+PyObject* route_topk_grad(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 10) return status(kNotTaken);
+    const int64_t T = c.number(0), E = c.number(1), k = c.number(2);
+    if (!sizes_ok(c, {T, E, k})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 3);
+    const Rows logits = rows_of(c, 3, type, T, E), dlogits = rows_of(c, 7, type, T, E);
+    const float *gates = c.floats(4, T * k), *dgates = c.floats(6, T * k);
+    const int32_t* experts = c.ints(5, T * k);
+    const int renormalise = c.small(8);
+    void* stream = c.stream(9);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_route_topk_grad(T, E, k, element_type(type), logits.data, logits.ld, renormalise, gates, experts, dgates,
+                                    dlogits.data, dlogits.ld, stream);
+    });
+}
+
+// T, k, D, Z, slot, gates or None, out, stream
+PyObject* route_combine(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 8) return status(kNotTaken);
+    const int64_t T = c.number(0), k = c.number(1), D = c.number(2);
+    if (!sizes_ok(c, {T, k, D})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 3);
+    const void* Z = c.data(3, type, T * k * D);
+    const int32_t* slot = c.ints(4, T * k);
+    const float* gates = arg[5] == Py_None ? nullptr : c.floats(5, T * k);
+    void* out = c.data(6, type, T * D);
+    void* stream = c.stream(7);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] { return sgap_route_combine(T, k, D, element_type(type), Z, slot, gates, out, stream); });
+}
+
+// T, k, D, Z, slot, order, gates, dout, dZ, dgates, stream
+PyObject* route_combine_grad(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 11) return status(kNotTaken);
+    const int64_t T = c.number(0), k = c.number(1), D = c.number(2);
+    if (!sizes_ok(c, {T, k, D})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 3);
+    const void *Z = c.data(3, type, T * k * D), *dout = c.data(7, type, T * D);
+    const int32_t *slot = c.ints(4, T * k), *order = c.ints(5, T * k);
+    const float* gates = c.floats(6, T * k);
+    void* dZ = c.data(8, type, T * k * D);
+    float* dgates = c.floats(9, T * k);
+    void* stream = c.stream(10);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_route_combine_grad(T, k, D, element_type(type), Z, slot, order, gates, dout, dZ, dgates, stream);
+    });
+}
+
+// the rows that a product over groups takes
+struct Grouped {
+    int64_t G, R, K, N, x_rows = 0, src_div;
+    at::ScalarType type;
+    const int32_t *offsets, *src;
+    Rows X;
+    // arguments 0 .. 3: G, R, K, N; then the places of offsets, X, src and src_div
+    Grouped(Call& c, int offsets_at, int x_at, int src_at)
+    {
+        G = c.number(0); R = c.number(1); K = c.number(2); N = c.number(3);
+        if (!sizes_ok(c, {G, R, K, N})) return;
+        offsets = c.arg[offsets_at] == Py_None ? nullptr : c.ints(offsets_at, G + 1);
+        type = type_of(c, x_at);
+        const at::Tensor* x = c.tensor(x_at);
+        if (x && x->dim() == 2) x_rows = x->size(0);
+        X = rows_of(c, x_at, type, x_rows, K);
+        src = c.arg[src_at] == Py_None ? nullptr : c.ints(src_at, R);
+        src_div = c.number(src_at + 1);
+    }
+};
+
+// G, R, K, N, offsets or None, X, W, Y, layout, src or None, src_div, stream
+PyObject* grouped_mm(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 12) return status(kNotTaken);
+    const Grouped m(c, 4, 5, 9);
+    if (!c.ok) return status(kNotTaken);
+    const void* W = c.data(6, m.type, m.G * m.K * m.N);
+    const Rows Y = rows_of(c, 7, m.type, m.R, m.N);
+    const int layout = c.small(8);
+    void* stream = c.stream(11);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_grouped_mm(m.G, m.R, m.K, m.N, element_type(m.type), m.offsets, m.X.data, m.X.ld, m.x_rows, m.src, m.src_div,
+                               W, layout, Y.data, Y.ld, stream);
+    });
+}
+
+// G, R, K, N, offsets or None, X, dY, dW, layout, src or None, src_div, stream
+PyObject* grouped_mm_wgrad(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 12) return status(kNotTaken);
+    const Grouped m(c, 4, 5, 9);
+    if (!c.ok) return status(kNotTaken);
+    const Rows dY = rows_of(c, 6, m.type, m.R, m.N);
+    void* dW = c.data(7, m.type, m.G * m.K * m.N);
+    const int layout = c.small(8);
+    void* stream = c.stream(11);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_grouped_mm_wgrad(m.G, m.R, m.K, m.N, element_type(m.type), m.offsets, m.X.data, m.X.ld, m.x_rows, m.src,
+                                     m.src_div, dY.data, dY.ld, dW, layout, stream);
+    });
+}
+
+// G, R, K, N, group_k, offsets or None, X, weights, Y, zeros, src or None, src_div, stream
+PyObject* grouped_mm_w4(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 13) return status(kNotTaken);
+    const Grouped m(c, 5, 6, 10);
+    if (!c.ok) return status(kNotTaken);
+    const int64_t group_k = c.number(4);
+    int64_t bytes = 0;
+    const void* weights = c.workspace(7, &bytes);
+    const Rows Y = rows_of(c, 8, m.type, m.R, m.N);
+    const int zeros = c.small(9);
+    void* stream = c.stream(12);
+    if (!c.ok || m.type == at::kFloat) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_grouped_mm_w4(m.G, m.R, m.K, m.N, element_type(m.type), group_k, zeros, m.offsets, m.X.data, m.X.ld, m.x_rows,
+                                  m.src, m.src_div, weights, bytes, Y.data, Y.ld, stream);
+    });
+}
+
 PyMethodDef kMethods[] = {
     {"spmm_csr_ex", (PyCFunction)(void (*)())spmm_csr_ex, METH_FASTCALL, nullptr},
     {"spmm_csr_cfg", (PyCFunction)(void (*)())spmm_csr_cfg, METH_FASTCALL, nullptr},
     {"sddmm_csr", (PyCFunction)(void (*)())sddmm_csr, METH_FASTCALL, nullptr},
     {"sddmm_csr_windows", (PyCFunction)(void (*)())sddmm_csr_windows, METH_FASTCALL, nullptr},
     {"mttkrp_csf_ex", (PyCFunction)(void (*)())mttkrp_csf_ex, METH_FASTCALL, nullptr},
+    {"route_topk", (PyCFunction)(void (*)())route_topk, METH_FASTCALL, nullptr},
+    {"route_topk_grad", (PyCFunction)(void (*)())route_topk_grad, METH_FASTCALL, nullptr},
+    {"route_combine", (PyCFunction)(void (*)())route_combine, METH_FASTCALL, nullptr},
+    {"route_combine_grad", (PyCFunction)(void (*)())route_combine_grad, METH_FASTCALL, nullptr},
+    {"grouped_mm", (PyCFunction)(void (*)())grouped_mm, METH_FASTCALL, nullptr},
+    {"grouped_mm_wgrad", (PyCFunction)(void (*)())grouped_mm_wgrad, METH_FASTCALL, nullptr},
+    {"grouped_mm_w4", (PyCFunction)(void (*)())grouped_mm_w4, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
