@@ -148,6 +148,10 @@ hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
 hipError_t launch_combine_grad(const CombineArgs& a, hipStream_t s);
 // dtype as in sgap.h
+// rows that are multiples of 16 bytes at 16-byte addresses (sgap_grouped_fast.hip); every other call: sgap_grouped_general.hip
+bool grouped_fast_applies(const GroupedArgs& a, int dtype);
+hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s);
+hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
 struct W4Sizes {

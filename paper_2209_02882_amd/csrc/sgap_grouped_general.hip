@@ -222,6 +222,7 @@ hipError_t wgrad(const GroupedArgs& a, hipStream_t s)
 
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s)
 {
+    if (grouped_fast_applies(a, dtype)) return launch_grouped_fast(a, dtype, s);
     switch (dtype) {
         case 0: return by_rows<float>(a, s);
         case 1: return by_rows<half_t>(a, s);
@@ -231,6 +232,7 @@ hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s)
 
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s)
 {
+    if (grouped_fast_applies(a, dtype)) return launch_grouped_wgrad_fast(a, dtype, s);
     switch (dtype) {
         case 0: return wgrad<float>(a, s);
         case 1: return wgrad<half_t>(a, s);
