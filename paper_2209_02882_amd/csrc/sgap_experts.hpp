@@ -55,14 +55,21 @@ __device__ __forceinline__ f32x4 mma16(piece_t<float> a, piece_t<float> b, f32x4
 // The rows that a product takes: row r is row src[r] / div of X, or row r itself without a list.
 struct RowSource {
     const int32_t* __restrict__ src;
-    uint32_t div;
+    uint32_t mul;  // n / div = n * mul >> shift for every n < 2^31 (shift = 31 + log2 of div, rounded up)
+    int shift;
     int64_t rows;  // rows of X; a row that lies outside counts as zeros
+    RowSource(const int32_t* src_, int64_t div, int64_t rows_) : src(src_), shift(31), rows(rows_)
+    {
+        while ((1ll << (shift - 31)) < div) ++shift;
+        // 2^shift / div, rounded up; shift is 62 at most
+        mul = (uint32_t)(((1ull << shift) + (uint64_t)div - 1) / (uint64_t)div);
+    }
     __device__ __forceinline__ int64_t row(int64_t r) const  // -1: no such row
     {
         if (!src) return r < rows ? r : -1;
         const int32_t s = src[r];
         if (s < 0) return -1;
-        const int64_t t = (uint32_t)s / div;
+        const int64_t t = (int64_t)(((uint64_t)(uint32_t)s * mul) >> shift);
         return t < rows ? t : -1;
     }
 };

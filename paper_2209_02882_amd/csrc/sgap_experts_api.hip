@@ -131,7 +131,7 @@ int sgap_grouped_mm(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, const
     if (layout != SGAP_WEIGHTS_NK && layout != SGAP_WEIGHTS_KN) return invalid("unknown layout of the weights");
     if (const int st = check_grouped(G, R, K, N, offsets, X, ldx, src, src_div, x_rows, W, Y, ldy)) return st;
     if (R == 0 || N == 0) return SGAP_OK;
-    const sgap::GroupedArgs a{G, R, K, N, offsets, {src, (uint32_t)src_div, x_rows}, X, ldx, W, Y, ldy, layout == SGAP_WEIGHTS_KN};
+    const sgap::GroupedArgs a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, W, Y, ldy, layout == SGAP_WEIGHTS_KN};
     return launched(sgap::launch_grouped_mm(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
@@ -143,7 +143,7 @@ int sgap_grouped_mm_wgrad(int64_t G, int64_t R, int64_t K, int64_t N, int dtype,
     if (layout != SGAP_WEIGHTS_NK && layout != SGAP_WEIGHTS_KN) return invalid("unknown layout of the weights");
     if (const int st = check_grouped(G, R, K, N, offsets, X, ldx, src, src_div, x_rows, dW, dY, lddy)) return st;
     if (K == 0 || N == 0) return SGAP_OK;
-    const sgap::GroupedArgs a{G, R, K, N, offsets, {src, (uint32_t)src_div, x_rows}, X, ldx, dW, const_cast<void*>(dY), lddy,
+    const sgap::GroupedArgs a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, dW, const_cast<void*>(dY), lddy,
                               layout == SGAP_WEIGHTS_KN};
     return launched(sgap::launch_grouped_wgrad(a, dtype, static_cast<hipStream_t>(stream)));
 }
@@ -193,7 +193,7 @@ int sgap_grouped_mm_w4(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, in
         return invalid("weights is smaller than sgap_w4_layout_size says");
     if (reinterpret_cast<uintptr_t>(weights) & 15) return invalid("weights must be 16-byte aligned");
     if (R == 0 || N == 0) return SGAP_OK;
-    const sgap::GroupedW4Args a{G, R, K, N, offsets, {src, (uint32_t)src_div, x_rows}, X, ldx, static_cast<const uint8_t*>(weights),
+    const sgap::GroupedW4Args a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, static_cast<const uint8_t*>(weights),
                                 (int)group_k, zeros != 0, Y, ldy};
     return launched(sgap::launch_grouped_w4(a, dtype, static_cast<hipStream_t>(stream)));
 }

@@ -42,12 +42,12 @@ __device__ __forceinline__ RowTile find_row_tile(const int32_t* __restrict__ off
         const uint64_t behind = __ballot(passed + upto > index);
         if (behind) {
             const int who = __builtin_ctzll(behind);
-            const int before = __shfl(upto - tiles, who);
-            const int first = __shfl((int)rows.first, who), end = __shfl((int)rows.end, who);
+            const int before = __builtin_amdgcn_readlane(upto - tiles, who);
+            const int first = __builtin_amdgcn_readlane((int)rows.first, who), end = __builtin_amdgcn_readlane((int)rows.end, who);
             const int64_t at = first + (index - passed - before) * BM;
             return {g0 + who, at, (int)min((int64_t)BM, end - at)};
         }
-        passed += __shfl(upto, 63);
+        passed += __builtin_amdgcn_readlane(upto, 63);
     }
     const int64_t last = group_rows(offsets, G - 1, R).end;
     const int64_t at = last + (index - passed) * BM;

@@ -1,4 +1,6 @@
 // Products over ragged groups where rows are multiples of 16 bytes at 16-byte addresses.
+#include <type_traits>
+
 #include "sgap_grouped_tiles.hpp"
 
 namespace sgap {
@@ -13,7 +15,8 @@ __device__ __forceinline__ int64_t dealt_item(uint32_t b)
     return (int64_t)((at >> 5) * 8 + die) * 32 + (at & 31);
 }
 
-template <typename T, int BM, int BN, bool KN, int THREADS>
+// WIDE: rows of X lie further than 32 bits of bytes from its first.
+template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
 __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, int64_t column_tiles, int64_t items)
 {
     using Wt = Tile<T, BN, !KN, THREADS>;
@@ -21,7 +24,6 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
     constexpr int kWaves = THREADS / 64, WN = kWaves / 2, WM = 2;
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kStage = Wt::kBytes + Xt::kBytes;
     const int64_t item = dealt_item(blockIdx.x);
     if (item >= items) return;
     const int64_t tile = item / column_tiles, n0 = (item - tile * column_tiles) * BN;
@@ -29,67 +31,68 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
     if (rows.rows <= 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wn = (wave % WN) * (BN / WN), wm = (wave / WN) * (BM / WM);
+    const bool active = rows.g < a.G && wm < rows.rows;
     f32x4 acc[MI][NJ];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const T* const zero = reinterpret_cast<const T*>(g_zero_piece);
     if (rows.g < a.G) {
-        const T* const W = static_cast<const T*>(a.W) + rows.g * a.N * a.K;
-        const T* wp[Wt::kRounds];
-        const T* xp[Xt::kRounds];
+        // columns and rows past the last are read from the last, and not stored; a row of X that does not exist is read
+        // from row 0, and zeros are stored
+        const char* const W = uniform(reinterpret_cast<const char*>(static_cast<const T*>(a.W) + rows.g * a.N * a.K + (KN ? n0 : n0 * a.K)));
+        const char* const X = static_cast<const char*>(a.X);
+        uint32_t wo[Wt::kRounds];
+        uint32_t xo[Xt::kRounds];
+        const char* xp[Xt::kRounds];
 #pragma unroll
         for (int i = 0; i < Wt::kRounds; ++i) {
-            if constexpr (!KN) {
-                const int64_t n = min(n0 + Wt::major(i), a.N - 1);  // columns past the last are not stored
-                wp[i] = W + n * a.K + Wt::minor(i) * Wt::P;
-            } else {
-                wp[i] = W + (int64_t)Wt::major(i) * a.N + min(n0 + Wt::minor(i) * Wt::P, a.N - Wt::P);
-            }
+            if constexpr (!KN) wo[i] = (uint32_t)((min((int64_t)Wt::major(i), a.N - 1 - n0) * a.K + Wt::minor(i) * Wt::P) * sizeof(T));
+            else wo[i] = (uint32_t)((Wt::major(i) * a.N + min((int64_t)Wt::minor(i) * Wt::P, a.N - Wt::P - n0)) * sizeof(T));
         }
 #pragma unroll
         for (int i = 0; i < Xt::kRounds; ++i) {
-            const int m = Xt::major(i);
-            const int64_t r = m < rows.rows ? a.from.row(rows.first + m) : -1;
-            xp[i] = r >= 0 ? static_cast<const T*>(a.X) + r * a.ldx + Xt::minor(i) * Xt::P : nullptr;
+            int64_t r = a.from.row(rows.first + min(Xt::major(i), rows.rows - 1));
+            r = ((r < 0 ? 0 : r) * a.ldx + Xt::minor(i) * Xt::P) * (int64_t)sizeof(T);
+            if constexpr (WIDE) xp[i] = X + r;
+            else xo[i] = (uint32_t)r;
         }
         const int tiles = (int)((a.K + Wt::kInner - 1) / Wt::kInner);
-        const auto load = [&](int t, char* to) {
+        // inner values that tile t has
+        const auto left = [&](int t) { return (int)min((int64_t)Wt::kInner, a.K - (int64_t)t * Wt::kInner); };
+        const auto load = [&](int t, uint32_t to, int i) {
             const int64_t k0 = (int64_t)t * Wt::kInner;
-#pragma unroll
-            for (int i = 0; i < Wt::kRounds; ++i) {
-                if constexpr (!KN) Wt::load(to, i, k0 + Wt::minor(i) * Wt::P < a.K ? wp[i] + k0 : zero);
-                else Wt::load(to, i, k0 + Wt::major(i) < a.K ? wp[i] + k0 * a.N : zero);
+            if (i < Wt::kRounds) {
+                const char* const w = uniform(W + (KN ? k0 * a.N : k0) * (int64_t)sizeof(T));
+                const bool there = (KN ? Wt::major(i) : Wt::minor(i) * Wt::P) < left(t);
+                // the tile's first inner values are there
+                const uint32_t first = KN ? wo[i] - Wt::major(i) * (uint32_t)(a.N * sizeof(T)) : wo[i] - Wt::minor(i) * 16u;
+                Wt::load(to, i, w, there ? wo[i] : first);
+            } else {
+                const int r = i - Wt::kRounds;
+                const int64_t x = k0 * (int64_t)sizeof(T);
+                const uint32_t back = Xt::minor(r) * Xt::P < left(t) ? 0u : Xt::minor(r) * 16u;
+                if constexpr (WIDE) Xt::load(to + Wt::kBytes, r, xp[r] + x - back);
+                else Xt::load(to + Wt::kBytes, r, uniform(X + x), xo[r] - back);
             }
+        };
+        const auto mend = [&](int t, uint32_t to) {
+            const int there = left(t);
+            if (there == Wt::kInner) return;
+#pragma unroll
+            for (int i = 0; i < Wt::kRounds; ++i)
+                if ((KN ? Wt::major(i) : Wt::minor(i) * Wt::P) >= there) Wt::clear(to, i);
 #pragma unroll
             for (int i = 0; i < Xt::kRounds; ++i)
-                Xt::load(to + Wt::kBytes, i, xp[i] && k0 + Xt::minor(i) * Xt::P < a.K ? xp[i] + k0 : zero);
+                if (Xt::minor(i) * Xt::P >= there) Xt::clear(to + Wt::kBytes, i);
         };
-        load(0, lds);
-        for (int t = 0; t < tiles; ++t) {
-            const char* const at = lds + (t & 1) * kStage;
-            wait_loads<0>();
-            __syncthreads();
-            if (t + 1 < tiles) load(t + 1, lds + ((t + 1) & 1) * kStage);
-#pragma unroll
-            for (int kc = 0; kc < 2; ++kc) {
-                piece_t<T> fw[MI], fx[NJ];
-#pragma unroll
-                for (int i = 0; i < MI; ++i) fw[i] = Wt::fragment(at, wn + 16 * i, kc);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) fx[j] = Xt::fragment(at + Wt::kBytes, wm + 16 * j, kc);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int i = 0; i < MI; ++i) acc[i][j] = mma16(fw[i], fx[j], acc[i][j]);
-            }
-        }
+        multiply_tiles<Wt, Xt, MI, NJ>(lds, tiles, load, mend, wn, wm, active, acc);
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
         const int m = wm + 16 * j + (lane & 15);
         if (m >= rows.rows) continue;
+        const bool real = rows.g < a.G && (!a.from.src || a.from.row(rows.first + m) >= 0);
         T* __restrict__ y = static_cast<T*>(a.Y) + (rows.first + m) * a.ldy;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
@@ -98,29 +101,32 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
             if (n < a.N) {
                 out4 o;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) o[r] = (T)acc[i][j][r];
+                for (int r = 0; r < 4; ++r) o[r] = (T)(real ? acc[i][j][r] : 0.0f);
                 *reinterpret_cast<out4*>(y + n) = o;
             }
         }
     }
 }
 
-// The gradient of the weights.  The inner dimension is the group's rows; both operands have their lines contiguous.
-// lines of the first: the result's contiguous dimension.
-template <typename T, int BM, int BN, bool KN, int THREADS>
+// The gradient of the weights.  The inner dimension is the group's rows; both operands have their lines contiguous, and
+// the first has the result's contiguous dimension.
+template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
 __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n, int64_t items)
 {
     using Lt = Tile<T, BN, false, THREADS>;
     using Rt = Tile<T, BM, false, THREADS>;
+    using Xt = std::conditional_t<KN, Rt, Lt>;
+    using Yt = std::conditional_t<KN, Lt, Rt>;
     constexpr int kWaves = THREADS / 64, WN = kWaves / 2, WM = 2;
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
+    constexpr int kXAt = KN ? Lt::kBytes : 0, kYAt = KN ? 0 : Lt::kBytes;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kStage = Lt::kBytes + Rt::kBytes;
     const int64_t item = dealt_item(blockIdx.x);
     if (item >= items) return;
     const int64_t per = tiles_m * tiles_n, g = item / per, in = item - g * per;
     const int64_t lines = KN ? a.K : a.N, columns = KN ? a.N : a.K;  // of the result
     const int64_t m0 = in / tiles_n * BM, n0 = in % tiles_n * BN;
+    const int64_t x0 = KN ? m0 : n0, y0 = KN ? n0 : m0;
     const GroupRows gr = group_rows(a.offsets, g, a.R);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wn = (wave % WN) * (BN / WN), wm = (wave / WN) * (BM / WM);
@@ -129,42 +135,70 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const T* const zero = reinterpret_cast<const T*>(g_zero_piece);
-    const T* const X = static_cast<const T*>(a.X);
-    const T* const dY = static_cast<const T*>(a.Y);
-    const auto piece = [&](bool of_x, int64_t r, int64_t line) -> const T* {
-        if (r >= gr.end) return zero;
-        if (!of_x) return dY + r * a.ldy + min(line, a.N - Lt::P);
-        const int64_t s = a.from.row(r);
-        return s < 0 ? zero : X + s * a.ldx + min(line, a.K - Lt::P);
-    };
-    const auto load = [&](int64_t r0, char* to) {
+    const char* const X = uniform(reinterpret_cast<const char*>(static_cast<const T*>(a.X) + x0));
+    const char* const dY = reinterpret_cast<const char*>(static_cast<const T*>(a.Y) + gr.first * a.ldy + y0);
+    // The rounds of a load are so many rows apart, and rows 16 apart have their pieces in the same places: one offset of
+    // the lines serves all rounds, or two those of floats, which are 8 rows apart.
+    constexpr int kRowsApart = THREADS / Yt::kAcross, kXRowsApart = THREADS / Xt::kAcross;
+    constexpr int kYKinds = kRowsApart % 16 ? 2 : 1, kXKinds = kXRowsApart % 16 ? 2 : 1;
+    static_assert(kRowsApart % 8 == 0 && kXRowsApart % 8 == 0, "");
+    uint32_t yo[kYKinds], xc[kXKinds];
 #pragma unroll
-        for (int i = 0; i < Lt::kRounds; ++i) Lt::load(to, i, piece(!KN, r0 + Lt::major(i), n0 + Lt::minor(i) * Lt::P));
+    for (int i = 0; i < kYKinds; ++i)
+        yo[i] = (uint32_t)((Yt::major(0) * a.ldy + min((int64_t)Yt::minor(i) * Yt::P, a.N - Yt::P - y0)) * sizeof(T));
 #pragma unroll
-        for (int i = 0; i < Rt::kRounds; ++i)
-            Rt::load(to + Lt::kBytes, i, piece(KN, r0 + Rt::major(i), m0 + Rt::minor(i) * Rt::P));
-    };
-    const int tiles = (int)((gr.end - gr.first + Lt::kInner - 1) / Lt::kInner);
-    if (tiles) load(gr.first, lds);
-    for (int t = 0; t < tiles; ++t) {
-        const char* const at = lds + (t & 1) * kStage;
-        wait_loads<0>();
-        __syncthreads();
-        if (t + 1 < tiles) load(gr.first + (int64_t)(t + 1) * Lt::kInner, lds + ((t + 1) & 1) * kStage);
+    for (int i = 0; i < kXKinds; ++i) xc[i] = (uint32_t)(min((int64_t)Xt::minor(i) * Xt::P, a.K - Xt::P - x0) * sizeof(T));
+    const int first = __builtin_amdgcn_readfirstlane((int)gr.first), end = __builtin_amdgcn_readfirstlane((int)gr.end);
+    // Rows of X of the tile that is loaded next (found while the tile before is on its way), -1 where there is none; which
+    // rounds had none in the last two tiles, a bit each.
+    int32_t row[Xt::kRounds];
+    uint32_t none[2] = {0, 0};
+    int next = first + Xt::major(0);
+    const auto find = [&] {
 #pragma unroll
-        for (int kc = 0; kc < 2; ++kc) {
-            piece_t<T> fl[MI], fr[NJ];
-#pragma unroll
-            for (int i = 0; i < MI; ++i) fl[i] = Lt::fragment(at, wn + 16 * i, kc);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) fr[j] = Rt::fragment(at + Lt::kBytes, wm + 16 * j, kc);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int i = 0; i < MI; ++i) acc[i][j] = mma16(fl[i], fr[j], acc[i][j]);
+        for (int i = 0; i < Xt::kRounds; ++i) {
+            const int r = next + i * kXRowsApart;
+            row[i] = r < end ? (int32_t)a.from.row(r) : -1;
         }
-    }
+        next += Xt::kInner;
+    };
+    const auto load = [&](int t, uint32_t to, int i) {
+        if (i < Yt::kRounds) {
+            const int r = i * kRowsApart, r0 = t * Yt::kInner + r;
+            // in place of a row past the last, the one that is the first of the tile
+            const bool there = first + r0 + Yt::major(0) < end;
+            const char* const y = uniform(dY + (int64_t)(t * Yt::kInner) * a.ldy * (int64_t)sizeof(T));
+            const uint32_t down = (uint32_t)(a.ldy * sizeof(T));
+            Yt::load(to + kYAt, i, y, there ? yo[i % kYKinds] + r * down : yo[i % kYKinds] - Yt::major(0) * down);
+        } else {
+            const int x = i - Yt::kRounds;
+            const int32_t r = max(row[x], 0);
+            none[1] = x == 0 ? 0 : none[1];
+            none[1] |= row[x] < 0 ? 1u << x : 0u;
+            if constexpr (WIDE) Xt::load(to + kXAt, x, X + r * a.ldx * (int64_t)sizeof(T) + xc[x % kXKinds]);
+            else Xt::load(to + kXAt, x, X, (uint32_t)r * (uint32_t)(a.ldx * sizeof(T)) + xc[x % kXKinds]);
+            if (x == Xt::kRounds - 1) find();
+        }
+    };
+    const auto mend = [&](int t, uint32_t to) {
+        const int left = end - first - t * Yt::kInner;
+        if (left < Yt::kInner) {
+#pragma unroll
+            for (int i = 0; i < Yt::kRounds; ++i)
+                if (Yt::major(0) + i * kRowsApart >= left) Yt::clear(to + kYAt, i);
+        }
+        const uint32_t missing = t == 0 ? none[0] : none[1];
+        if (__any(missing != 0)) {
+#pragma unroll
+            for (int i = 0; i < Xt::kRounds; ++i)
+                if (missing >> i & 1) Xt::clear(to + kXAt, i);
+        }
+    };
+    const int tiles = (end - first + Lt::kInner - 1) / Lt::kInner;
+    find();
+#pragma unroll
+    for (int i = 0; i < Xt::kRounds; ++i) none[0] |= row[i] < 0 ? 1u << i : 0u;
+    multiply_tiles<Lt, Rt, MI, NJ>(lds, tiles, load, mend, wn, wm, true, acc);
     T* __restrict__ dW = static_cast<T*>(const_cast<void*>(a.W)) + g * a.N * a.K;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -198,42 +232,64 @@ hipError_t allow_lds(K kernel, int bytes, uint64_t& allowed)
 
 unsigned dealt_grid(int64_t items) { return (unsigned)((items + 255) / 256 * 256); }
 
-template <typename T, int BM, int BN, bool KN, int THREADS>
+template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
 hipError_t run_fast(const GroupedArgs& a, hipStream_t s)
 {
     const int64_t columns = (a.N + BN - 1) / BN, items = columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr);
     if (items > 0x7fffff00LL) return hipErrorInvalidConfiguration;
     constexpr int kLds = 2 * 128 * (BM + BN);
     static uint64_t allowed = 0;
-    if (const hipError_t err = allow_lds(grouped_fast_kernel<T, BM, BN, KN, THREADS>, kLds, allowed)) return err;
-    grouped_fast_kernel<T, BM, BN, KN, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, columns, items);
+    if (const hipError_t err = allow_lds(grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS>, kLds, allowed)) return err;
+    grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, columns, items);
     return hipGetLastError();
 }
 
-template <typename T, int BM, int BN, bool KN, int THREADS>
+template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
 hipError_t run_wgrad_fast(const GroupedArgs& a, hipStream_t s)
 {
     const int64_t tm = ((KN ? a.K : a.N) + BM - 1) / BM, tn = ((KN ? a.N : a.K) + BN - 1) / BN, items = a.G * tm * tn;
     if (items > 0x7fffff00LL) return hipErrorInvalidConfiguration;
     constexpr int kLds = 2 * 128 * (BM + BN);
     static uint64_t allowed = 0;
-    if (const hipError_t err = allow_lds(grouped_wgrad_fast_kernel<T, BM, BN, KN, THREADS>, kLds, allowed)) return err;
-    grouped_wgrad_fast_kernel<T, BM, BN, KN, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, tm, tn, items);
+    if (const hipError_t err = allow_lds(grouped_wgrad_fast_kernel<T, BM, BN, KN, WIDE, THREADS>, kLds, allowed)) return err;
+    grouped_wgrad_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, tm, tn, items);
     return hipGetLastError();
 }
 
-template <typename T, bool KN>
+template <typename T, bool KN, bool WIDE>
 hipError_t by_size(const GroupedArgs& a, hipStream_t s)
 {
-    if (a.R >= 192 * a.G) return run_fast<T, 256, 256, KN, 512>(a, s);
-    return run_fast<T, 128, 128, KN, 256>(a, s);
+    if (a.R >= 192 * a.G) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    return run_fast<T, 128, 128, KN, WIDE, 256>(a, s);
 }
 
-template <typename T, bool KN>
+template <typename T, bool KN, bool WIDE>
 hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
 {
-    if (a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 128) return run_wgrad_fast<T, 256, 256, KN, 512>(a, s);
-    return run_wgrad_fast<T, 128, 128, KN, 256>(a, s);
+    if (a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 128) return run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    return run_wgrad_fast<T, 128, 128, KN, WIDE, 256>(a, s);
+}
+
+template <typename T>
+hipError_t by_layout(const GroupedArgs& a, bool gradient, hipStream_t s)
+{
+    // bytes of X from its first row to the end of its last
+    const bool wide = a.from.rows * a.ldx * (int64_t)sizeof(T) > 0xffffffffLL;
+    if (gradient) {
+        if (wide) return a.weights_kn ? wgrad_by_size<T, true, true>(a, s) : wgrad_by_size<T, false, true>(a, s);
+        return a.weights_kn ? wgrad_by_size<T, true, false>(a, s) : wgrad_by_size<T, false, false>(a, s);
+    }
+    if (wide) return a.weights_kn ? by_size<T, true, true>(a, s) : by_size<T, false, true>(a, s);
+    return a.weights_kn ? by_size<T, true, false>(a, s) : by_size<T, false, false>(a, s);
+}
+
+hipError_t by_type(const GroupedArgs& a, int dtype, bool gradient, hipStream_t s)
+{
+    switch (dtype) {
+        case 0: return by_layout<float>(a, gradient, s);
+        case 1: return by_layout<half_t>(a, gradient, s);
+        default: return by_layout<bf16_t>(a, gradient, s);
+    }
 }
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -243,26 +299,13 @@ bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 bool grouped_fast_applies(const GroupedArgs& a, int dtype)
 {
     const int64_t piece = dtype == 0 ? 4 : 8;
-    return a.K > 0 && a.K % piece == 0 && a.N % piece == 0 && a.ldx % piece == 0 && a.ldy % piece == 0 && a.from.rows > 0 &&
+    // 256 lines of an operand have to lie within 32 bits of bytes
+    constexpr int64_t kLongest = 1 << 22;
+    return a.K > 0 && a.K <= kLongest && a.N <= kLongest && a.ldx <= kLongest && a.ldy <= kLongest && a.K % piece == 0 && a.N % piece == 0 && a.ldx % piece == 0 && a.ldy % piece == 0 && a.from.rows > 0 &&
            aligned(a.X) && aligned(a.W) && aligned(a.Y);
 }
 
-hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s)
-{
-    switch (dtype) {
-        case 0: return a.weights_kn ? by_size<float, true>(a, s) : by_size<float, false>(a, s);
-        case 1: return a.weights_kn ? by_size<half_t, true>(a, s) : by_size<half_t, false>(a, s);
-        default: return a.weights_kn ? by_size<bf16_t, true>(a, s) : by_size<bf16_t, false>(a, s);
-    }
-}
-
-hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s)
-{
-    switch (dtype) {
-        case 0: return a.weights_kn ? wgrad_by_size<float, true>(a, s) : wgrad_by_size<float, false>(a, s);
-        case 1: return a.weights_kn ? wgrad_by_size<half_t, true>(a, s) : wgrad_by_size<half_t, false>(a, s);
-        default: return a.weights_kn ? wgrad_by_size<bf16_t, true>(a, s) : wgrad_by_size<bf16_t, false>(a, s);
-    }
-}
+hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s) { return by_type(a, dtype, false, s); }
+hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s) { return by_type(a, dtype, true, s); }
 
 }  // namespace sgap

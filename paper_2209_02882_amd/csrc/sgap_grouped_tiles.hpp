@@ -7,21 +7,30 @@
 //                     places are rotated by the row's number, so that the rows that lanes read together lie apart.  16-bit
 //                     values are turned by the LDS itself on the way out (four inner values of sixteen lines at a time),
 //                     floats are read one by one.
-// The loads write LDS in the order of the lanes, so it is the addresses they read from that are rotated.  A piece that
-// does not exist (inner values past the end, rows that are not there) is read from 16 bytes of zeros.
+// The loads write LDS in the order of the lanes, so it is the addresses they read from that are rotated.  In place of a
+// piece that does not exist (inner values past the end, rows that are not there) a lane reads one that does, and writes
+// zeros over it when it has arrived.
 #pragma once
 #include "sgap_grouped.hpp"
 
 namespace sgap {
 
-// what pieces that do not exist are read from
-static __device__ __align__(16) const uint32_t g_zero_piece[4] = {0, 0, 0, 0};
+// The same in every lane of the wavefront, in scalar registers.
+template <typename P>
+__device__ __forceinline__ const P* uniform(const P* p)
+{
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (const P*)(uintptr_t)((uint64_t)hi << 32 | lo);
+}
 
-// Until at most LEFT of this wavefront's loads are still on their way; to the compiler, nothing moves across.
-template <int LEFT>
+// Until none of this wavefront's loads is on its way; to the compiler, nothing moves across.  (The builtin tells it that
+// its own loads have arrived as well: vmcnt 0, the other counters as they are.)
 __device__ __forceinline__ void wait_loads()
 {
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(LEFT) : "memory");
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 }
 
 template <typename T, int LINES, bool INNER, int THREADS>
@@ -49,45 +58,163 @@ struct Tile {
 
     // In the assembler's words, because the compiler, which cannot tell the stage that is being filled from the one that is
     // read, would wait for every load before the next read.  They count as vector memory loads: wait_loads().
-    static __device__ __forceinline__ void load(char* lds, int round, const T* from)
+    // `lds`: the tile's LDS address; the wavefront's lanes fill 1,024 consecutive bytes of it a round.
+    static __device__ __forceinline__ uint32_t place(uint32_t lds, int round)
     {
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds + (round * THREADS + wave * 64) * 16);
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        return lds + (round * THREADS + wave * 64) * 16;
+    }
+    static __device__ __forceinline__ void load(uint32_t lds, int round, const void* base, uint32_t offset)  // base: the wavefront's
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                      :
-                     : "s"(__builtin_amdgcn_readfirstlane(to)), "v"(from)
+                     : "s"(place(lds, round)), "v"(offset), "s"(base)
                      : "m0", "memory");
     }
+    static __device__ __forceinline__ void load(uint32_t lds, int round, const void* from)
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                     :
+                     : "s"(place(lds, round)), "v"(from)
+                     : "m0", "memory");
+    }
+    // zeros in the place that this lane's load would fill
+    static __device__ __forceinline__ void clear(uint32_t lds, int round)
+    {
+        typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
+        *(lds_piece*)(uintptr_t)(lds + (round * THREADS + threadIdx.x) * 16) = piece_t<T>{};
+    }
 
-    // lanes' pieces of lines line0 .. line0 + 16, inner values of step kc of 2
-    static __device__ __forceinline__ piece_t<T> fragment(const char* lds, int line0, int kc)
+    // Where in a tile this lane's fragments begin, for the lines from line0 (a multiple of 64) on.
+    static __device__ __forceinline__ uint32_t lane_base(int line0)
     {
         const int lane = threadIdx.x & 63, row = lane & 15, part = lane >> 4;
+        if constexpr (INNER) return (uint32_t)((line0 + row) * 128 + ((part ^ (row & 7)) << 4));
+        const int chunk = line0 >> 4;
+        if constexpr (sizeof(T) == 2) {
+            const int k = part * 8 + (row >> 2);  // this lane's row of the four that are turned together; four rows on: the same turn
+            return (uint32_t)(k * (LINES * 2) + (chunk >> 3) * 256 + (((chunk & 7) ^ turn(k)) << 5) + (row & 3) * 8);
+        }
+        const int k = part * 4;
+        return (uint32_t)(k * (LINES * 4) + (chunk >> 2) * 256 + (turn(k) << 6) + row * 4);
+    }
+
+    // Lanes' pieces of the sixteen lines number i behind lane_base's, inner values of step kc of 2.  `base`: the LDS address.
+    static __device__ __forceinline__ piece_t<T> fragment(uint32_t base, int i, int kc)
+    {
+        typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
         if constexpr (INNER) {
-            const int line = line0 + row;
-            return *reinterpret_cast<const piece_t<T>*>(lds + line * 128 + (((kc * 4 + part) ^ (line & 7)) << 4));
+            return *(const lds_piece*)(uintptr_t)((base ^ (kc << 6)) + i * 2048);
         } else if constexpr (sizeof(T) == 2) {
             typedef short short4_t __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) short4_t lds_short4;
             union {
                 short4_t h[2];
                 piece_t<T> v;
             } r;
-            const int k = kc * 32 + part * 8 + (row >> 2);  // this lane's row of four, and four rows on
-            const int chunk = line0 >> 4, within = (row & 3) * 8;
+            const uint32_t at = (base ^ ((i & 7) << 5)) + (i >> 3) * 256 + kc * (32 * LINES * 2);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                r.h[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)(
-                    lds + (k + 4 * i) * (LINES * 2) + ((chunk ^ turn(k + 4 * i)) << 5) + within));
+            for (int h = 0; h < 2; ++h)
+                r.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(uintptr_t)(at + h * (4 * LINES * 2)));
             return r.v;
         } else {
+            typedef __attribute__((address_space(3))) float lds_float;
             piece_t<T> v;
-            const int k = kc * 16 + part * 4, chunk = line0 >> 4;
+            const uint32_t at = (base ^ ((i & 3) << 6)) + (i >> 2) * 256 + kc * (16 * LINES * 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[i] = *reinterpret_cast<const float*>(lds + (k + i) * (LINES * 4) + ((chunk ^ turn(k)) << 6) + row * 4);
+            for (int h = 0; h < 4; ++h) v[h] = *(const lds_float*)(uintptr_t)(at + h * (LINES * 4));
             return v;
         }
     }
 };
+
+// acc += first x second over `tiles` tiles of the inner dimension.  Two stages: the loads of a tile have the whole of the
+// one before to arrive in, the fragments of a half tile the products of the half before, so that the matrix unit waits for
+// neither; one barrier a tile, in its middle, says that everyone has read the stage that is filled next and that the other
+// stage is full.  Loads, fragments and products are dealt out evenly (the compiler by itself puts all fragments behind the
+// products, and then waits).
+//   load(t, stage, i)   starts load i of LOADS of tile t; every lane reads something that is there
+//   mend(t, stage)      after tile t's loads have arrived: zeros where a lane had nothing to read
+// ACTIVE: this wavefront has products to make.
+template <typename L, typename R, int MI, int NJ, bool ACTIVE, typename F, typename M>
+__device__ __forceinline__ void multiply_tiles_as(uint32_t lds, int tiles, F&& load, M&& mend, int l0, int r0, f32x4 (&acc)[MI][NJ])
+{
+    constexpr uint32_t kStage = L::kBytes + R::kBytes;
+    constexpr int kLoads = L::kRounds + R::kRounds;
+    using frag = decltype(L::fragment(0u, 0, 0));
+    frag fl[2][MI], fr[2][NJ];
+    const uint32_t lbase = lds + L::lane_base(l0), rbase = lds + L::kBytes + R::lane_base(r0);
+    uint32_t lb, rb;
+    const auto at = [&](uint32_t stage) {
+        lb = lbase + stage, rb = rbase + stage;
+        asm volatile("" : "+v"(lb), "+v"(rb));  // the fragments' addresses are made anew each time, not kept in registers
+    };
+    const auto read = [&](int kc, int i) {
+        if (i < MI) fl[kc][i] = L::fragment(lb, i, kc);
+        else fr[kc][i - MI] = R::fragment(rb, i - MI, kc);
+    };
+    // the products of one half, with the reads of the next and, if any, the loads of a tile between them
+    const auto half = [&](int kc, auto&& between) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            between(j);
+            if constexpr (ACTIVE) {
+#pragma unroll
+                for (int i = j * (MI + NJ) / NJ; i < (j + 1) * (MI + NJ) / NJ; ++i) read(1 - kc, i);
+#pragma unroll
+                for (int i = 0; i < MI; ++i) acc[i][j] = mma16(fl[kc][i], fr[kc][j], acc[i][j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const auto meet = [&](int t) {
+        wait_loads();
+        if (t < tiles) mend(t, lds + (t & 1) * kStage);
+        __syncthreads();
+    };
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(0, lds, i);
+    if (tiles > 1) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(1, lds + kStage, i);
+    }
+    wait_loads();
+    mend(0, lds);
+    __syncthreads();
+    at(0);
+    if constexpr (ACTIVE) {
+#pragma unroll
+        for (int i = 0; i < MI + NJ; ++i) read(0, i);
+    }
+    int t = 0;
+    for (; t + 2 < tiles; ++t) {
+        const uint32_t stage = (t & 1) * kStage;
+        at(stage);
+        half(0, [](int) {});
+        meet(t + 1);
+        at(kStage - stage);
+        half(1, [&](int j) {
+#pragma unroll
+            for (int i = j * kLoads / NJ; i < (j + 1) * kLoads / NJ; ++i) load(t + 2, lds + stage, i);
+        });
+    }
+    for (; t < tiles; ++t) {
+        const uint32_t stage = (t & 1) * kStage;
+        at(stage);
+        half(0, [](int) {});
+        meet(t + 1);
+        at(kStage - stage);
+        half(1, [](int) {});  // behind the last tile the fragments that are read are not used
+    }
+}
+template <typename L, typename R, int MI, int NJ, typename F, typename M>
+__device__ __forceinline__ void multiply_tiles(char* shared, int tiles, F&& load, M&& mend, int l0, int r0, bool active,
+                                               f32x4 (&acc)[MI][NJ])
+{
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)shared;
+    if (tiles == 0) return;
+    if (active) multiply_tiles_as<L, R, MI, NJ, true>(lds, tiles, load, mend, l0, r0, acc);
+    else multiply_tiles_as<L, R, MI, NJ, false>(lds, tiles, load, mend, l0, r0, acc);
+}
 
 }  // namespace sgap
