@@ -259,14 +259,14 @@ hipError_t run_wgrad_fast(const GroupedArgs& a, hipStream_t s)
 template <typename T, bool KN, bool WIDE>
 hipError_t by_size(const GroupedArgs& a, hipStream_t s)
 {
-    if (a.R >= 192 * a.G) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    if (sizeof(T) == 2 && a.R >= 192 * a.G && (a.R / 256 + a.G / 2) * ((a.N + 255) / 256) >= 192) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
     return run_fast<T, 128, 128, KN, WIDE, 256>(a, s);
 }
 
 template <typename T, bool KN, bool WIDE>
 hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
 {
-    if (a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 128) return run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    if (sizeof(T) == 2 && a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 192) return run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s);
     return run_wgrad_fast<T, 128, 128, KN, WIDE, 256>(a, s);
 }
 

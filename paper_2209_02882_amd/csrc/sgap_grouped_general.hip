@@ -1,110 +1,58 @@
 // Products over ragged groups, for every shape, layout and alignment:
 //   Y[r, :]  = X[src(r), :] * op(W[g])              r in group g; W[g] is N x K or K x N
 //   dW[g]    = sum over the rows r of g of dY[r, :] (x) X[src(r), :]
-// Both are C = A * B^T over tiles of 128 bytes of the inner dimension, kept in LDS row by row with their 16-byte pieces
-// rotated (piece p of row r lies at p ^ (r & 7)), so that sixteen lanes reading one piece of sixteen rows meet in no bank.
-// An operand whose inner dimension is not the contiguous one is turned while it is put into LDS, element by element.
-// Sums in 32 bits, rounded once when they are stored.
-#include "sgap_grouped.hpp"
+// Tiles go through registers into LDS, so that rows may begin at any element; inner values past the end and rows that do
+// not exist become zeros on the way.  Sums in 32 bits, rounded once when they are stored.
+#include "sgap_grouped_tiles.hpp"
 
 namespace sgap {
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRowBytes = 128;  // inner bytes of a tile
 
-// One operand: `lines` rows of it (columns of the result or rows), `inner` values each.
-// INNER: the inner dimension is contiguous, line l starts at ptr(l); else inner value k starts at ptr(k) and the lines lie
-// side by side.  `at(i)` gives the row number that is multiplied by ld: -1 for a row of zeros.
-template <typename T, int LINES, bool INNER, bool WHOLE, typename RowAt>
-__device__ __forceinline__ void stage(T* lds, const T* __restrict__ base, int64_t ld, int64_t line0, int lines, int64_t k0,
-                                      int64_t K, RowAt&& at)
+// The 16 bytes at p, of which `count` elements are there (all of them, or fewer: one by one).
+template <typename T>
+__device__ __forceinline__ piece_t<T> part_of_piece(const T* __restrict__ p, int64_t count)
 {
-    constexpr int P = Piece<T>::kCount, kTileK = kRowBytes / (int)sizeof(T);
-    const int tid = threadIdx.x;
-    if constexpr (INNER) {
-        const int piece = tid & 7;
+    if (count >= Piece<T>::kCount) return load_piece(p);
+    piece_t<T> v = {};
 #pragma unroll
-        for (int i = 0; i < LINES / 32; ++i) {
-            const int line = (tid >> 3) + 32 * i;
-            const int64_t k = k0 + piece * P;
-            piece_t<T> v = {};
-            const int64_t row = line < lines ? at(line0 + line) : -1;
-            if (row >= 0) {
-                const T* __restrict__ p = base + row * ld + k;
-                if (WHOLE || k + P <= K) {
-                    if (k < K) v = load_piece(p);
-                } else {
+    for (int j = 0; j < Piece<T>::kCount; ++j)
+        if (j < count) v[j] = p[j];
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_four(T* __restrict__ p, f32x4 v, int64_t count)
+{
+    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    if (count >= 4) {
+        four o;
 #pragma unroll
-                    for (int j = 0; j < P; ++j)
-                        if (k + j < K) v[j] = p[j];
-                }
-            }
-            *reinterpret_cast<piece_t<T>*>(lds + line * kTileK + ((piece ^ (line & 7)) * P)) = v;
-        }
+        for (int r = 0; r < 4; ++r) o[r] = (T)v[r];
+        *reinterpret_cast<four*>(p) = o;
     } else {
-        constexpr int kAcross = LINES / P;  // pieces side by side
 #pragma unroll
-        for (int i = 0; i < kTileK * kAcross / kThreads; ++i) {
-            const int id = tid + kThreads * i;
-            const int kk = id / kAcross, line = (id % kAcross) * P;
-            const int64_t k = k0 + kk;
-            piece_t<T> v = {};
-            const int64_t row = k < K ? at(k) : -1;
-            if (row >= 0) {
-                const T* __restrict__ p = base + row * ld + line0 + line;
-                if (line + P <= lines) {
-                    v = load_piece(p);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < P; ++j)
-                        if (line + j < lines) v[j] = p[j];
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                const int l = line + j;
-                lds[l * kTileK + (((kk / P) ^ (l & 7)) * P) + kk % P] = v[j];
-            }
-        }
+        for (int r = 0; r < 4; ++r)
+            if (r < count) p[r] = (T)v[r];
     }
 }
 
-// acc[i][j] += (A lines 16 i ..) x (B lines 16 j ..) over the tile in LDS
-template <typename T, int MI, int NJ>
-__device__ __forceinline__ void multiply(const T* a, const T* b, f32x4 (&acc)[MI][NJ])
-{
-    constexpr int P = Piece<T>::kCount, kTileK = kRowBytes / (int)sizeof(T);
-    const int lane = threadIdx.x & 63, row = lane & 15, part = lane >> 4;
-#pragma unroll
-    for (int kc = 0; kc < 2; ++kc) {
-        const int at = ((kc * 4 + part) ^ (row & 7)) * P;
-        piece_t<T> fa[MI], fb[NJ];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) fa[i] = *reinterpret_cast<const piece_t<T>*>(a + (16 * i + row) * kTileK + at);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) fb[j] = *reinterpret_cast<const piece_t<T>*>(b + (16 * j + row) * kTileK + at);
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] = mma16(fa[i], fb[j], acc[i][j]);
-    }
-}
-
-// A tile of BN columns (A, the weights) by BM rows (B): a lane ends up with four neighbouring columns of one row.
+// A tile of 128 columns (the weights) by BM rows: a lane ends up with four neighbouring columns of one row.
 template <typename T, int BM, bool KN>
 __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a, int64_t column_tiles)
 {
-    constexpr int BN = 128, kTileK = kRowBytes / (int)sizeof(T);
+    constexpr int BN = 128;
+    using Wt = Tile<T, BN, !KN, kThreads>;
+    using Xt = Tile<T, BM, true, kThreads>;
     constexpr int WN = BM >= 128 ? 2 : 4, WM = 4 / WN;  // wavefronts along the columns and the rows
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
-    __shared__ __align__(16) T wt[BN * kTileK];
-    __shared__ __align__(16) T xt[BM * kTileK];
+    __shared__ __align__(16) char lds[2 * (Wt::kBytes + Xt::kBytes)];
     const int64_t tile = blockIdx.x / column_tiles, n0 = (blockIdx.x - tile * column_tiles) * BN;
     const RowTile rows = find_row_tile<BM>(a.offsets, a.G, a.R, tile);
     if (rows.rows <= 0) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wn = (wave % WN) * (BN / WN), wm = (wave / WN) * (BM / WM);
     f32x4 acc[MI][NJ];
 #pragma unroll
@@ -112,17 +60,27 @@ __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (rows.g < a.G) {
-        const T* __restrict__ W = static_cast<const T*>(a.W) + rows.g * a.N * a.K;
-        const T* __restrict__ X = static_cast<const T*>(a.X);
-        const int columns = (int)min((int64_t)BN, a.N - n0);
-        for (int64_t k0 = 0; k0 < a.K; k0 += kTileK) {
-            __syncthreads();
-            stage<T, BN, !KN, false>(wt, W, KN ? a.N : a.K, n0, columns, k0, a.K, [](int64_t r) { return r; });
-            stage<T, BM, true, false>(xt, X, a.ldx, 0, rows.rows, k0, a.K,
-                                      [&](int64_t r) { return a.from.row(rows.first + r); });
-            __syncthreads();
-            multiply<T, MI, NJ>(wt + wn * kTileK, xt + wm * kTileK, acc);
+        const T* const W = static_cast<const T*>(a.W) + rows.g * a.N * a.K;
+        const T* x[Xt::kRounds];
+#pragma unroll
+        for (int i = 0; i < Xt::kRounds; ++i) {
+            const int m = Xt::major(i);
+            const int64_t r = m < rows.rows ? a.from.row(rows.first + m) : -1;
+            x[i] = r >= 0 ? static_cast<const T*>(a.X) + r * a.ldx : nullptr;
         }
+        const auto fetch = [&](int t, int i) -> piece_t<T> {
+            const int64_t k0 = (int64_t)t * Wt::kInner;
+            if (i >= Wt::kRounds) {
+                const int r = i - Wt::kRounds;
+                const int64_t k = k0 + Xt::minor(r) * Xt::P;
+                return x[r] ? part_of_piece(x[r] + k, a.K - k) : piece_t<T>{};
+            }
+            const int64_t k = k0 + (KN ? Wt::major(i) : Wt::minor(i) * Wt::P);
+            const int64_t n = n0 + (KN ? Wt::minor(i) * Wt::P : Wt::major(i));
+            if (k >= a.K || n >= a.N) return piece_t<T>{};
+            return KN ? part_of_piece(W + k * a.N + n, a.N - n) : part_of_piece(W + n * a.K + k, a.K - k);
+        };
+        multiply_tiles_staged<Wt, Xt, MI, NJ, T>(lds, (int)((a.K + Wt::kInner - 1) / Wt::kInner), fetch, wn, wm, acc);
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -132,60 +90,50 @@ __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int64_t n = n0 + wn + 16 * i + 4 * (lane >> 4);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (n + r < a.N) y[n + r] = (T)acc[i][j][r];
+            if (n < a.N) store_four(y + n, acc[i][j], a.N - n);
         }
     }
 }
 
-// A tile of the weights' gradient, 128 x 128, over all rows of its group.  FIRST lies along the rows of the result:
-// N of N x K, K of K x N.
+// A tile of the weights' gradient, 128 x 128, over all rows of its group: the rows of the result are N of N x K, K of K x N.
 template <typename T, bool KN>
 __global__ __launch_bounds__(kThreads) void grouped_wgrad_general_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n)
 {
-    constexpr int B = 128, kTileK = kRowBytes / (int)sizeof(T);
-    __shared__ __align__(16) T lt[B * kTileK];
-    __shared__ __align__(16) T rt[B * kTileK];
+    constexpr int B = 128;
+    using Bt = Tile<T, B, false, kThreads>;
+    __shared__ __align__(16) char lds[4 * Bt::kBytes];
     const int64_t per = tiles_m * tiles_n, g = blockIdx.x / per, in = blockIdx.x - g * per;
-    const int64_t rows = KN ? a.K : a.N, columns = KN ? a.N : a.K;
+    const int64_t lines = KN ? a.K : a.N, columns = KN ? a.N : a.K;
     const int64_t m0 = in / tiles_n * B, n0 = in % tiles_n * B;
-    const int m_rows = (int)min((int64_t)B, rows - m0), n_columns = (int)min((int64_t)B, columns - n0);
     const GroupRows gr = group_rows(a.offsets, g, a.R);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wn = (wave & 1) * 64, wm = (wave >> 1) * 64;
     f32x4 acc[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const T* __restrict__ X = static_cast<const T*>(a.X);
-    const T* __restrict__ dY = static_cast<const T*>(a.Y);
-    const auto x_row = [&](int64_t r) { return a.from.row(r); };
-    const auto y_row = [](int64_t r) { return r; };
-    for (int64_t r0 = gr.first; r0 < gr.end; r0 += kTileK) {
-        __syncthreads();
-        if constexpr (KN) {
-            stage<T, B, false, false>(lt, dY, a.ldy, n0, n_columns, r0, gr.end, y_row);
-            stage<T, B, false, false>(rt, X, a.ldx, m0, m_rows, r0, gr.end, x_row);
-        } else {
-            stage<T, B, false, false>(lt, X, a.ldx, n0, n_columns, r0, gr.end, x_row);
-            stage<T, B, false, false>(rt, dY, a.ldy, m0, m_rows, r0, gr.end, y_row);
-        }
-        __syncthreads();
-        multiply<T, 4, 4>(lt + wn * kTileK, rt + wm * kTileK, acc);
-    }
+    const T* const X = static_cast<const T*>(a.X);
+    const T* const dY = static_cast<const T*>(a.Y);
+    const auto fetch = [&](int t, int i) -> piece_t<T> {
+        const int64_t r = gr.first + (int64_t)t * Bt::kInner + Bt::major(i % Bt::kRounds);
+        const bool first = i < Bt::kRounds;  // the operand that has the result's columns
+        const int64_t line = (first ? n0 : m0) + Bt::minor(i % Bt::kRounds) * Bt::P;
+        if (r >= gr.end || line >= (first ? columns : lines)) return piece_t<T>{};
+        if (first == KN) return part_of_piece(dY + r * a.ldy + line, a.N - line);
+        const int64_t row = a.from.row(r);
+        return row >= 0 ? part_of_piece(X + row * a.ldx + line, a.K - line) : piece_t<T>{};
+    };
+    multiply_tiles_staged<Bt, Bt, 4, 4, T>(lds, (int)((gr.end - gr.first + Bt::kInner - 1) / Bt::kInner), fetch, wn, wm, acc);
     T* __restrict__ dW = static_cast<T*>(const_cast<void*>(a.W)) + g * a.N * a.K;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t m = m0 + wm + 16 * j + (lane & 15);
-        if (m >= rows) continue;
+        if (m >= lines) continue;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t n = n0 + wn + 16 * i + 4 * (lane >> 4);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (n + r < columns) dW[m * columns + n + r] = (T)acc[i][j][r];
+            if (n < columns) store_four(dW + m * columns + n, acc[i][j], columns - n);
         }
     }
 }

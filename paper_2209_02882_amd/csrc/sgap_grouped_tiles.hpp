@@ -40,7 +40,7 @@ struct Tile {
     static constexpr int kBytes = LINES * 128;
     static constexpr int kRounds = kBytes / 16 / THREADS;
     static constexpr int kAcross = LINES / P;  // pieces of a row (lines contiguous)
-    static_assert(kRounds >= 1 && (INNER || LINES >= 128), "");
+    static_assert(kBytes % (16 * THREADS) == 0 && (INNER || LINES >= 128), "");
 
     // the rotation of row k's chunks
     static __device__ __forceinline__ int turn(int k) { return sizeof(T) == 2 ? (k & 3) | ((k >> 3) & 1) << 2 : (k >> 2) & 3; }
@@ -78,14 +78,16 @@ struct Tile {
                      : "s"(place(lds, round)), "v"(from)
                      : "m0", "memory");
     }
-    // zeros in the place that this lane's load would fill
-    static __device__ __forceinline__ void clear(uint32_t lds, int round)
+    // into the place that this lane's load would fill
+    static __device__ __forceinline__ void put(uint32_t lds, int round, piece_t<T> v)
     {
         typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
-        *(lds_piece*)(uintptr_t)(lds + (round * THREADS + threadIdx.x) * 16) = piece_t<T>{};
+        *(lds_piece*)(uintptr_t)(lds + (round * THREADS + threadIdx.x) * 16) = v;
     }
+    static __device__ __forceinline__ void clear(uint32_t lds, int round) { put(lds, round, piece_t<T>{}); }
 
-    // Where in a tile this lane's fragments begin, for the lines from line0 (a multiple of 64) on.
+    // Where in a tile this lane's fragments begin, for the lines from line0 on: a multiple of sixteen times the power of two that
+    // the wavefront's fragments are.
     static __device__ __forceinline__ uint32_t lane_base(int line0)
     {
         const int lane = threadIdx.x & 63, row = lane & 15, part = lane >> 4;
@@ -96,7 +98,7 @@ struct Tile {
             return (uint32_t)(k * (LINES * 2) + (chunk >> 3) * 256 + (((chunk & 7) ^ turn(k)) << 5) + (row & 3) * 8);
         }
         const int k = part * 4;
-        return (uint32_t)(k * (LINES * 4) + (chunk >> 2) * 256 + (turn(k) << 6) + row * 4);
+        return (uint32_t)(k * (LINES * 4) + (chunk >> 2) * 256 + (((chunk & 3) ^ turn(k)) << 6) + row * 4);
     }
 
     // Lanes' pieces of the sixteen lines number i behind lane_base's, inner values of step kc of 2.  `base`: the LDS address.
@@ -215,6 +217,67 @@ __device__ __forceinline__ void multiply_tiles(char* shared, int tiles, F&& load
     if (tiles == 0) return;
     if (active) multiply_tiles_as<L, R, MI, NJ, true>(lds, tiles, load, mend, l0, r0, acc);
     else multiply_tiles_as<L, R, MI, NJ, false>(lds, tiles, load, mend, l0, r0, acc);
+}
+
+// The same where the loads cannot go past the registers (rows at addresses that are no multiples of 16 bytes): a tile's
+// pieces wait in registers from the middle of one tile to the middle of the next and are then put into LDS.
+//   fetch(t, i)  piece i of LOADS of tile t, zeros for what is not there
+template <typename L, typename R, int MI, int NJ, typename T, typename F>
+__device__ __forceinline__ void multiply_tiles_staged(char* shared, int tiles, F&& fetch, int l0, int r0, f32x4 (&acc)[MI][NJ])
+{
+    constexpr uint32_t kStage = L::kBytes + R::kBytes;
+    constexpr int kLoads = L::kRounds + R::kRounds;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)shared;
+    if (tiles == 0) return;
+    piece_t<T> fl[2][MI], fr[2][NJ], coming[kLoads];
+    const uint32_t lbase = lds + L::lane_base(l0), rbase = lds + L::kBytes + R::lane_base(r0);
+    uint32_t lb, rb;
+    const auto at = [&](uint32_t stage) {
+        lb = lbase + stage, rb = rbase + stage;
+        asm volatile("" : "+v"(lb), "+v"(rb));
+    };
+    const auto read = [&](int kc, int i) {
+        if (i < MI) fl[kc][i] = L::fragment(lb, i, kc);
+        else fr[kc][i - MI] = R::fragment(rb, i - MI, kc);
+    };
+    const auto half = [&](int kc) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+            for (int i = j * (MI + NJ) / NJ; i < (j + 1) * (MI + NJ) / NJ; ++i) read(1 - kc, i);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(fl[kc][i], fr[kc][j], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const auto get = [&](int t) {
+        if (t >= tiles) return;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) coming[i] = fetch(t, i);
+    };
+    const auto put = [&](uint32_t stage) {
+#pragma unroll
+        for (int i = 0; i < L::kRounds; ++i) L::put(lds + stage, i, coming[i]);
+#pragma unroll
+        for (int i = 0; i < R::kRounds; ++i) R::put(lds + stage + L::kBytes, i, coming[L::kRounds + i]);
+    };
+    get(0);
+    put(0);
+    get(1);
+    __syncthreads();
+    at(0);
+#pragma unroll
+    for (int i = 0; i < MI + NJ; ++i) read(0, i);
+    for (int t = 0; t < tiles; ++t) {
+        const uint32_t stage = (t & 1) * kStage;
+        at(stage);
+        half(0);
+        if (t + 1 < tiles) put(kStage - stage);
+        __syncthreads();
+        get(t + 2);
+        at(kStage - stage);
+        half(1);
+    }
 }
 
 }  // namespace sgap

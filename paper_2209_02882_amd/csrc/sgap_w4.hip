@@ -11,6 +11,8 @@
 //
 // Where x is infinite or so large that the sums overflow, that difference is no number although the definition may be
 // one: an element that comes out not finite is computed again value by value.
+#include <type_traits>
+
 #include "sgap_grouped.hpp"
 
 namespace sgap {
@@ -58,8 +60,11 @@ __device__ __forceinline__ uint32_t code_at(const uint8_t* __restrict__ tiles, i
     return (at[nibble >> 1] >> (4 * (nibble & 1))) & 15;
 }
 
-// One byte of the laid-out codes, scales and zero points per thread.
-__global__ __launch_bounds__(256) void w4_layout_kernel(int64_t G, int64_t K, int64_t N, int64_t blocks_scale, bool zeros, W4Sizes z,
+// scales (and zero points) of a block of 128 values
+inline __host__ __device__ int scales_of_block(int group_k) { return group_k >= 128 ? 1 : 128 / group_k; }
+
+// One byte of the laid-out codes, one scale and one zero point per thread and turn.
+__global__ __launch_bounds__(256) void w4_layout_kernel(int64_t G, int64_t K, int64_t N, int group_k, bool zeros, W4Sizes z,
                                                         const uint8_t* __restrict__ q, const uint16_t* __restrict__ scales,
                                                         const uint8_t* __restrict__ zero, uint8_t* __restrict__ out)
 {
@@ -81,21 +86,46 @@ __global__ __launch_bounds__(256) void w4_layout_kernel(int64_t G, int64_t K, in
         }
         out[i] = (uint8_t)v;
     }
-    const int64_t many = G * z.tiles_n * blocks_scale * kTileN;
+    const int per = scales_of_block(group_k);
+    const int64_t many = G * z.tiles_n * z.scales_k * kTileN;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < many; i += steps) {
-        const int64_t b = i / kTileN % blocks_scale, t = i / kTileN / blocks_scale;
-        const int64_t g = t / z.tiles_n, n = t % z.tiles_n * kTileN + i % kTileN;
-        const int64_t from = (g * N + n) * blocks_scale + b;
-        reinterpret_cast<uint16_t*>(out + z.scales_at)[i] = n < N ? scales[from] : 0;
-        if (zeros) (out + z.zeros_at)[i] = n < N ? zero[from] : 8;
+        // scale s of block (or group) b of column i / per % 16
+        const int64_t b = i / per / kTileN % (z.scales_k / per), t = i / kTileN / z.scales_k;
+        const int64_t g = t / z.tiles_n, n = t % z.tiles_n * kTileN + i / per % kTileN, s = b * per + i % per;
+        const bool there = n < N && s < K / group_k;
+        const int64_t from = (g * N + n) * (K / group_k) + s;
+        reinterpret_cast<uint16_t*>(out + z.scales_at)[i] = there ? scales[from] : 0;
+        if (zeros) (out + z.zeros_at)[i] = there ? zero[from] : 8;
     }
 }
 
-// NT tiles of columns and MT tiles of 16 rows to a wavefront; STEPS matrix instructions (32 values each) to a scale, or,
-// with STEPS = 4, any whole number of blocks of 128.  The wavefronts of the workgroup share the inner dimension.
+// What a wavefront needs of a block of 128 values: codes of NT tiles, pieces of MT times 16 rows, scales.
 template <typename T, int STEPS, int NT, int MT, bool ZEROS>
-__global__ __launch_bounds__(NT * MT > 1 ? 512 : 1024) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items)
+struct W4Block {
+    static constexpr int kPer = 4 / STEPS;
+    // as they lie in memory: taken apart where they are used, which is what the registers are enough for
+    typedef std::conditional_t<kPer == 4, uint64_t, std::conditional_t<kPer == 2, uint32_t, uint16_t>> scales_t;
+    typedef std::conditional_t<kPer == 4, uint32_t, std::conditional_t<kPer == 2, uint16_t, uint8_t>> zeros_t;
+    uint4 w[NT];
+    piece_t<T> x[MT][4];
+    scales_t scale[NT];
+    zeros_t zero[NT];
+    __device__ __forceinline__ float scale_of(int nt, int s) const
+    {
+        const uint16_t bits = (uint16_t)(scale[nt] >> (16 * s));
+        return (float)__builtin_bit_cast(T, bits);
+    }
+    __device__ __forceinline__ float zero_of(int nt, int s) const { return (float)(uint8_t)(zero[nt] >> (8 * s)); }
+};
+
+// NT tiles of columns and MT tiles of 16 rows to a wavefront; STEPS matrix instructions (32 values each) to a scale, or,
+// with STEPS = 4, any whole number of blocks of 128.  The wavefronts of the workgroup share the inner dimension; a block's
+// loads are on their way while the block before is multiplied.
+template <typename T, int STEPS, int NT, int MT, bool ZEROS>
+__global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items, int64_t blocks, bool tail)
 {
+    using Block = W4Block<T, STEPS, NT, MT, ZEROS>;
+    constexpr int kPer = Block::kPer;
     __shared__ f32x4 part[16][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
@@ -104,75 +134,101 @@ __global__ __launch_bounds__(NT * MT > 1 ? 512 : 1024) void grouped_w4_kernel(Gr
     const uint8_t* __restrict__ tiles = a.weights + g * z.tiles_n * z.blocks_k * kTileBytes;
     const T* __restrict__ scales = reinterpret_cast<const T*>(a.weights + z.scales_at) + g * z.tiles_n * z.scales_k * kTileN;
     const uint8_t* __restrict__ zeros = a.weights + z.zeros_at + g * z.tiles_n * z.scales_k * kTileN;
-    GroupRows gr = {0, 0};
-    if (g < a.G) gr = group_rows(a.offsets, g, a.R);
+    const GroupRows gr = group_rows(a.offsets, g, a.R);
     const T* __restrict__ X = static_cast<const T*>(a.X);
     T* __restrict__ Y = static_cast<T*>(a.Y);
+    const int64_t scale_groups = z.scales_k / kPer;
     piece_t<T> ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (T)1.0f;
     for (int64_t m0 = gr.first + (int64_t)blockIdx.y * 16 * MT; m0 < gr.end; m0 += (int64_t)gridDim.y * 16 * MT) {
+        // lanes behind the last row read it once more, and their results are not stored; a row that does not exist is read
+        // from row 0, and zeros are stored
         const T* __restrict__ x[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            const int64_t m = m0 + mt * 16 + row;
-            const int64_t r = m < gr.end ? a.from.row(m) : -1;
-            x[mt] = r >= 0 ? X + r * a.ldx + piece * 8 : nullptr;
+            const int64_t r = a.from.row(min(m0 + mt * 16 + row, gr.end - 1));
+            x[mt] = X + (r < 0 ? 0 : r) * a.ldx + piece * 8;
         }
         f32x4 acc[NT][MT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int64_t kb = wave; kb < z.blocks_k; kb += waves) {
-            uint4 w[NT];
+        // Offsets of a block are the wavefront's; made anew each time (or the compiler keeps a pointer for every load, and
+        // runs out of registers).
+        const auto fetch = [&](int64_t kb, Block& b, bool whole) {
+            asm volatile("" : "+s"(kb));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int64_t t = min(tile0 + nt, z.tiles_n - 1);  // a tile behind the last is not stored
-                w[nt] = *reinterpret_cast<const uint4*>(tiles + (t * z.blocks_k + kb) * kTileBytes + lane * 16);
+                b.w[nt] = *reinterpret_cast<const uint4*>(tiles + (t * z.blocks_k + kb) * kTileBytes + lane * 16);
+                const int64_t at = (t * scale_groups + (STEPS == 4 && a.group_k > kBlockK ? kb * kBlockK / a.group_k : kb)) * (kTileN * kPer);
+                b.scale[nt] = *reinterpret_cast<const typename Block::scales_t*>(scales + at + row * kPer);
+                if (ZEROS) b.zero[nt] = *reinterpret_cast<const typename Block::zeros_t*>(zeros + at + row * kPer);
             }
-            const int steps = (int)min((int64_t)4, (a.K - kb * kBlockK) / 32);
 #pragma unroll
-            for (int s0 = 0; s0 < 4; s0 += STEPS) {
-                if (s0 >= steps) break;
-                piece_t<T> xf[MT][STEPS];
+            for (int mt = 0; mt < MT; ++mt) {
+                const T* __restrict__ p = x[mt] + kb * kBlockK;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
+                for (int i = 0; i < 4; ++i) {
+                    // A step of 32 values that the last block does not have reads the block's first once more: the scales
+                    // there are zeros, and a row with values that are not finite is computed again below in any case.
+                    b.x[mt][i] = load_piece(p + (whole || kb * kBlockK + i * 32 < a.K ? i * 32 : 0));
+                }
+            }
+        };
+        const auto multiply = [&](const Block& b) {
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i) {
-                        xf[mt][i] = piece_t<T>{};
-                        if (x[mt] && s0 + i < steps) xf[mt][i] = load_piece(x[mt] + kb * kBlockK + (s0 + i) * 32);
-                    }
+            for (int s = 0; s < kPer; ++s) {
                 f32x4 sum[MT];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     sum[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i) sum[mt] = mma16(xf[mt][i], ones, sum[mt]);
+                    for (int i = 0; i < STEPS; ++i) sum[mt] = mma16(b.x[mt][s * STEPS + i], ones, sum[mt]);
                 }
-                const int64_t sb = (kb * kBlockK + s0 * 32) / a.group_k;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    const int64_t t = min(tile0 + nt, z.tiles_n - 1);
-                    const float scale = (float)scales[(t * z.scales_k + sb) * kTileN + row];
-                    const float zero = ZEROS ? 16.0f + (float)zeros[(t * z.scales_k + sb) * kTileN + row] : 24.0f;
-                    const uint32_t d[4] = {w[nt].x, w[nt].y, w[nt].z, w[nt].w};
+                    const float scale = b.scale_of(nt, s);
+                    const float zero = ZEROS ? 16.0f + b.zero_of(nt, s) : 24.0f;
+                    const uint32_t d[4] = {b.w[nt].x, b.w[nt].y, b.w[nt].z, b.w[nt].w};
                     f32x4 dot[MT];
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) dot[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int i = 0; i < STEPS; ++i) {
-                        const piece_t<T> wf = decode<T>(d[s0 + i]);
+                        const piece_t<T> wf = decode<T>(d[s * STEPS + i]);
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) dot[mt] = mma16(xf[mt][i], wf, dot[mt]);
+                        for (int mt = 0; mt < MT; ++mt) dot[mt] = mma16(b.x[mt][s * STEPS + i], wf, dot[mt]);
                     }
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             acc[nt][mt][r] = __builtin_fmaf(scale, __builtin_fmaf(-zero, sum[mt][r], dot[mt][r]), acc[nt][mt][r]);
+                    // (or the compiler decodes everything first and runs out of registers)
+                    if constexpr (NT * MT > 1) __builtin_amdgcn_sched_barrier(0);
                 }
             }
+        };
+        if (wave < blocks) {
+            Block one, two;
+            int64_t kb = wave;
+            fetch(kb, one, true);
+            for (;;) {
+                if (kb + waves < blocks) fetch(kb + waves, two, true);
+                multiply(one);
+                if ((kb += waves) >= blocks) break;
+                if (kb + waves < blocks) fetch(kb + waves, one, true);
+                multiply(two);
+                if ((kb += waves) >= blocks) break;
+            }
+        }
+        if (STEPS < 4 && tail && wave == blocks % waves) {  // the block that is not whole
+            Block last;
+            fetch(blocks, last, false);
+            multiply(last);
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -189,11 +245,14 @@ __global__ __launch_bounds__(NT * MT > 1 ? 512 : 1024) void grouped_w4_kernel(Gr
                     for (int w = 0; w < waves; ++w) v += reinterpret_cast<const float*>(&part[w][from])[r];
                     const int64_t at = m0 + mt * 16 + m;
                     if (at >= gr.end || n0 + n >= a.N) continue;
-                    if (!__builtin_isfinite(v)) {
-                        const int64_t xr = a.from.row(at);
+                    const int64_t xr = a.from.src || !__builtin_isfinite(v) ? a.from.row(at) : 0;
+                    if (xr < 0) {
                         v = 0.0f;
-                        for (int64_t k = 0; xr >= 0 && k < a.K; ++k) {
-                            const int64_t sc = ((tile0 + nt) * z.scales_k + k / a.group_k) * kTileN + n;
+                    } else if (!__builtin_isfinite(v)) {
+                        v = 0.0f;
+                        for (int64_t k = 0; k < a.K; ++k) {
+                            const int64_t s = k / a.group_k;
+                            const int64_t sc = (((tile0 + nt) * scale_groups + s / kPer) * kTileN + n) * kPer + s % kPer;
                             const float zero = ZEROS ? (float)zeros[sc] : 8.0f;
                             const float wv = ((float)code_at(tiles, z.blocks_k, n0 + n, k) - zero) * (float)scales[sc];
                             v = __builtin_fmaf(wv, (float)X[xr * a.ldx + k], v);
@@ -217,8 +276,11 @@ hipError_t run_w4(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_i
     const int64_t items = (z.tiles_n + NT - 1) / NT;
     if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)(a.G * items), (unsigned)row_items);
-    if (a.zeros) grouped_w4_kernel<T, STEPS, NT, MT, true><<<grid, 64 * waves, 0, s>>>(a, z, items);
-    else grouped_w4_kernel<T, STEPS, NT, MT, false><<<grid, 64 * waves, 0, s>>>(a, z, items);
+    // whole blocks, and one that is not; without a row of X there is nothing to read
+    const int64_t blocks = a.from.rows > 0 ? a.K / kBlockK : 0;
+    const bool tail = a.from.rows > 0 && a.K % kBlockK;
+    if (a.zeros) grouped_w4_kernel<T, STEPS, NT, MT, true><<<grid, 64 * waves, 0, s>>>(a, z, items, blocks, tail);
+    else grouped_w4_kernel<T, STEPS, NT, MT, false><<<grid, 64 * waves, 0, s>>>(a, z, items, blocks, tail);
     return hipGetLastError();
 }
 
@@ -229,9 +291,12 @@ hipError_t by_rows(const GroupedW4Args& a, const W4Sizes& z, hipStream_t s)
     const int64_t w = (z.blocks_k + 3) / 4;
     const int waves = w <= 4 ? 4 : w <= 8 ? 8 : 16;
     const int64_t mean = (a.R + a.G - 1) / a.G;
-    const auto items = [&](int rows) { const int64_t n = (2 * mean + rows - 1) / rows; return (int)(n < 1 ? 1 : n > 64 ? 64 : n); };
-    if (mean <= 8 || (a.G == 1 && mean <= 16)) return run_w4<T, STEPS, 1, 1>(a, z, waves, a.G == 1 ? 1 : items(16), s);
-    return run_w4<T, STEPS, 2, 3>(a, z, waves < 8 ? waves : 8, a.G == 1 ? (items(48) + 1) / 2 : items(48), s);
+    const auto items = [&](int rows) {
+        const int64_t n = a.G == 1 ? (mean + rows - 1) / rows : (2 * mean + rows - 1) / rows;
+        return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    };
+    if (mean <= 8 || (a.G == 1 && mean <= 16)) return run_w4<T, STEPS, 1, 1>(a, z, waves, items(16), s);
+    return run_w4<T, STEPS, 2, 3>(a, z, waves < 8 ? waves : 8, items(48), s);
 }
 
 template <typename T>
@@ -251,7 +316,7 @@ W4Sizes w4_sizes(int64_t G, int64_t K, int64_t N, int group_k, bool zeros)
     W4Sizes z;
     z.tiles_n = (N + kTileN - 1) / kTileN;
     z.blocks_k = (K + kBlockK - 1) / kBlockK;
-    z.scales_k = K / group_k;
+    z.scales_k = group_k >= 128 ? K / group_k : z.blocks_k * scales_of_block(group_k);  // whole blocks of them
     const int64_t codes = G * z.tiles_n * z.blocks_k * kTileBytes, many = G * z.tiles_n * z.scales_k * kTileN;
     z.scales_at = up(codes, 256);
     z.zeros_at = z.scales_at + up(2 * many, 256);
@@ -265,7 +330,7 @@ hipError_t launch_w4_layout(int64_t G, int64_t K, int64_t N, int group_k, const 
     const W4Sizes z = w4_sizes(G, K, N, group_k, zeros != nullptr);
     const int64_t blocks = (z.bytes + 255) / 256;
     w4_layout_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, s>>>(
-        G, K, N, z.scales_k, zeros != nullptr, z, q, static_cast<const uint16_t*>(scales), zeros, out);
+        G, K, N, group_k, zeros != nullptr, z, q, static_cast<const uint16_t*>(scales), zeros, out);
     return hipGetLastError();
 }
 
