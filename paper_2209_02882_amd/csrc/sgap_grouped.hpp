@@ -60,4 +60,25 @@ inline int64_t most_row_tiles(int64_t G, int64_t R, int BM, bool offsets)
     return offsets ? (R + BM - 1) / BM + (G < R ? G : R) + 1 : (R + BM - 1) / BM;
 }
 
+// More LDS than a launch gets unasked; `allowed` has a bit for each device on which that has been asked for.
+template <typename K>
+inline hipError_t allow_lds(K kernel, int bytes, uint64_t& allowed)
+{
+    int device = 0;
+    if (const hipError_t err = hipGetDevice(&device)) return err;
+    if (device < 64 && (allowed >> device & 1)) return hipSuccess;
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (err == hipSuccess && device < 64) allowed |= 1ull << device;
+    return err;
+}
+
+// Until none of this wavefront's loads is on its way; to the compiler, nothing moves across.  (The builtin tells it that
+// its own loads have arrived as well: vmcnt 0, the other counters as they are.)
+__device__ __forceinline__ void wait_loads()
+{
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+}
+
 }  // namespace sgap

@@ -218,18 +218,6 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     }
 }
 
-// More LDS than a launch gets unasked; `allowed` has a bit for each device on which that has been asked for.
-template <typename K>
-hipError_t allow_lds(K kernel, int bytes, uint64_t& allowed)
-{
-    int device = 0;
-    if (const hipError_t err = hipGetDevice(&device)) return err;
-    if (device < 64 && (allowed >> device & 1)) return hipSuccess;
-    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (err == hipSuccess && device < 64) allowed |= 1ull << device;
-    return err;
-}
-
 unsigned dealt_grid(int64_t items) { return (unsigned)((items + 255) / 256 * 256); }
 
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>

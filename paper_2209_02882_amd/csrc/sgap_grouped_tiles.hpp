@@ -24,15 +24,6 @@ __device__ __forceinline__ const P* uniform(const P* p)
     return (const P*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
-// Until none of this wavefront's loads is on its way; to the compiler, nothing moves across.  (The builtin tells it that
-// its own loads have arrived as well: vmcnt 0, the other counters as they are.)
-__device__ __forceinline__ void wait_loads()
-{
-    asm volatile("" : : : "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-}
-
 template <typename T, int LINES, bool INNER, int THREADS>
 struct Tile {
     static constexpr int P = Piece<T>::kCount;

@@ -99,15 +99,14 @@ __global__ __launch_bounds__(256) void w4_layout_kernel(int64_t G, int64_t K, in
     }
 }
 
-// What a wavefront needs of a block of 128 values: codes of NT tiles, pieces of MT times 16 rows, scales.
-template <typename T, int STEPS, int NT, int MT, bool ZEROS>
+// What a wavefront needs of the weights of a block of 128 values: codes of NT tiles and their scales.
+template <typename T, int STEPS, int NT, bool ZEROS>
 struct W4Block {
     static constexpr int kPer = 4 / STEPS;
     // as they lie in memory: taken apart where they are used, which is what the registers are enough for
     typedef std::conditional_t<kPer == 4, uint64_t, std::conditional_t<kPer == 2, uint32_t, uint16_t>> scales_t;
     typedef std::conditional_t<kPer == 4, uint32_t, std::conditional_t<kPer == 2, uint16_t, uint8_t>> zeros_t;
     uint4 w[NT];
-    piece_t<T> x[MT][4];
     scales_t scale[NT];
     zeros_t zero[NT];
     __device__ __forceinline__ float scale_of(int nt, int s) const
@@ -118,15 +117,23 @@ struct W4Block {
     __device__ __forceinline__ float zero_of(int nt, int s) const { return (float)(uint8_t)(zero[nt] >> (8 * s)); }
 };
 
+constexpr int most_waves(int NT, int MT) { return NT * MT > 2 ? 8 : 16; }
+
 // NT tiles of columns and MT tiles of 16 rows to a wavefront; STEPS matrix instructions (32 values each) to a scale, or,
 // with STEPS = 4, any whole number of blocks of 128.  The wavefronts of the workgroup share the inner dimension; a block's
 // loads are on their way while the block before is multiplied.
-template <typename T, int STEPS, int NT, int MT, bool ZEROS>
-__global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items, int64_t blocks, bool tail)
+// STAGED: the rows of X go through LDS, 256 bytes of a row to sixteen lanes, piece p of row r at place p ^ r.  The matrix
+// unit wants neighbouring lanes to have different rows, and loads like that take the cache a turn for every lane: with 48
+// rows of 8,192 values by 8,192 columns 34 us, 53,000 of a compute unit's 74,000 clocks, where the rows' loads through LDS
+// take 16 lanes to one turn.  For rows at addresses that are multiples of 16 bytes; others load as the unit wants them.
+template <typename T, int STEPS, int NT, int MT, bool ZEROS, bool STAGED>
+__global__ __launch_bounds__(64 * most_waves(NT, MT)) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items,
+                                                                              int64_t blocks, bool tail)
 {
-    using Block = W4Block<T, STEPS, NT, MT, ZEROS>;
-    constexpr int kPer = Block::kPer;
-    __shared__ f32x4 part[16][64];
+    using Block = W4Block<T, STEPS, NT, ZEROS>;
+    constexpr int kPer = Block::kPer, kRowBytes = 2 * kBlockK, kStaged = MT * 16 * kRowBytes;
+    extern __shared__ __align__(16) char lds[];  // the rows of X, and at the end the sums of all wavefronts
+    f32x4(*const part)[64] = reinterpret_cast<f32x4(*)[64]>(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
     const int64_t g = blockIdx.x / column_items, item = blockIdx.x - g * column_items;
@@ -138,26 +145,29 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
     const T* __restrict__ X = static_cast<const T*>(a.X);
     T* __restrict__ Y = static_cast<T*>(a.Y);
     const int64_t scale_groups = z.scales_k / kPer;
+    const uint32_t staged = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * kStaged;
     piece_t<T> ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (T)1.0f;
     for (int64_t m0 = gr.first + (int64_t)blockIdx.y * 16 * MT; m0 < gr.end; m0 += (int64_t)gridDim.y * 16 * MT) {
-        // lanes behind the last row read it once more, and their results are not stored; a row that does not exist is read
-        // from row 0, and zeros are stored
-        const T* __restrict__ x[MT];
+        // Lanes behind the last row read it once more, and their results are not stored; a row that does not exist is read
+        // from row 0, and zeros are stored.  A lane has MT rows, or, STAGED, four of each MT times sixteen.
+        constexpr int kRows = STAGED ? 4 * MT : MT;
+        const T* __restrict__ x[kRows];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const int64_t r = a.from.row(min(m0 + mt * 16 + row, gr.end - 1));
-            x[mt] = X + (r < 0 ? 0 : r) * a.ldx + piece * 8;
+        for (int i = 0; i < kRows; ++i) {
+            const int64_t r = a.from.row(min(m0 + (STAGED ? 4 * i + piece : 16 * i + row), gr.end - 1));
+            x[i] = X + (r < 0 ? 0 : r) * a.ldx + (STAGED ? 0 : piece * 8);
         }
         f32x4 acc[NT][MT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        piece_t<T> xf[MT][4], coming[STAGED ? 1 : MT][4];
         // Offsets of a block are the wavefront's; made anew each time (or the compiler keeps a pointer for every load, and
         // runs out of registers).
-        const auto fetch = [&](int64_t kb, Block& b, bool whole) {
+        const auto fetch = [&](int64_t kb, Block& b) {
             asm volatile("" : "+s"(kb));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -167,15 +177,47 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
                 b.scale[nt] = *reinterpret_cast<const typename Block::scales_t*>(scales + at + row * kPer);
                 if (ZEROS) b.zero[nt] = *reinterpret_cast<const typename Block::zeros_t*>(zeros + at + row * kPer);
             }
+        };
+        // Rows of X of a block; STAGED: into LDS.  A step of 32 values that the last block does not have reads the block's
+        // first once more: the scales there are zeros, and a row with values that are not finite is computed again below in
+        // any case.
+        const auto fetch_rows = [&](int64_t kb, bool whole) {
+            asm volatile("" : "+s"(kb));
+            const int left = whole ? kBlockK : (int)(a.K - kb * kBlockK);
+            if constexpr (STAGED) {
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const T* __restrict__ p = x[mt] + kb * kBlockK;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    // A step of 32 values that the last block does not have reads the block's first once more: the scales
-                    // there are zeros, and a row with values that are not finite is computed again below in any case.
-                    b.x[mt][i] = load_piece(p + (whole || kb * kBlockK + i * 32 < a.K ? i * 32 : 0));
+                for (int i = 0; i < kRows; ++i) {
+                    int k = (row ^ ((4 * i + piece) & 15)) * 8;
+                    if (k >= left) k &= 31;
+                    const T* from = x[i] + kb * kBlockK + k;
+                    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                                 :
+                                 : "s"(staged + i * 1024), "v"(from)
+                                 : "m0", "memory");
                 }
+            } else {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) coming[mt][i] = load_piece(x[mt] + kb * kBlockK + (i * 32 < left ? i * 32 : 0));
+            }
+        };
+        // STAGED: the rows that have arrived, out of LDS, which is then free for the next
+        const auto take_rows = [&] {
+            if constexpr (STAGED) {
+                typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
+                wait_loads();
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        xf[mt][i] = *(const lds_piece*)(uintptr_t)(staged + (mt * 16 + row) * kRowBytes + (((i * 4 + piece) ^ row) << 4));
+                asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+            } else {
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) xf[mt][i] = coming[mt][i];
             }
         };
         const auto multiply = [&](const Block& b) {
@@ -186,7 +228,7 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
                 for (int mt = 0; mt < MT; ++mt) {
                     sum[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int i = 0; i < STEPS; ++i) sum[mt] = mma16(b.x[mt][s * STEPS + i], ones, sum[mt]);
+                    for (int i = 0; i < STEPS; ++i) sum[mt] = mma16(xf[mt][s * STEPS + i], ones, sum[mt]);
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
@@ -200,7 +242,7 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
                     for (int i = 0; i < STEPS; ++i) {
                         const piece_t<T> wf = decode<T>(d[s * STEPS + i]);
 #pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) dot[mt] = mma16(b.x[mt][s * STEPS + i], wf, dot[mt]);
+                        for (int mt = 0; mt < MT; ++mt) dot[mt] = mma16(xf[mt][s * STEPS + i], wf, dot[mt]);
                     }
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
@@ -212,23 +254,27 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
                 }
             }
         };
-        if (wave < blocks) {
+        // blocks wave, wave + waves, .. of the whole ones; the one that is not whole goes to the wavefront whose turn it is
+        const int64_t all = blocks + (STEPS < 4 && tail ? 1 : 0);
+        if (wave < all) {
+            const auto ask = [&](int64_t kb, Block& b) {
+                if (kb >= all) return;
+                fetch(kb, b);
+                fetch_rows(kb, STEPS == 4 || kb < blocks);
+            };
             Block one, two;
             int64_t kb = wave;
-            fetch(kb, one, true);
+            ask(kb, one);
             for (;;) {
-                if (kb + waves < blocks) fetch(kb + waves, two, true);
+                take_rows();
+                ask(kb + waves, two);
                 multiply(one);
-                if ((kb += waves) >= blocks) break;
-                if (kb + waves < blocks) fetch(kb + waves, one, true);
+                if ((kb += waves) >= all) break;
+                take_rows();
+                ask(kb + waves, one);
                 multiply(two);
-                if ((kb += waves) >= blocks) break;
+                if ((kb += waves) >= all) break;
             }
-        }
-        if (STEPS < 4 && tail && wave == blocks % waves) {  // the block that is not whole
-            Block last;
-            fetch(blocks, last, false);
-            multiply(last);
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -261,6 +307,7 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
                     Y[at * a.ldy + n0 + n] = (T)v;
                 }
             }
+        if constexpr (STAGED) __syncthreads();  // the sums have been read: their place is the next rows'
     }
     // rows behind the last group
     if (a.offsets && g == a.G - 1) {
@@ -270,8 +317,8 @@ __global__ __launch_bounds__(NT * MT > 2 ? 512 : 1024) void grouped_w4_kernel(Gr
     }
 }
 
-template <typename T, int STEPS, int NT, int MT>
-hipError_t run_w4(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_items, hipStream_t s)
+template <typename T, int STEPS, int NT, int MT, bool ZEROS, bool STAGED>
+hipError_t launch_as(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_items, hipStream_t s)
 {
     const int64_t items = (z.tiles_n + NT - 1) / NT;
     if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
@@ -279,9 +326,23 @@ hipError_t run_w4(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_i
     // whole blocks, and one that is not; without a row of X there is nothing to read
     const int64_t blocks = a.from.rows > 0 ? a.K / kBlockK : 0;
     const bool tail = a.from.rows > 0 && a.K % kBlockK;
-    if (a.zeros) grouped_w4_kernel<T, STEPS, NT, MT, true><<<grid, 64 * waves, 0, s>>>(a, z, items, blocks, tail);
-    else grouped_w4_kernel<T, STEPS, NT, MT, false><<<grid, 64 * waves, 0, s>>>(a, z, items, blocks, tail);
+    static uint64_t allowed = 0;
+    constexpr int kEach = STAGED ? MT * 4096 : 1024;
+    if (const hipError_t err = allow_lds(grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED>, most_waves(NT, MT) * kEach, allowed)) return err;
+    grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED><<<grid, 64 * waves, waves * kEach, s>>>(a, z, items, blocks, tail);
     return hipGetLastError();
+}
+
+template <typename T, int STEPS, int NT, int MT>
+hipError_t run_w4(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_items, bool staged, hipStream_t s)
+{
+    if constexpr (MT != 2) {  // two times sixteen rows: staged only
+        if (!staged)
+            return a.zeros ? launch_as<T, STEPS, NT, MT, true, false>(a, z, waves, row_items, s)
+                           : launch_as<T, STEPS, NT, MT, false, false>(a, z, waves, row_items, s);
+    }
+    return a.zeros ? launch_as<T, STEPS, NT, MT, true, true>(a, z, waves, row_items, s)
+                   : launch_as<T, STEPS, NT, MT, false, true>(a, z, waves, row_items, s);
 }
 
 template <typename T, int STEPS>
@@ -289,14 +350,18 @@ hipError_t by_rows(const GroupedW4Args& a, const W4Sizes& z, hipStream_t s)
 {
     // a wavefront for four blocks of 128 values, 4 to 16 of them
     const int64_t w = (z.blocks_k + 3) / 4;
-    const int waves = w <= 4 ? 4 : w <= 8 ? 8 : 16;
+    const int waves = w <= 4 ? 4 : w <= 8 ? 8 : 16, few = waves < 8 ? waves : 8;
     const int64_t mean = (a.R + a.G - 1) / a.G;
     const auto items = [&](int rows) {
         const int64_t n = a.G == 1 ? (mean + rows - 1) / rows : (2 * mean + rows - 1) / rows;
         return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
     };
-    if (mean <= 8 || (a.G == 1 && mean <= 16)) return run_w4<T, STEPS, 1, 1>(a, z, waves, items(16), s);
-    return run_w4<T, STEPS, 2, 3>(a, z, waves < 8 ? waves : 8, items(48), s);
+    const bool staged = a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0;
+    const int64_t most = a.G == 1 ? mean : 2 * mean;  // rows that a group has, or has often
+    // (one row or two: sixteen lanes of a load share a row, and the way through LDS would only be longer)
+    if (most <= 16) return run_w4<T, STEPS, 1, 1>(a, z, waves, items(16), staged && most > 2, s);
+    if (most <= 32 && staged) return run_w4<T, STEPS, 2, 2>(a, z, few, items(32), staged, s);
+    return run_w4<T, STEPS, 2, 3>(a, z, few, items(48), staged, s);
 }
 
 template <typename T>
