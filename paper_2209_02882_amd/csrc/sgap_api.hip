@@ -277,6 +277,14 @@ int compute_units()
     return cus;
 }
 
+}  // namespace
+
+namespace sgap {
+int device_compute_units() { return compute_units(); }
+}  // namespace sgap
+
+namespace {
+
 // The library's choice for every knob a caller may leave open, with the process-wide overrides of
 // sgap_set_tuning filled in: what the entry points without a configuration argument run with.
 sgap_config config_from_globals(int schedule, int strategy, int group_size, int reduce_size)

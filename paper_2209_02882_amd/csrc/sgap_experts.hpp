@@ -97,6 +97,7 @@ struct GroupedArgs {
     void* __restrict__ Y;
     int64_t ldy;
     bool weights_kn;  // K x N
+    int compute_units;
 };
 
 // dW of the same: Y holds the gradient of the product's result (read), W the gradient of the weights (written).

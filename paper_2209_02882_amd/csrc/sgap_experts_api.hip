@@ -5,7 +5,9 @@
 #include "sgap_experts.hpp"
 
 namespace sgap {
-int fail_call(int status, const char* detail);  // sgap_api.hip: what sgap_last_error() says
+// sgap_api.hip
+int fail_call(int status, const char* detail);  // what sgap_last_error() says
+int device_compute_units();
 }
 
 namespace {
@@ -131,7 +133,8 @@ int sgap_grouped_mm(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, const
     if (layout != SGAP_WEIGHTS_NK && layout != SGAP_WEIGHTS_KN) return invalid("unknown layout of the weights");
     if (const int st = check_grouped(G, R, K, N, offsets, X, ldx, src, src_div, x_rows, W, Y, ldy)) return st;
     if (R == 0 || N == 0) return SGAP_OK;
-    const sgap::GroupedArgs a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, W, Y, ldy, layout == SGAP_WEIGHTS_KN};
+    const sgap::GroupedArgs a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, W, Y, ldy, layout == SGAP_WEIGHTS_KN,
+                              sgap::device_compute_units()};
     return launched(sgap::launch_grouped_mm(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
@@ -144,7 +147,7 @@ int sgap_grouped_mm_wgrad(int64_t G, int64_t R, int64_t K, int64_t N, int dtype,
     if (const int st = check_grouped(G, R, K, N, offsets, X, ldx, src, src_div, x_rows, dW, dY, lddy)) return st;
     if (K == 0 || N == 0) return SGAP_OK;
     const sgap::GroupedArgs a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, dW, const_cast<void*>(dY), lddy,
-                              layout == SGAP_WEIGHTS_KN};
+                              layout == SGAP_WEIGHTS_KN, sgap::device_compute_units()};
     return launched(sgap::launch_grouped_wgrad(a, dtype, static_cast<hipStream_t>(stream)));
 }
 

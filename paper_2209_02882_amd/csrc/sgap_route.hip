@@ -10,14 +10,17 @@
 //
 // Grouping is a counting sort that keeps the pairs' order: every block counts its pairs by expert and ranks them among
 // themselves (pairs of one expert found by comparing the bits of 64 experts at a time), the counts are summed up over
-// the blocks, and every pair is put in its place.  No atomics, so that the lists are the same on every run.
+// the blocks, and every pair is put in its place.  No atomics, so that the lists are the same on every run.  One launch
+// for the tokens of one block, otherwise two: the second one's blocks each sum up the counts for themselves, as long as
+// those are few; with many a kernel between them does it once.
 #include "sgap_experts.hpp"
 
 namespace sgap {
 
 namespace {
 
-constexpr int kRouteThreads = 256;
+constexpr int kRouteThreads = 1024;  // sixteen wavefronts: what hides the rounds' latency
+constexpr int kGradThreads = 256;
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxChosen = 16;
 constexpr int kBlockPairs = 1024;  // pairs of a block at most
@@ -57,6 +60,14 @@ __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
     }
     return v;
 }
+__device__ __forceinline__ int lanes_sum16(int v)
+{
+    v += (int)dpp<kRor8>((uint32_t)v);
+    v += (int)dpp<kRor4>((uint32_t)v);
+    v += (int)dpp<kRor2>((uint32_t)v);
+    v += (int)dpp<kRor1>((uint32_t)v);
+    return v;
+}
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v)
 {
@@ -71,45 +82,73 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
+// V consecutive experts of a row, as one access where all of them are there
+template <typename T, int V>
+struct Experts {
+    typedef T loose __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+};
+
 template <typename T, int V>
 __device__ __forceinline__ void load_row(const T* __restrict__ row, int e0, int E, float (&x)[V])
 {
+    if (V > 1 && e0 + V <= E) {
+        const typename Experts<T, V>::loose v = *reinterpret_cast<const typename Experts<T, V>::loose*>(row + e0);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (float)v[i];
+        return;
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] = e0 + v < E ? (float)row[e0 + v] : -__builtin_inff();
 }
 
-// The k largest of a row that LANES lanes hold, V experts each (expert sub * V + v).  Lane j of them gets choice j.
+template <typename T, int V>
+__device__ __forceinline__ void store_row(T* __restrict__ row, int e0, int E, const float (&x)[V])
+{
+    if (V > 1 && e0 + V <= E) {
+        typename Experts<T, V>::loose v;
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (T)x[i];
+        *reinterpret_cast<typename Experts<T, V>::loose*>(row + e0) = v;
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (e0 + v < E) row[e0 + v] = (T)x[v];
+}
+
+// The k largest of a row that LANES lanes hold, V experts each (expert sub * V + v), largest first, left in chosen[0 .. k)
+// (-1: nothing left); lane j of them gets choice j's gate.
 template <int LANES, int V>
-__device__ __forceinline__ void choose(const float (&x)[V], int k, bool renormalise, float& gate, int& expert)
+__device__ __forceinline__ float choose(const float (&x)[V], int k, bool renormalise, int32_t* chosen)
 {
     const int lane = threadIdx.x & 63, sub = lane & (LANES - 1);
+    // the row's lanes below this one
+    const uint64_t below = ((1ull << lane) - 1) & (LANES == 64 ? ~0ull : 0xffffull << (lane & 48));
     uint32_t key[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) key[v] = order_key(x[v]);
-    uint32_t own = 0;
-    expert = -1;
-    uint32_t first = 0;
+    uint32_t own = 0, first = 0;
     for (int j = 0; j < k; ++j) {
         uint32_t top = 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) top = max(top, key[v]);
         const uint32_t most = lanes_max<LANES>(top);
         if (j == 0) first = most;
+        if (sub == j) own = most;
+        // the lowest lane that holds it: its first value of that size leaves
         const uint64_t who = __ballot(top == most);
-        const uint64_t mine = LANES == 64 ? who : (who >> (lane & 48)) & 0xffffu;
-        const int winner = __builtin_ctzll(mine);
-        // the winner's first value of that size leaves; every lane learns which it was
-        int at = 0;
+        if (top == most && (who & below) == 0) {
+            int at = 0;
 #pragma unroll
-        for (int v = V - 1; v >= 0; --v) at = key[v] == most ? v : at;
-        const int e = __shfl(sub * V + at, winner, LANES);
+            for (int v = V - 1; v >= 0; --v) at = key[v] == most ? v : at;
+            chosen[j] = most ? sub * V + at : -1;
 #pragma unroll
-        for (int v = 0; v < V; ++v) key[v] = sub == winner && v == at ? 0u : key[v];
-        if (sub == j && most != 0) { own = most; expert = e; }
+            for (int v = 0; v < V; ++v) key[v] = v == at ? 0u : key[v];
+        }
     }
     // first = 0: a row of which nothing is left, and all gates are zero
     const float m = first ? key_value(first) : 0.0f;
-    const float mine = expert >= 0 ? expf(key_value(own) - m) : 0.0f;
+    const float mine = own ? expf(key_value(own) - m) : 0.0f;
     float part = mine;
     if (!renormalise) {
         part = 0.0f;
@@ -117,61 +156,70 @@ __device__ __forceinline__ void choose(const float (&x)[V], int k, bool renormal
         for (int v = 0; v < V; ++v) part += expf(x[v] - m);  // of -infinity: 0
     }
     const float total = lanes_sum<LANES>(part);
-    gate = expert >= 0 ? mine / total : 0.0f;
+    return own ? mine / total : 0.0f;
 }
 
+// In shared memory, behind one another: the block's experts by pair, and the pairs of each expert in each wavefront's
+// share of them.
 struct RouteShared {
-    int32_t expert[kBlockPairs];
-    int32_t count[kWaves][kMaxExperts];  // pairs of each expert in a wavefront's share of the pairs
+    int32_t* expert;  // kBlockPairs
+    uint16_t* count;  // kWaves x E
 };
-
-// Ranks the pairs of a block among those of the same expert, in their order.  In: s.expert (-1: none).  Out: per pair
-// the rank among the earlier pairs of the wavefront's share, in `rank` for the pairs this lane looks at, and s.count.
-// A wavefront's share: pairs_per_wave consecutive ones, 64 at a time.
-template <typename F>
-__device__ __forceinline__ void rank_pairs(RouteShared& s, int E, int pairs, int pairs_per_wave, F&& put)
+__device__ __forceinline__ RouteShared route_shared(char* lds)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int e = lane; e < E; e += 64) s.count[wave][e] = 0;
-    const uint64_t below = (1ull << lane) - 1;
+    return {reinterpret_cast<int32_t*>(lds), reinterpret_cast<uint16_t*>(lds + kBlockPairs * 4)};
+}
+int route_shared_bytes(int E) { return kBlockPairs * 4 + kWaves * E * 2; }
+
+// A wavefront's share of the block's pairs: 64 of them, or a part.
+__device__ __forceinline__ int my_pair() { return threadIdx.x; }
+
+// Ranks the pairs of a block among those of the same expert, in their order: each thread gets its pair's (-1: a missing
+// choice), and s.count what every wavefront's share has of each expert.
+__device__ __forceinline__ int rank_pair(const RouteShared& s, int E, int pairs)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = my_pair();
+    uint16_t* const count = s.count + wave * E;
+    for (int e = lane; e < E; e += 64) count[e] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int e = p < pairs ? s.expert[p] : -1;
+    uint64_t same = __ballot(e >= 0);
     const int bits = 32 - __builtin_clz(E);
-    const int end = min(pairs, (wave + 1) * pairs_per_wave);
-    for (int p0 = wave * pairs_per_wave; p0 < end; p0 += 64) {
-        const int p = p0 + lane;
-        const int e = p < end ? s.expert[p] : -1;
-        uint64_t same = __ballot(e >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot((e >> b) & 1);
-            same &= (e >> b) & 1 ? set : ~set;
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (e >= 0) {
-            const int before = s.count[wave][e];
-            put(p, before + __popcll(same & below));
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if ((same & below) == 0) s.count[wave][e] = before + __popcll(same);
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((e >> b) & 1);
+        same &= (e >> b) & 1 ? set : ~set;
     }
+    if (e < 0) return -1;
+    const uint64_t before = same & ((1ull << lane) - 1);
+    if (before == 0) count[e] = (uint16_t)__popcll(same);
+    return __popcll(before);
+}
+
+// count[w][e] becomes the pairs of e in the shares before w; the sum of all of them
+__device__ __forceinline__ int sum_shares(const RouteShared& s, int E, int e)
+{
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const int c = s.count[w * E + e];
+        s.count[w * E + e] = (uint16_t)sum;
+        sum += c;
+    }
+    return sum;
 }
 
 // Rows of the block are chosen for, their experts left in s.expert.
 template <typename T, int LANES, int V>
-__device__ __forceinline__ void choose_rows(const RouteArgs& a, RouteShared& s, int64_t row0, int rows)
+__device__ __forceinline__ void choose_rows(const RouteArgs& a, const RouteShared& s, int64_t row0, int rows)
 {
     constexpr int kGroups = kRouteThreads / LANES;
     const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES;
     for (int i = group; i < rows; i += kGroups) {
         const int64_t t = row0 + i;
-        float x[V], gate;
-        int expert;
+        float x[V];
         load_row<T, V>(static_cast<const T*>(a.logits) + t * a.ld, sub * V, a.E, x);
-        choose<LANES, V>(x, a.k, a.renormalise, gate, expert);
-        if (sub < a.k) {
-            a.gates[t * a.k + sub] = gate;
-            a.experts[t * a.k + sub] = expert;
-            s.expert[i * a.k + sub] = expert;
-        }
+        const float gate = choose<LANES, V>(x, a.k, a.renormalise, s.expert + i * a.k);
+        if (sub < a.k) a.gates[t * a.k + sub] = gate;
     }
 }
 
@@ -214,94 +262,53 @@ __device__ __forceinline__ void block_offsets(const int32_t* in, int32_t* out, i
 template <typename T, int LANES, int V>
 __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(RouteArgs a)
 {
-    __shared__ RouteShared s;
+    extern __shared__ __align__(16) char lds[];
     __shared__ int32_t total[kMaxExperts], start[kMaxExperts + 1], wave_total[kWaves];
-    const int pairs = (int)a.T * a.k;
+    const RouteShared s = route_shared(lds);
+    const int pairs = (int)a.T * a.k, p = my_pair();
     choose_rows<T, LANES, V>(a, s, 0, (int)a.T);
     __syncthreads();
-    const int per_wave = (pairs + 64 * kWaves - 1) / (64 * kWaves) * 64;
-    // the ranks wait in registers: a lane looks at kBlockPairs / 256 pairs at most
-    int rank[kBlockPairs / kRouteThreads];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 0; i < kBlockPairs / kRouteThreads; ++i) rank[i] = 0;
-    rank_pairs(s, a.E, pairs, per_wave, [&](int p, int r) {
-        const int at = (p - wave * per_wave) >> 6;
-#pragma unroll
-        for (int i = 0; i < kBlockPairs / kRouteThreads; ++i) rank[i] = at == i ? r : rank[i];
-    });
+    const int rank = rank_pair(s, a.E, pairs);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
-        int sum = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            const int c = s.count[w][e];
-            s.count[w][e] = sum;
-            sum += c;
-        }
-        total[e] = sum;
-    }
+    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) total[e] = sum_shares(s, a.E, e);
     __syncthreads();
     block_offsets(total, start, a.E, wave_total);
     for (int e = threadIdx.x; e <= a.E; e += kRouteThreads) a.offsets[e] = start[e];
-#pragma unroll
-    for (int i = 0; i < kBlockPairs / kRouteThreads; ++i) {
-        const int p = wave * per_wave + i * 64 + lane;
-        if (i * 64 < per_wave && p < pairs) {
-            const int e = s.expert[p];
-            const int at = e >= 0 ? start[e] + s.count[wave][e] + rank[i] : -1;
-            a.slot[p] = at;
-            if (e >= 0) a.order[at] = p;
-        }
-    }
-    for (int p = start[a.E] + threadIdx.x; p < pairs; p += kRouteThreads) a.order[p] = -1;
+    if (p >= pairs) return;
+    const int e = s.expert[p];
+    const int at = e >= 0 ? start[e] + s.count[(threadIdx.x >> 6) * a.E + e] + rank : -1;
+    a.experts[p] = e;
+    a.slot[p] = at;
+    if (e >= 0) a.order[at] = p;
+    if (p >= start[a.E]) a.order[p] = -1;  // places that no pair has
 }
 
-// Three launches for more: the choice, with the blocks' counts by expert (count[e * blocks + b]) and the pairs' ranks
-// within their block (in slot) ...
+// More tokens: the choice, with the blocks' counts by expert (count[e * blocks + b]) and the pairs' ranks within their
+// block (in slot) ...
 template <typename T, int LANES, int V>
 __global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, int rows_per_block, int32_t* count, int blocks)
 {
-    __shared__ RouteShared s;
+    extern __shared__ __align__(16) char lds[];
+    const RouteShared s = route_shared(lds);
     const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
     const int rows = (int)min((int64_t)rows_per_block, a.T - row0);
-    const int pairs = rows * a.k;
+    const int pairs = rows * a.k, p = my_pair();
     choose_rows<T, LANES, V>(a, s, row0, rows);
     __syncthreads();
-    const int per_wave = (pairs + 64 * kWaves - 1) / (64 * kWaves) * 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int rank[kBlockPairs / kRouteThreads];
-#pragma unroll
-    for (int i = 0; i < kBlockPairs / kRouteThreads; ++i) rank[i] = 0;
-    rank_pairs(s, a.E, pairs, per_wave, [&](int p, int r) {
-        const int at = (p - wave * per_wave) >> 6;
-#pragma unroll
-        for (int i = 0; i < kBlockPairs / kRouteThreads; ++i) rank[i] = at == i ? r : rank[i];
-    });
+    const int rank = rank_pair(s, a.E, pairs);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
-        int sum = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            const int c = s.count[w][e];
-            s.count[w][e] = sum;
-            sum += c;
-        }
-        count[(int64_t)e * blocks + blockIdx.x] = sum;
-    }
+    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) count[(int64_t)e * blocks + blockIdx.x] = sum_shares(s, a.E, e);
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kBlockPairs / kRouteThreads; ++i) {
-        const int p = wave * per_wave + i * 64 + lane;
-        if (i * 64 < per_wave && p < pairs) {
-            const int e = s.expert[p];
-            a.slot[row0 * a.k + p] = e >= 0 ? s.count[wave][e] + rank[i] : -1;
-        }
-    }
+    if (p >= pairs) return;
+    const int e = s.expert[p];
+    a.experts[row0 * a.k + p] = e;
+    a.slot[row0 * a.k + p] = e >= 0 ? s.count[(threadIdx.x >> 6) * a.E + e] + rank : -1;
 }
 
-// ... the counts of one expert summed up over the blocks (a wavefront per expert) ...
-__global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(int32_t* count, int32_t* total, int blocks, int E)
+// ... the counts of one expert summed up over the blocks (a wavefront per expert), where there are many of them ...
+__global__ __launch_bounds__(256) void route_scan_kernel(int32_t* count, int32_t* total, int blocks, int E)
 {
-    const int e = blockIdx.x * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int e = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (e >= E) return;
     int32_t* row = count + (int64_t)e * blocks;
     int carry = 0;
@@ -315,32 +322,57 @@ __global__ __launch_bounds__(kRouteThreads) void route_scan_kernel(int32_t* coun
     if (lane == 0) total[e] = carry;
 }
 
-// ... and every pair into its place.
+// ... and every pair into its place.  SUM: sixteen lanes sum up the counts of an expert, those of the blocks before this one
+// and all of them.
+template <bool SUM>
 __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a, int rows_per_block, const int32_t* count,
                                                                     const int32_t* total, int blocks)
 {
-    __shared__ int32_t start[kMaxExperts + 1], wave_total[kWaves];
-    block_offsets(total, start, a.E, wave_total);
-    if (blockIdx.x == 0)
-        for (int e = threadIdx.x; e <= a.E; e += kRouteThreads) a.offsets[e] = start[e];
-    const int64_t first = (int64_t)blockIdx.x * rows_per_block * a.k;
-    const int64_t end = min(first + (int64_t)rows_per_block * a.k, a.T * a.k);
-    for (int64_t p = first + threadIdx.x; p < end; p += kRouteThreads) {
-        const int e = a.experts[p];
-        if (e >= 0) {
-            const int at = start[e] + count[(int64_t)e * blocks + blockIdx.x] + a.slot[p];
-            a.slot[p] = at;
-            a.order[at] = (int32_t)p;
+    __shared__ int32_t all[kMaxExperts], before[kMaxExperts], start[kMaxExperts + 1], wave_total[kWaves];
+    const int mine = blockIdx.x;
+    if constexpr (SUM) {
+        const int sub = threadIdx.x & 15;
+        for (int e = threadIdx.x >> 4; e < a.E; e += kRouteThreads / 16) {
+            const int32_t* const row = count + (int64_t)e * blocks;
+            int sum = 0, earlier = 0;
+            for (int b = sub; b < blocks; b += 16) {
+                const int c = row[b];
+                sum += c;
+                earlier += b < mine ? c : 0;
+            }
+            sum = lanes_sum16(sum);
+            earlier = lanes_sum16(earlier);
+            if (sub == 0) {
+                all[e] = sum;
+                before[e] = earlier;
+            }
         }
-        if (p >= start[a.E]) a.order[p] = -1;  // places that no pair has
+    } else {
+        for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
+            all[e] = total[e];
+            before[e] = count[(int64_t)e * blocks + mine];
+        }
     }
+    __syncthreads();
+    block_offsets(all, start, a.E, wave_total);
+    if (mine == 0)
+        for (int e = threadIdx.x; e <= a.E; e += kRouteThreads) a.offsets[e] = start[e];
+    const int64_t p = (int64_t)mine * rows_per_block * a.k + threadIdx.x;
+    if ((int)threadIdx.x >= rows_per_block * a.k || p >= a.T * a.k) return;
+    const int e = a.experts[p];
+    if (e >= 0) {
+        const int at = start[e] + before[e] + a.slot[p];
+        a.slot[p] = at;
+        a.order[at] = (int32_t)p;
+    }
+    if (p >= start[a.E]) a.order[p] = -1;
 }
 
 // dl_e = p_e ([e chosen] dg_e - sum of g dg) with p over all experts, or, renormalised, the same over the chosen ones alone.
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(RouteGradArgs a)
+__global__ __launch_bounds__(kGradThreads) void route_grad_kernel(RouteGradArgs a)
 {
-    constexpr int kGroups = kRouteThreads / LANES;
+    constexpr int kGroups = kGradThreads / LANES;
     const int sub = threadIdx.x & (LANES - 1);
     const int64_t t = (int64_t)blockIdx.x * kGroups + threadIdx.x / LANES;
     if (t >= a.T) return;
@@ -384,10 +416,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(RouteGradArgs
 #pragma unroll
         for (int v = 0; v < V; ++v) d[v] += e == v ? g : 0.0f;
     }
-    T* __restrict__ out = static_cast<T*>(a.dlogits) + t * a.ldd;
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (sub * V + v < a.E) out[sub * V + v] = (T)d[v];
+    store_row<T, V>(static_cast<T*>(a.dlogits) + t * a.ldd, sub * V, a.E, d);
 }
 
 template <typename F, typename T>
@@ -412,7 +441,7 @@ bool by_type(int dtype, int E, F&& f)
     }
 }
 
-// Rows of a block: up to kBlockPairs pairs; 64 rows unless there are so many tokens that the blocks' counts would be long.
+// Rows of a block: 64, a pass of its groups of sixteen lanes; a thread has one pair at most.
 int rows_per_block(int64_t T, int k)
 {
     const int most = kBlockPairs / k;
@@ -423,7 +452,7 @@ struct RouteFew {
     const RouteArgs& a;
     hipStream_t s;
     template <typename T, int LANES, int V>
-    void operator()() const { route_few_kernel<T, LANES, V><<<1, kRouteThreads, 0, s>>>(a); }
+    void operator()() const { route_few_kernel<T, LANES, V><<<1, kRouteThreads, route_shared_bytes(a.E), s>>>(a); }
 };
 struct RouteChoose {
     const RouteArgs& a;
@@ -431,7 +460,7 @@ struct RouteChoose {
     int rows, blocks;
     int32_t* count;
     template <typename T, int LANES, int V>
-    void operator()() const { route_choose_kernel<T, LANES, V><<<blocks, kRouteThreads, 0, s>>>(a, rows, count, blocks); }
+    void operator()() const { route_choose_kernel<T, LANES, V><<<blocks, kRouteThreads, route_shared_bytes(a.E), s>>>(a, rows, count, blocks); }
 };
 struct RouteGrad {
     const RouteGradArgs& a;
@@ -439,12 +468,12 @@ struct RouteGrad {
     template <typename T, int LANES, int V>
     void operator()() const
     {
-        constexpr int kGroups = kRouteThreads / LANES;
-        route_grad_kernel<T, LANES, V><<<(unsigned)((a.T + kGroups - 1) / kGroups), kRouteThreads, 0, s>>>(a);
+        constexpr int kGroups = kGradThreads / LANES;
+        route_grad_kernel<T, LANES, V><<<(unsigned)((a.T + kGroups - 1) / kGroups), kGradThreads, 0, s>>>(a);
     }
 };
 
-// One workgroup for all tokens: up to 64 rows, four passes of its sixteen groups of lanes.
+// One workgroup for all tokens: as many as a block of more has.
 bool route_in_one(int64_t T, int k) { return T <= 64 && T * k <= kBlockPairs; }
 
 }  // namespace
@@ -465,8 +494,12 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s)
     const int rows = rows_per_block(a.T, a.k), blocks = (int)((a.T + rows - 1) / rows);
     int32_t *count = static_cast<int32_t*>(a.workspace), *total = count + (int64_t)a.E * blocks;
     by_type(a.dtype, a.E, RouteChoose{a, s, rows, blocks, count});
-    route_scan_kernel<<<(a.E + kWaves - 1) / kWaves, kRouteThreads, 0, s>>>(count, total, blocks, a.E);
-    route_place_kernel<<<blocks, kRouteThreads, 0, s>>>(a, rows, count, total, blocks);
+    if ((int64_t)a.E * blocks <= 65536) {  // 256 KB of counts to each block
+        route_place_kernel<true><<<blocks, kRouteThreads, 0, s>>>(a, rows, count, total, blocks);
+    } else {
+        route_scan_kernel<<<(a.E + 3) / 4, 256, 0, s>>>(count, total, blocks, a.E);
+        route_place_kernel<false><<<blocks, kRouteThreads, 0, s>>>(a, rows, count, total, blocks);
+    }
     return hipGetLastError();
 }
 

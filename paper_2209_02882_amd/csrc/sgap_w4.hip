@@ -6,7 +6,7 @@
 // which the matrix instruction wants them.  No weight is ever rounded: a code goes into the top of the mantissa of the
 // number 16 (16 + q, exact in both 16-bit types, one shift and one and-or for two codes), the matrix unit sums
 // (16 + q) x and, against ones, x itself over a scale's values in 32 bits, and then
-//     acc += s * (sum of (16 + q) x - (16 + z) * sum of x).
+//     acc += s * (-(16 + z) * sum of x + sum of (16 + q) x).
 // The wavefronts of a workgroup have shares of the inner dimension and are summed up through LDS at the end.
 //
 // Where x is infinite or so large that the sums overflow, that difference is no number although the definition may be
@@ -117,7 +117,7 @@ struct W4Block {
     __device__ __forceinline__ float zero_of(int nt, int s) const { return (float)(uint8_t)(zero[nt] >> (8 * s)); }
 };
 
-constexpr int most_waves(int NT, int MT) { return NT * MT > 2 ? 8 : 16; }
+constexpr int kMostWaves = 8;
 
 // NT tiles of columns and MT tiles of 16 rows to a wavefront; STEPS matrix instructions (32 values each) to a scale, or,
 // with STEPS = 4, any whole number of blocks of 128.  The wavefronts of the workgroup share the inner dimension; a block's
@@ -127,7 +127,7 @@ constexpr int most_waves(int NT, int MT) { return NT * MT > 2 ? 8 : 16; }
 // rows of 8,192 values by 8,192 columns 34 us, 53,000 of a compute unit's 74,000 clocks, where the rows' loads through LDS
 // take 16 lanes to one turn.  For rows at addresses that are multiples of 16 bytes; others load as the unit wants them.
 template <typename T, int STEPS, int NT, int MT, bool ZEROS, bool STAGED>
-__global__ __launch_bounds__(64 * most_waves(NT, MT)) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items,
+__global__ __launch_bounds__(64 * kMostWaves) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items,
                                                                               int64_t blocks, bool tail)
 {
     using Block = W4Block<T, STEPS, NT, ZEROS>;
@@ -229,15 +229,25 @@ __global__ __launch_bounds__(64 * most_waves(NT, MT)) void grouped_w4_kernel(Gro
                     sum[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int i = 0; i < STEPS; ++i) sum[mt] = mma16(xf[mt][s * STEPS + i], ones, sum[mt]);
+                    if (!ZEROS) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) sum[mt][r] *= -24.0f;  // the same zero point for all: 16 + 8
+                    }
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     const float scale = b.scale_of(nt, s);
-                    const float zero = ZEROS ? 16.0f + b.zero_of(nt, s) : 24.0f;
+                    const float zero = ZEROS ? -16.0f - b.zero_of(nt, s) : 0.0f;
                     const uint32_t d[4] = {b.w[nt].x, b.w[nt].y, b.w[nt].z, b.w[nt].w};
                     f32x4 dot[MT];
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) dot[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int mt = 0; mt < MT; ++mt) {  // the sums begin with what the zero point takes away
+                        dot[mt] = sum[mt];
+                        if (ZEROS) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) dot[mt][r] *= zero;
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < STEPS; ++i) {
                         const piece_t<T> wf = decode<T>(d[s * STEPS + i]);
@@ -248,7 +258,7 @@ __global__ __launch_bounds__(64 * most_waves(NT, MT)) void grouped_w4_kernel(Gro
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            acc[nt][mt][r] = __builtin_fmaf(scale, __builtin_fmaf(-zero, sum[mt][r], dot[mt][r]), acc[nt][mt][r]);
+                            acc[nt][mt][r] = __builtin_fmaf(scale, dot[mt][r], acc[nt][mt][r]);
                     // (or the compiler decodes everything first and runs out of registers)
                     if constexpr (NT * MT > 1) __builtin_amdgcn_sched_barrier(0);
                 }
@@ -328,7 +338,7 @@ hipError_t launch_as(const GroupedW4Args& a, const W4Sizes& z, int waves, int ro
     const bool tail = a.from.rows > 0 && a.K % kBlockK;
     static uint64_t allowed = 0;
     constexpr int kEach = STAGED ? MT * 4096 : 1024;
-    if (const hipError_t err = allow_lds(grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED>, most_waves(NT, MT) * kEach, allowed)) return err;
+    if (const hipError_t err = allow_lds(grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED>, kMostWaves * kEach, allowed)) return err;
     grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED><<<grid, 64 * waves, waves * kEach, s>>>(a, z, items, blocks, tail);
     return hipGetLastError();
 }
@@ -348,20 +358,27 @@ hipError_t run_w4(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_i
 template <typename T, int STEPS>
 hipError_t by_rows(const GroupedW4Args& a, const W4Sizes& z, hipStream_t s)
 {
-    // a wavefront for four blocks of 128 values, 4 to 16 of them
-    const int64_t w = (z.blocks_k + 3) / 4;
-    const int waves = w <= 4 ? 4 : w <= 8 ? 8 : 16, few = waves < 8 ? waves : 8;
     const int64_t mean = (a.R + a.G - 1) / a.G;
+    const int64_t most = a.G == 1 ? mean : 2 * mean;  // rows that a group has, or has often
     const auto items = [&](int rows) {
-        const int64_t n = a.G == 1 ? (mean + rows - 1) / rows : (2 * mean + rows - 1) / rows;
+        const int64_t n = (most + rows - 1) / rows;
         return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
     };
+    // Wavefronts that share the inner dimension: eight where the workgroups alone would not fill the chip, two where they
+    // do several times over, so that a wavefront's start is spread over more blocks.  8 groups of 32 rows by 4,096 x 4,096
+    // (2,048 workgroups): 8 60 us, 4 41.6, 2 35.6; 64 experts for 64 rows (5,632): 4 21.5, 2 20.7; one row by 8,192 x 8,192
+    // (512): 16 14.7, 8 12.6, 4 14.3; 128 rows by 8,192 x 8,192 (768): 8 55, 4 45, 2 48.
+    const auto waves = [&](int columns, int rows) {
+        const int64_t groups = a.G * ((z.tiles_n * kTileN + columns - 1) / columns) * items(rows);
+        int w = groups <= 512 ? 8 : groups <= 1024 ? 4 : 2;
+        while (w > 1 && w / 2 >= z.blocks_k) w /= 2;
+        return w;
+    };
     const bool staged = a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0;
-    const int64_t most = a.G == 1 ? mean : 2 * mean;  // rows that a group has, or has often
     // (one row or two: sixteen lanes of a load share a row, and the way through LDS would only be longer)
-    if (most <= 16) return run_w4<T, STEPS, 1, 1>(a, z, waves, items(16), staged && most > 2, s);
-    if (most <= 32 && staged) return run_w4<T, STEPS, 2, 2>(a, z, few, items(32), staged, s);
-    return run_w4<T, STEPS, 2, 3>(a, z, few, items(48), staged, s);
+    if (most <= 16) return run_w4<T, STEPS, 1, 1>(a, z, waves(16, 16), items(16), staged && most > 2, s);
+    if (most <= 32 && staged) return run_w4<T, STEPS, 2, 2>(a, z, waves(32, 32), items(32), staged, s);
+    return run_w4<T, STEPS, 2, 3>(a, z, waves(32, 48), items(48), staged, s);
 }
 
 template <typename T>
