@@ -64,14 +64,15 @@ struct RowSource {
         // 2^shift / div, rounded up; shift is 62 at most
         mul = (uint32_t)(((1ull << shift) + (uint64_t)div - 1) / (uint64_t)div);
     }
-    __device__ __forceinline__ int64_t row(int64_t r) const  // -1: no such row
+    // what the list says for row r, and what row of X that is (-1: none): in two steps, for who wants the first to be on
+    // its way for a while
+    __device__ __forceinline__ int32_t entry(int64_t r) const { return src ? src[r] : (int32_t)r; }
+    __device__ __forceinline__ int32_t row_of(int32_t e) const
     {
-        if (!src) return r < rows ? r : -1;
-        const int32_t s = src[r];
-        if (s < 0) return -1;
-        const int64_t t = (int64_t)(((uint64_t)(uint32_t)s * mul) >> shift);
-        return t < rows ? t : -1;
+        const int32_t t = src ? (int32_t)(((uint64_t)(uint32_t)e * mul) >> shift) : e;
+        return e < 0 || t >= rows ? -1 : t;
     }
+    __device__ __forceinline__ int64_t row(int64_t r) const { return row_of(entry(r)); }
 };
 
 // Rows first .. end of group g; nothing outside 0 .. rows whatever the offsets hold.  Without offsets: one group of all rows.

@@ -1,4 +1,5 @@
 // Products over ragged groups where rows are multiples of 16 bytes at 16-byte addresses.
+#include <algorithm>
 #include <type_traits>
 
 #include "sgap_grouped_tiles.hpp"
@@ -7,13 +8,17 @@ namespace sgap {
 
 namespace {
 
-// Work items are dealt to the eight dies (workgroup b runs on die b % 8) in runs of 32 neighbours, which share rows of X
+// Work items are dealt to the eight dies (workgroup b runs on die b % 8) in runs of RUN neighbours, which share rows of X
 // or weights in the die's L2.  Runs in turn, so that the items that turn out not to exist, all at the end, leave no die idle.
+template <int RUN>
 __device__ __forceinline__ int64_t dealt_item(uint32_t b)
 {
     const uint32_t die = b & 7, at = b >> 3;
-    return (int64_t)((at >> 5) * 8 + die) * 32 + (at & 31);
+    return (int64_t)((at / RUN) * 8 + die) * RUN + at % RUN;
 }
+// so many of a product's tiles, and so many of a gradient's: its groups' tiles differ in length, so that every die should
+// have some of each (16 groups of 128 tiles)
+constexpr int kRun = 32, kGradientRun = 16;
 
 // WIDE: rows of X lie further than 32 bits of bytes from its first.
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
@@ -24,7 +29,7 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
     constexpr int kWaves = THREADS / 64, WN = kWaves / 2, WM = 2;
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     extern __shared__ __align__(16) char lds[];
-    const int64_t item = dealt_item(blockIdx.x);
+    const int64_t item = dealt_item<kRun>(blockIdx.x);
     if (item >= items) return;
     const int64_t tile = item / column_tiles, n0 = (item - tile * column_tiles) * BN;
     const RowTile rows = find_row_tile<BM>(a.offsets, a.G, a.R, tile);
@@ -121,7 +126,7 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     constexpr int kXAt = KN ? Lt::kBytes : 0, kYAt = KN ? 0 : Lt::kBytes;
     extern __shared__ __align__(16) char lds[];
-    const int64_t item = dealt_item(blockIdx.x);
+    const int64_t item = dealt_item<kGradientRun>(blockIdx.x);
     if (item >= items) return;
     const int64_t per = tiles_m * tiles_n, g = item / per, in = item - g * per;
     const int64_t lines = KN ? a.K : a.N, columns = KN ? a.N : a.K;  // of the result
@@ -149,16 +154,18 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
 #pragma unroll
     for (int i = 0; i < kXKinds; ++i) xc[i] = (uint32_t)(min((int64_t)Xt::minor(i) * Xt::P, a.K - Xt::P - x0) * sizeof(T));
     const int first = __builtin_amdgcn_readfirstlane((int)gr.first), end = __builtin_amdgcn_readfirstlane((int)gr.end);
-    // Rows of X of the tile that is loaded next (found while the tile before is on its way), -1 where there is none; which
-    // rounds had none in the last two tiles, a bit each.
-    int32_t row[Xt::kRounds];
+    // What the list says of the rows of the tile that is loaded next (asked for while the tile before is on its way, and
+    // looked at when it has arrived: the loads come back in their order); which rounds had no row of X in the last tile and
+    // the first, a bit each.
+    int32_t entry[Xt::kRounds];
     uint32_t none[2] = {0, 0};
     int next = first + Xt::major(0);
     const auto find = [&] {
 #pragma unroll
         for (int i = 0; i < Xt::kRounds; ++i) {
             const int r = next + i * kXRowsApart;
-            row[i] = r < end ? (int32_t)a.from.row(r) : -1;
+            entry[i] = -1;
+            if (r < end) entry[i] = a.from.entry(r);
         }
         next += Xt::kInner;
     };
@@ -172,9 +179,9 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
             Yt::load(to + kYAt, i, y, there ? yo[i % kYKinds] + r * down : yo[i % kYKinds] - Yt::major(0) * down);
         } else {
             const int x = i - Yt::kRounds;
-            const int32_t r = max(row[x], 0);
+            const int32_t found = a.from.row_of(entry[x]), r = max(found, 0);
             none[1] = x == 0 ? 0 : none[1];
-            none[1] |= row[x] < 0 ? 1u << x : 0u;
+            none[1] |= found < 0 ? 1u << x : 0u;
             if constexpr (WIDE) Xt::load(to + kXAt, x, X + r * a.ldx * (int64_t)sizeof(T) + xc[x % kXKinds]);
             else Xt::load(to + kXAt, x, X, (uint32_t)r * (uint32_t)(a.ldx * sizeof(T)) + xc[x % kXKinds]);
             if (x == Xt::kRounds - 1) find();
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     const int tiles = (end - first + Lt::kInner - 1) / Lt::kInner;
     find();
 #pragma unroll
-    for (int i = 0; i < Xt::kRounds; ++i) none[0] |= row[i] < 0 ? 1u << i : 0u;
+    for (int i = 0; i < Xt::kRounds; ++i) none[0] |= a.from.row_of(entry[i]) < 0 ? 1u << i : 0u;
     multiply_tiles<Lt, Rt, MI, NJ>(lds, tiles, load, mend, wn, wm, true, acc);
     T* __restrict__ dW = static_cast<T*>(const_cast<void*>(a.W)) + g * a.N * a.K;
 #pragma unroll
@@ -218,6 +225,7 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     }
 }
 
+// whole turns of the dies' runs
 unsigned dealt_grid(int64_t items) { return (unsigned)((items + 255) / 256 * 256); }
 
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
@@ -251,19 +259,23 @@ double turns(int64_t tiles, int compute_units, int BM, int BN, double rate)
     return (double)((tiles + compute_units - 1) / compute_units) * BM * BN / rate;
 }
 
-// 256 x 256, 128 x 128 or 64 x 128, whichever leaves the least to the unit that has most; groups end half a tile early in
-// the mean.  In one group of 8,192 rows, K = N = 4,096, the large tile reaches 1.31 PFLOP/s, the middle one 0.95.  Floats,
-// whose products take sixteen times as long, lose nothing with small tiles: 8 groups, 4,096 rows, 1,024 x 1,024: 243 us
-// with 256 x 256, 135 with 128 x 128.
+// 256 x 256, 128 x 128 or 64 x 128, whichever leaves the least to the unit that has most.  A group has a last tile that
+// is not full: 0.6 of a tile more than its rows in the mean.  16 groups, 16,384 rows, 4,096 x 2,048 bf16: 317 us with
+// 256 x 256, 372 with 128 x 128; 64 groups, 8,192 rows, 1,024 x 2,048: 101 and 86.  Floats, whose products take sixteen
+// times as long, lose nothing with small tiles: 8 groups, 4,096 rows, 1,024 x 1,024: 243 us with 256 x 256, 135 with
+// 128 x 128, 97 with 64 x 128.
 template <typename T, bool KN, bool WIDE>
 hipError_t by_size(const GroupedArgs& a, hipStream_t s)
 {
-    const int cus = a.compute_units;
-    const bool wide = sizeof(T) == 2;
-    const auto tiles = [&](int BM, int BN) { return (a.R / BM + (a.G + 1) / 2) * ((a.N + BN - 1) / BN); };
-    const double large = turns(tiles(256, 256), cus, 256, 256, 1.0), middle = turns(tiles(128, 128), cus, 128, 128, wide ? 0.75 : 1.0),
-                 small = turns(tiles(64, 128), cus, 64, 128, wide ? 0.6 : 0.95);
-    if (wide && large <= middle && large <= small) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    constexpr bool kHalf = sizeof(T) == 2;
+    const auto tiles = [&](int BM, int BN) {
+        const double down = a.G == 1 ? (double)((a.R + BM - 1) / BM) : (double)a.R / BM + 0.6 * (double)a.G;
+        return (int64_t)(down * (double)((a.N + BN - 1) / BN));
+    };
+    const double large = turns(tiles(256, 256), a.compute_units, 256, 256, 1.0);
+    const double middle = turns(tiles(128, 128), a.compute_units, 128, 128, kHalf ? 0.7 : 1.0);
+    const double small = turns(tiles(64, 128), a.compute_units, 64, 128, kHalf ? 0.55 : 0.95);
+    if (kHalf && large <= std::min(middle, small)) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
     if (middle <= small) return run_fast<T, 128, 128, KN, WIDE, 256>(a, s);
     return run_fast<T, 64, 128, KN, WIDE, 256>(a, s);
 }

@@ -20,11 +20,11 @@ namespace sgap {
 namespace {
 
 constexpr int kRouteThreads = 1024;  // sixteen wavefronts: what hides the rounds' latency
+constexpr int kFewThreads = 256;     // a few tokens: a start and barriers that cost less
 constexpr int kGradThreads = 256;
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxChosen = 16;
 constexpr int kBlockPairs = 1024;  // pairs of a block at most
-constexpr int kWaves = kRouteThreads / 64;
 
 // Ordered like the floats: NaN above everything (as a sort has it), -infinity, which is never chosen, 0.  -0 is +0.
 __device__ __forceinline__ uint32_t order_key(float x)
@@ -163,13 +163,13 @@ __device__ __forceinline__ float choose(const float (&x)[V], int k, bool renorma
 // share of them.
 struct RouteShared {
     int32_t* expert;  // kBlockPairs
-    uint16_t* count;  // kWaves x E
+    uint16_t* count;  // wavefronts x E
 };
 __device__ __forceinline__ RouteShared route_shared(char* lds)
 {
     return {reinterpret_cast<int32_t*>(lds), reinterpret_cast<uint16_t*>(lds + kBlockPairs * 4)};
 }
-int route_shared_bytes(int E) { return kBlockPairs * 4 + kWaves * E * 2; }
+int route_shared_bytes(int threads, int E) { return kBlockPairs * 4 + threads / 64 * E * 2; }
 
 // A wavefront's share of the block's pairs: 64 of them, or a part.
 __device__ __forceinline__ int my_pair() { return threadIdx.x; }
@@ -196,11 +196,12 @@ __device__ __forceinline__ int rank_pair(const RouteShared& s, int E, int pairs)
 }
 
 // count[w][e] becomes the pairs of e in the shares before w; the sum of all of them
+template <int THREADS>
 __device__ __forceinline__ int sum_shares(const RouteShared& s, int E, int e)
 {
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         const int c = s.count[w * E + e];
         s.count[w * E + e] = (uint16_t)sum;
         sum += c;
@@ -209,10 +210,10 @@ __device__ __forceinline__ int sum_shares(const RouteShared& s, int E, int e)
 }
 
 // Rows of the block are chosen for, their experts left in s.expert.
-template <typename T, int LANES, int V>
+template <typename T, int LANES, int V, int THREADS>
 __device__ __forceinline__ void choose_rows(const RouteArgs& a, const RouteShared& s, int64_t row0, int rows)
 {
-    constexpr int kGroups = kRouteThreads / LANES;
+    constexpr int kGroups = THREADS / LANES;
     const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES;
     for (int i = group; i < rows; i += kGroups) {
         const int64_t t = row0 + i;
@@ -236,18 +237,19 @@ __device__ __forceinline__ int wave_scan(int v)
 }
 
 // out[e] = sum of in[0 .. e) for e <= n, by the whole workgroup, through shared memory
+template <int THREADS>
 __device__ __forceinline__ void block_offsets(const int32_t* in, int32_t* out, int n, int32_t* wave_total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int carry = 0;
-    for (int e0 = 0; e0 < n; e0 += kRouteThreads) {
+    for (int e0 = 0; e0 < n; e0 += THREADS) {
         const int e = e0 + threadIdx.x;
         const int v = e < n ? in[e] : 0;
         const int inc = wave_scan(v);
         if (lane == 63) wave_total[wave] = inc;
         __syncthreads();
         int base = carry;
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w < wave) base += wave_total[w];
             carry += wave_total[w];
         }
@@ -259,21 +261,21 @@ __device__ __forceinline__ void block_offsets(const int32_t* in, int32_t* out, i
 }
 
 // All tokens in one workgroup: one launch, which is what a few tokens cost.
-template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_few_kernel(RouteArgs a)
+template <typename T, int LANES, int V, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_few_kernel(RouteArgs a)
 {
     extern __shared__ __align__(16) char lds[];
-    __shared__ int32_t total[kMaxExperts], start[kMaxExperts + 1], wave_total[kWaves];
+    __shared__ int32_t total[kMaxExperts], start[kMaxExperts + 1], wave_total[THREADS / 64];
     const RouteShared s = route_shared(lds);
     const int pairs = (int)a.T * a.k, p = my_pair();
-    choose_rows<T, LANES, V>(a, s, 0, (int)a.T);
+    choose_rows<T, LANES, V, THREADS>(a, s, 0, (int)a.T);
     __syncthreads();
     const int rank = rank_pair(s, a.E, pairs);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) total[e] = sum_shares(s, a.E, e);
+    for (int e = threadIdx.x; e < a.E; e += THREADS) total[e] = sum_shares<THREADS>(s, a.E, e);
     __syncthreads();
-    block_offsets(total, start, a.E, wave_total);
-    for (int e = threadIdx.x; e <= a.E; e += kRouteThreads) a.offsets[e] = start[e];
+    block_offsets<THREADS>(total, start, a.E, wave_total);
+    for (int e = threadIdx.x; e <= a.E; e += THREADS) a.offsets[e] = start[e];
     if (p >= pairs) return;
     const int e = s.expert[p];
     const int at = e >= 0 ? start[e] + s.count[(threadIdx.x >> 6) * a.E + e] + rank : -1;
@@ -283,21 +285,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(RouteArgs a)
     if (p >= start[a.E]) a.order[p] = -1;  // places that no pair has
 }
 
-// More tokens: the choice, with the blocks' counts by expert (count[e * blocks + b]) and the pairs' ranks within their
+// More tokens: the choice, with the blocks' counts by expert (count[e * stride + b]) and the pairs' ranks within their
 // block (in slot) ...
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, int rows_per_block, int32_t* count, int blocks)
+__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, int rows_per_block, uint16_t* count, int stride)
 {
     extern __shared__ __align__(16) char lds[];
     const RouteShared s = route_shared(lds);
     const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
     const int rows = (int)min((int64_t)rows_per_block, a.T - row0);
     const int pairs = rows * a.k, p = my_pair();
-    choose_rows<T, LANES, V>(a, s, row0, rows);
+    choose_rows<T, LANES, V, kRouteThreads>(a, s, row0, rows);
     __syncthreads();
     const int rank = rank_pair(s, a.E, pairs);
     __syncthreads();
-    for (int e = threadIdx.x; e < a.E; e += kRouteThreads) count[(int64_t)e * blocks + blockIdx.x] = sum_shares(s, a.E, e);
+    for (int e = threadIdx.x; e < a.E; e += kRouteThreads)
+        count[(int64_t)e * stride + blockIdx.x] = (uint16_t)sum_shares<kRouteThreads>(s, a.E, e);
     __syncthreads();
     if (p >= pairs) return;
     const int e = s.expert[p];
@@ -306,39 +309,43 @@ __global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a
 }
 
 // ... the counts of one expert summed up over the blocks (a wavefront per expert), where there are many of them ...
-__global__ __launch_bounds__(256) void route_scan_kernel(int32_t* count, int32_t* total, int blocks, int E)
+__global__ __launch_bounds__(256) void route_scan_kernel(const uint16_t* count, int32_t* before, int32_t* total, int blocks, int stride, int E)
 {
     const int e = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (e >= E) return;
-    int32_t* row = count + (int64_t)e * blocks;
     int carry = 0;
     for (int b0 = 0; b0 < blocks; b0 += 64) {
         const int b = b0 + lane;
-        const int v = b < blocks ? row[b] : 0;
+        const int v = b < blocks ? count[(int64_t)e * stride + b] : 0;
         const int inc = wave_scan(v);
-        if (b < blocks) row[b] = carry + inc - v;
+        if (b < blocks) before[(int64_t)e * stride + b] = carry + inc - v;
         carry += __shfl(inc, 63);
     }
     if (lane == 0) total[e] = carry;
 }
 
-// ... and every pair into its place.  SUM: sixteen lanes sum up the counts of an expert, those of the blocks before this one
-// and all of them.
+// ... and every pair into its place.  SUM: sixteen lanes sum up the counts of an expert, eight to a load: those of the
+// blocks before this one, and all of them.
 template <bool SUM>
-__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a, int rows_per_block, const int32_t* count,
-                                                                    const int32_t* total, int blocks)
+__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a, int rows_per_block, const uint16_t* count,
+                                                                    const int32_t* summed, const int32_t* total, int blocks, int stride)
 {
-    __shared__ int32_t all[kMaxExperts], before[kMaxExperts], start[kMaxExperts + 1], wave_total[kWaves];
+    __shared__ int32_t all[kMaxExperts], before[kMaxExperts], start[kMaxExperts + 1], wave_total[kRouteThreads / 64];
     const int mine = blockIdx.x;
     if constexpr (SUM) {
         const int sub = threadIdx.x & 15;
         for (int e = threadIdx.x >> 4; e < a.E; e += kRouteThreads / 16) {
-            const int32_t* const row = count + (int64_t)e * blocks;
             int sum = 0, earlier = 0;
-            for (int b = sub; b < blocks; b += 16) {
-                const int c = row[b];
-                sum += c;
-                earlier += b < mine ? c : 0;
+#pragma unroll 2
+            for (int b = sub * 8; b < blocks; b += 128) {
+                const uint4 v = *reinterpret_cast<const uint4*>(count + (int64_t)e * stride + b);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = (int)(i & 1 ? w[i >> 1] >> 16 : w[i >> 1] & 0xffffu);
+                    sum += b + i < blocks ? c : 0;
+                    earlier += b + i < mine ? c : 0;
+                }
             }
             sum = lanes_sum16(sum);
             earlier = lanes_sum16(earlier);
@@ -350,11 +357,11 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a,
     } else {
         for (int e = threadIdx.x; e < a.E; e += kRouteThreads) {
             all[e] = total[e];
-            before[e] = count[(int64_t)e * blocks + mine];
+            before[e] = summed[(int64_t)e * stride + mine];
         }
     }
     __syncthreads();
-    block_offsets(all, start, a.E, wave_total);
+    block_offsets<kRouteThreads>(all, start, a.E, wave_total);
     if (mine == 0)
         for (int e = threadIdx.x; e <= a.E; e += kRouteThreads) a.offsets[e] = start[e];
     const int64_t p = (int64_t)mine * rows_per_block * a.k + threadIdx.x;
@@ -452,15 +459,45 @@ struct RouteFew {
     const RouteArgs& a;
     hipStream_t s;
     template <typename T, int LANES, int V>
-    void operator()() const { route_few_kernel<T, LANES, V><<<1, kRouteThreads, route_shared_bytes(a.E), s>>>(a); }
+    void operator()() const
+    {
+        // a pass of the small block's groups of lanes, and a pair to a thread
+        if (a.T <= kFewThreads / LANES && a.T * a.k <= kFewThreads)
+            route_few_kernel<T, LANES, V, kFewThreads><<<1, kFewThreads, route_shared_bytes(kFewThreads, a.E), s>>>(a);
+        else
+            route_few_kernel<T, LANES, V, kRouteThreads><<<1, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(a);
+    }
 };
+
+// Where the counts lie in the workspace.
+struct RouteCounts {
+    int rows, blocks, stride;        // rows of a block; blocks, and as many in whole loads
+    int64_t summed_at, total_at, bytes;
+    bool each;                       // each block sums them up for itself: no more than 128 KB of them
+};
+RouteCounts route_counts(int64_t T, int64_t E, int k)
+{
+    RouteCounts c;
+    c.rows = rows_per_block(T, k);
+    c.blocks = (int)((T + c.rows - 1) / c.rows);
+    c.stride = (c.blocks + 7) / 8 * 8;
+    c.each = E * c.stride <= 65536;
+    c.summed_at = (E * c.stride * 2 + 15) / 16 * 16;
+    c.total_at = c.summed_at + (c.each ? 0 : E * c.stride * 4);
+    c.bytes = c.total_at + (c.each ? 0 : E * 4);
+    return c;
+}
+
 struct RouteChoose {
     const RouteArgs& a;
+    const RouteCounts& c;
     hipStream_t s;
-    int rows, blocks;
-    int32_t* count;
     template <typename T, int LANES, int V>
-    void operator()() const { route_choose_kernel<T, LANES, V><<<blocks, kRouteThreads, route_shared_bytes(a.E), s>>>(a, rows, count, blocks); }
+    void operator()() const
+    {
+        route_choose_kernel<T, LANES, V><<<c.blocks, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(
+            a, c.rows, static_cast<uint16_t*>(a.workspace), c.stride);
+    }
 };
 struct RouteGrad {
     const RouteGradArgs& a;
@@ -480,9 +517,7 @@ bool route_in_one(int64_t T, int k) { return T <= 64 && T * k <= kBlockPairs; }
 
 int64_t route_workspace_bytes(int64_t T, int64_t E, int64_t k)
 {
-    if (route_in_one(T, (int)k)) return 0;
-    const int64_t rows = rows_per_block(T, (int)k), blocks = (T + rows - 1) / rows;
-    return 4 * E * (blocks + 1);
+    return route_in_one(T, (int)k) ? 0 : route_counts(T, E, (int)k).bytes;
 }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s)
@@ -491,14 +526,16 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t s)
         by_type(a.dtype, a.E, RouteFew{a, s});
         return hipGetLastError();
     }
-    const int rows = rows_per_block(a.T, a.k), blocks = (int)((a.T + rows - 1) / rows);
-    int32_t *count = static_cast<int32_t*>(a.workspace), *total = count + (int64_t)a.E * blocks;
-    by_type(a.dtype, a.E, RouteChoose{a, s, rows, blocks, count});
-    if ((int64_t)a.E * blocks <= 65536) {  // 256 KB of counts to each block
-        route_place_kernel<true><<<blocks, kRouteThreads, 0, s>>>(a, rows, count, total, blocks);
+    const RouteCounts c = route_counts(a.T, a.E, a.k);
+    char* const at = static_cast<char*>(a.workspace);
+    const uint16_t* const count = reinterpret_cast<const uint16_t*>(at);
+    int32_t *summed = reinterpret_cast<int32_t*>(at + c.summed_at), *total = reinterpret_cast<int32_t*>(at + c.total_at);
+    by_type(a.dtype, a.E, RouteChoose{a, c, s});
+    if (c.each) {
+        route_place_kernel<true><<<c.blocks, kRouteThreads, 0, s>>>(a, c.rows, count, nullptr, nullptr, c.blocks, c.stride);
     } else {
-        route_scan_kernel<<<(a.E + 3) / 4, 256, 0, s>>>(count, total, blocks, a.E);
-        route_place_kernel<false><<<blocks, kRouteThreads, 0, s>>>(a, rows, count, total, blocks);
+        route_scan_kernel<<<(a.E + 3) / 4, 256, 0, s>>>(count, summed, total, c.blocks, c.stride, a.E);
+        route_place_kernel<false><<<c.blocks, kRouteThreads, 0, s>>>(a, c.rows, count, summed, total, c.blocks, c.stride);
     }
     return hipGetLastError();
 }
