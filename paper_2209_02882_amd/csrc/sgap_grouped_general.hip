@@ -11,14 +11,29 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The 16 bytes at p, of which `count` elements are there (all of them, or fewer: one by one).
+// The 16 bytes at p, of which `count` elements are there, zeros behind them; `before`: elements of the row in front of p.
+// At the end of a row the 16 bytes up to the end are read and moved down.
 template <typename T>
-__device__ __forceinline__ piece_t<T> part_of_piece(const T* __restrict__ p, int64_t count)
+__device__ __forceinline__ piece_t<T> part_of_piece(const T* __restrict__ p, int count, int before)
 {
-    if (count >= Piece<T>::kCount) return load_piece(p);
+    constexpr int P = Piece<T>::kCount;
+    if (count >= P) return load_piece(p);
+    if (count <= 0) return piece_t<T>{};
+    if (count + before >= P) {
+        union {
+            piece_t<T> v;
+            uint64_t u[2];
+        } r;
+        r.v = load_piece(p - (P - count));
+        const int down = (P - count) * (int)sizeof(T) * 8;  // bits, 16 to 112
+        const uint64_t lo = down < 64 ? r.u[0] >> down | r.u[1] << (64 - down) : r.u[1] >> (down - 64);
+        r.u[1] = down < 64 ? r.u[1] >> down : 0;
+        r.u[0] = lo;
+        return r.v;
+    }
     piece_t<T> v = {};
 #pragma unroll
-    for (int j = 0; j < Piece<T>::kCount; ++j)
+    for (int j = 0; j < P; ++j)
         if (j < count) v[j] = p[j];
     return v;
 }
@@ -46,7 +61,7 @@ __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a
     constexpr int BN = 128;
     using Wt = Tile<T, BN, !KN, kThreads>;
     using Xt = Tile<T, BM, true, kThreads>;
-    constexpr int WN = BM >= 128 ? 2 : 4, WM = 4 / WN;  // wavefronts along the columns and the rows
+    constexpr int WN = BM >= 64 ? 2 : 4, WM = 4 / WN;  // wavefronts along the columns and the rows
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     __shared__ __align__(16) char lds[2 * (Wt::kBytes + Xt::kBytes)];
     const int64_t tile = blockIdx.x / column_tiles, n0 = (blockIdx.x - tile * column_tiles) * BN;
@@ -60,25 +75,39 @@ __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (rows.g < a.G) {
-        const T* const W = static_cast<const T*>(a.W) + rows.g * a.N * a.K;
+        // where each load of the next tile begins: the tiles come in their order, and a step from one to the next is the
+        // same for all (64-bit products for every load are what this kernel was bound by)
+        const int N = (int)a.N, K = (int)a.K;
+        const int64_t down = KN ? Wt::kInner * a.N : Wt::kInner;
+        const T* w[Wt::kRounds];
         const T* x[Xt::kRounds];
+#pragma unroll
+        for (int i = 0; i < Wt::kRounds; ++i) {
+            const int64_t k = KN ? Wt::major(i) : Wt::minor(i) * Wt::P, n = n0 + (KN ? Wt::minor(i) * Wt::P : Wt::major(i));
+            w[i] = static_cast<const T*>(a.W) + rows.g * a.N * a.K + (KN ? k * a.N + n : n * a.K + k);
+        }
+        uint32_t real = 0;  // rounds whose row of X there is
 #pragma unroll
         for (int i = 0; i < Xt::kRounds; ++i) {
             const int m = Xt::major(i);
             const int64_t r = m < rows.rows ? a.from.row(rows.first + m) : -1;
-            x[i] = r >= 0 ? static_cast<const T*>(a.X) + r * a.ldx : nullptr;
+            real |= r >= 0 ? 1u << i : 0u;
+            x[i] = static_cast<const T*>(a.X) + r * a.ldx + Xt::minor(i) * Xt::P;
         }
         const auto fetch = [&](int t, int i) -> piece_t<T> {
-            const int64_t k0 = (int64_t)t * Wt::kInner;
+            const int k0 = t * Wt::kInner;
+            piece_t<T> v = {};
             if (i >= Wt::kRounds) {
-                const int r = i - Wt::kRounds;
-                const int64_t k = k0 + Xt::minor(r) * Xt::P;
-                return x[r] ? part_of_piece(x[r] + k, a.K - k) : piece_t<T>{};
+                const int r = i - Wt::kRounds, k = k0 + Xt::minor(r) * Xt::P;
+                if (real >> r & 1) v = part_of_piece(x[r], K - k, k);
+                x[r] += Xt::kInner;
+                return v;
             }
-            const int64_t k = k0 + (KN ? Wt::major(i) : Wt::minor(i) * Wt::P);
-            const int64_t n = n0 + (KN ? Wt::minor(i) * Wt::P : Wt::major(i));
-            if (k >= a.K || n >= a.N) return piece_t<T>{};
-            return KN ? part_of_piece(W + k * a.N + n, a.N - n) : part_of_piece(W + n * a.K + k, a.K - k);
+            const int k = k0 + (KN ? Wt::major(i) : Wt::minor(i) * Wt::P);
+            const int n = (int)n0 + (KN ? Wt::minor(i) * Wt::P : Wt::major(i));
+            if (k < K && n < N) v = KN ? part_of_piece(w[i], N - n, n) : part_of_piece(w[i], K - k, k);
+            w[i] += down;
+            return v;
         };
         multiply_tiles_staged<Wt, Xt, MI, NJ, T>(lds, (int)((a.K + Wt::kInner - 1) / Wt::kInner), fetch, wn, wm, acc);
     }
@@ -113,17 +142,33 @@ __global__ __launch_bounds__(kThreads) void grouped_wgrad_general_kernel(Grouped
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const T* const X = static_cast<const T*>(a.X);
-    const T* const dY = static_cast<const T*>(a.Y);
+    // The loads of a tile: rows of the first operand, which has the result's columns, then of the second.  Those of dY
+    // begin a step further down with every tile; what the list says of X's rows is asked for a tile ahead.
+    constexpr int kRounds = Bt::kRounds, kXAt = KN ? kRounds : 0, kYAt = KN ? 0 : kRounds;
+    const int first = (int)gr.first, end = (int)gr.end, N = (int)a.N, K = (int)a.K;
+    const int x0 = (int)(KN ? m0 : n0), y0 = (int)(KN ? n0 : m0);
+    const T* y[kRounds];
+    int32_t entry[kRounds];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+        y[i] = static_cast<const T*>(a.Y) + (gr.first + Bt::major(i)) * a.ldy + y0 + Bt::minor(i) * Bt::P;
+        entry[i] = first + Bt::major(i) < end ? a.from.entry(first + Bt::major(i)) : -1;
+    }
     const auto fetch = [&](int t, int i) -> piece_t<T> {
-        const int64_t r = gr.first + (int64_t)t * Bt::kInner + Bt::major(i % Bt::kRounds);
-        const bool first = i < Bt::kRounds;  // the operand that has the result's columns
-        const int64_t line = (first ? n0 : m0) + Bt::minor(i % Bt::kRounds) * Bt::P;
-        if (r >= gr.end || line >= (first ? columns : lines)) return piece_t<T>{};
-        if (first == KN) return part_of_piece(dY + r * a.ldy + line, a.N - line);
-        const int64_t row = a.from.row(r);
-        return row >= 0 ? part_of_piece(X + row * a.ldx + line, a.K - line) : piece_t<T>{};
+        const int round = i % kRounds, r = first + t * Bt::kInner + Bt::major(round);
+        piece_t<T> v = {};
+        if (i - round == kYAt) {
+            const int line = y0 + Bt::minor(round) * Bt::P;
+            if (r < end && line < N) v = part_of_piece(y[round], N - line, line);
+            y[round] += Bt::kInner * a.ldy;
+        } else {
+            const int line = x0 + Bt::minor(round) * Bt::P, row = a.from.row_of(entry[round]);
+            if (r < end && line < K && row >= 0) v = part_of_piece(static_cast<const T*>(a.X) + row * a.ldx + line, K - line, line);
+            entry[round] = r + Bt::kInner < end ? a.from.entry(r + Bt::kInner) : -1;
+        }
+        return v;
     };
+    static_assert(kXAt + kYAt == kRounds, "");
     multiply_tiles_staged<Bt, Bt, 4, 4, T>(lds, (int)((gr.end - gr.first + Bt::kInner - 1) / Bt::kInner), fetch, wn, wm, acc);
     T* __restrict__ dW = static_cast<T*>(const_cast<void*>(a.W)) + g * a.N * a.K;
 #pragma unroll
@@ -151,8 +196,11 @@ hipError_t general(const GroupedArgs& a, hipStream_t s)
 template <typename T>
 hipError_t by_rows(const GroupedArgs& a, hipStream_t s)
 {
-    // tiles as long as a group is in the mean: an empty half of a tile costs as much as a full one
+    // Tiles no longer than a group is in the mean (an empty half of a tile costs as much as a full one), and shorter ones
+    // where there are not enough for the chip.
     if (a.R <= 48 * a.G) return general<T, 32>(a, s);
+    const int64_t columns = (a.N + 127) / 128;
+    if ((a.R / 128 + a.G / 2) * columns < 3 * a.compute_units) return general<T, 64>(a, s);
     return general<T, 128>(a, s);
 }
 
