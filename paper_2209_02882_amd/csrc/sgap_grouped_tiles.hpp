@@ -212,9 +212,10 @@ __device__ __forceinline__ void multiply_tiles(char* shared, int tiles, F&& load
 
 // The same where the loads cannot go past the registers (rows at addresses that are no multiples of 16 bytes): a tile's
 // pieces wait in registers from the middle of one tile to the middle of the next and are then put into LDS.
-//   fetch(t, i)  piece i of LOADS of tile t, zeros for what is not there
-template <typename L, typename R, int MI, int NJ, typename T, typename F>
-__device__ __forceinline__ void multiply_tiles_staged(char* shared, int tiles, F&& fetch, int l0, int r0, f32x4 (&acc)[MI][NJ])
+//   fetch(t, i)    piece i of LOADS of tile t as it lies in memory; called for one tile after the other
+//   mend(t, i, v)  what of it belongs there, looked at when it has arrived
+template <typename L, typename R, int MI, int NJ, typename T, typename F, typename M>
+__device__ __forceinline__ void multiply_tiles_staged(char* shared, int tiles, F&& fetch, M&& mend, int l0, int r0, f32x4 (&acc)[MI][NJ])
 {
     constexpr uint32_t kStage = L::kBytes + R::kBytes;
     constexpr int kLoads = L::kRounds + R::kRounds;
@@ -246,14 +247,14 @@ __device__ __forceinline__ void multiply_tiles_staged(char* shared, int tiles, F
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) coming[i] = fetch(t, i);
     };
-    const auto put = [&](uint32_t stage) {
+    const auto put = [&](int t, uint32_t stage) {
 #pragma unroll
-        for (int i = 0; i < L::kRounds; ++i) L::put(lds + stage, i, coming[i]);
+        for (int i = 0; i < L::kRounds; ++i) L::put(lds + stage, i, mend(t, i, coming[i]));
 #pragma unroll
-        for (int i = 0; i < R::kRounds; ++i) R::put(lds + stage + L::kBytes, i, coming[L::kRounds + i]);
+        for (int i = 0; i < R::kRounds; ++i) R::put(lds + stage + L::kBytes, i, mend(t, L::kRounds + i, coming[L::kRounds + i]));
     };
     get(0);
-    put(0);
+    put(0, 0);
     get(1);
     __syncthreads();
     at(0);
@@ -263,7 +264,7 @@ __device__ __forceinline__ void multiply_tiles_staged(char* shared, int tiles, F
         const uint32_t stage = (t & 1) * kStage;
         at(stage);
         half(0);
-        if (t + 1 < tiles) put(kStage - stage);
+        if (t + 1 < tiles) put(t + 1, kStage - stage);
         __syncthreads();
         get(t + 2);
         at(kStage - stage);
