@@ -91,7 +91,12 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
             for (int i = 0; i < Xt::kRounds; ++i)
                 if (Xt::minor(i) * Xt::P >= there) Xt::clear(to + Wt::kBytes, i);
         };
-        multiply_tiles<Wt, Xt, MI, NJ>(lds, tiles, load, mend, wn, wm, active, acc);
+        bool done = false;
+        if constexpr (sizeof(T) == 4) {
+            multiply_tiles_split<Wt, Xt, MI, NJ>(lds, tiles, load, mend, wn, wm, active, acc);
+            done = !start_over(acc);
+        }
+        if (!done) multiply_tiles<Wt, Xt, MI, NJ>(lds, tiles, load, mend, wn, wm, active, acc);
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -159,7 +164,7 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     // the first, a bit each.
     int32_t entry[Xt::kRounds];
     uint32_t none[2] = {0, 0};
-    int next = first + Xt::major(0);
+    int next;
     const auto find = [&] {
 #pragma unroll
         for (int i = 0; i < Xt::kRounds; ++i) {
@@ -202,10 +207,23 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
         }
     };
     const int tiles = (end - first + Lt::kInner - 1) / Lt::kInner;
-    find();
+    const auto start = [&] {
+        next = first + Xt::major(0);
+        find();
+        none[0] = 0;
 #pragma unroll
-    for (int i = 0; i < Xt::kRounds; ++i) none[0] |= a.from.row_of(entry[i]) < 0 ? 1u << i : 0u;
-    multiply_tiles<Lt, Rt, MI, NJ>(lds, tiles, load, mend, wn, wm, true, acc);
+        for (int i = 0; i < Xt::kRounds; ++i) none[0] |= a.from.row_of(entry[i]) < 0 ? 1u << i : 0u;
+    };
+    bool done = false;
+    if constexpr (sizeof(T) == 4) {
+        start();
+        multiply_tiles_split<Lt, Rt, MI, NJ>(lds, tiles, load, mend, wn, wm, true, acc);
+        done = !start_over(acc);
+    }
+    if (!done) {
+        start();
+        multiply_tiles<Lt, Rt, MI, NJ>(lds, tiles, load, mend, wn, wm, true, acc);
+    }
     T* __restrict__ dW = static_cast<T*>(const_cast<void*>(a.W)) + g * a.N * a.K;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -261,9 +279,8 @@ double turns(int64_t tiles, int compute_units, int BM, int BN, double rate)
 
 // 256 x 256, 128 x 128 or 64 x 128, whichever leaves the least to the unit that has most.  A group has a last tile that
 // is not full: 0.6 of a tile more than its rows in the mean.  16 groups, 16,384 rows, 4,096 x 2,048 bf16: 317 us with
-// 256 x 256, 372 with 128 x 128; 64 groups, 8,192 rows, 1,024 x 2,048: 101 and 86.  Floats, whose products take sixteen
-// times as long, lose nothing with small tiles: 8 groups, 4,096 rows, 1,024 x 1,024: 243 us with 256 x 256, 135 with
-// 128 x 128, 97 with 64 x 128.
+// 256 x 256, 372 with 128 x 128; 64 groups, 8,192 rows, 1,024 x 2,048: 101 and 86.  Floats have the two
+// small ones: the instruction's six products of parts leave no registers for the large.
 template <typename T, bool KN, bool WIDE>
 hipError_t by_size(const GroupedArgs& a, hipStream_t s)
 {
@@ -274,8 +291,10 @@ hipError_t by_size(const GroupedArgs& a, hipStream_t s)
     };
     const double large = turns(tiles(256, 256), a.compute_units, 256, 256, 1.0);
     const double middle = turns(tiles(128, 128), a.compute_units, 128, 128, kHalf ? 0.7 : 1.0);
-    const double small = turns(tiles(64, 128), a.compute_units, 64, 128, kHalf ? 0.55 : 0.95);
-    if (kHalf && large <= std::min(middle, small)) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    const double small = turns(tiles(64, 128), a.compute_units, 64, 128, kHalf ? 0.55 : 0.8);
+    if constexpr (kHalf) {
+        if (large <= std::min(middle, small)) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    }
     if (middle <= small) return run_fast<T, 128, 128, KN, WIDE, 256>(a, s);
     return run_fast<T, 64, 128, KN, WIDE, 256>(a, s);
 }
@@ -283,7 +302,9 @@ hipError_t by_size(const GroupedArgs& a, hipStream_t s)
 template <typename T, bool KN, bool WIDE>
 hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
 {
-    if (sizeof(T) == 2 && a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 192) return run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    if constexpr (sizeof(T) == 2) {
+        if (a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 192) return run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+    }
     return run_wgrad_fast<T, 128, 128, KN, WIDE, 256>(a, s);
 }
 

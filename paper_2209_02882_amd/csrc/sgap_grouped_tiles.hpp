@@ -210,6 +210,119 @@ __device__ __forceinline__ void multiply_tiles(char* shared, int tiles, F&& load
     else multiply_tiles_as<L, R, MI, NJ, false>(lds, tiles, load, mend, l0, r0, acc);
 }
 
+// Eight floats as three times eight 16-bit ones, x = high + middle + low: eight bits of x's 24 each, rounded to nearest, so
+// that the middle one is at most 2^-9 of x and the low one 2^-17.
+struct Split {
+    piece_t<bf16_t> high, middle, low;
+};
+// Two floats rounded to 16 bits, and in `rest` what that leaves of them (exact): an instruction for both, and four.
+__device__ __forceinline__ uint32_t round_two(float x, float y, float (&rest)[2])
+{
+    typedef float float2_t __attribute__((ext_vector_type(2)));
+    typedef bf16_t bf2_t __attribute__((ext_vector_type(2)));
+    const uint32_t both = __builtin_bit_cast(uint32_t, __builtin_convertvector(float2_t{x, y}, bf2_t));
+    rest[0] = x - __uint_as_float(both << 16);
+    rest[1] = y - __uint_as_float(both & 0xffff0000u);
+    return both;
+}
+__device__ __forceinline__ Split split(piece_t<float> x, piece_t<float> y)
+{
+    uint32_t high[4], middle[4], low[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float r[2], q[2], none[2];
+        high[i] = round_two(i < 2 ? x[2 * i] : y[2 * i - 4], i < 2 ? x[2 * i + 1] : y[2 * i - 3], r);
+        middle[i] = round_two(r[0], r[1], q);
+        low[i] = round_two(q[0], q[1], none);
+    }
+    Split s;
+    __builtin_memcpy(&s.high, high, 16);
+    __builtin_memcpy(&s.middle, middle, 16);
+    __builtin_memcpy(&s.low, low, 16);
+    return s;
+}
+
+// Products of floats on the 16-bit matrix instruction, which makes sixteen times as many in the same time as the one for
+// floats: of the nine products of the parts the six that count, and what is left out (middle x low and low x low) is
+// under 2^-25 of a product, less than the rounding of a float.  The two half tiles are the instruction's 32 inner values.
+// Where a value is infinite, no number or rounds up to infinity, every result that it has a part in comes out not finite,
+// and the caller computes the tile again with the instruction for floats.
+template <typename L, typename R, int MI, int NJ, typename F, typename M>
+__device__ __forceinline__ void multiply_tiles_split(char* shared, int tiles, F&& load, M&& mend, int l0, int r0, bool active,
+                                                     f32x4 (&acc)[MI][NJ])
+{
+    constexpr uint32_t kStage = L::kBytes + R::kBytes;
+    constexpr int kLoads = L::kRounds + R::kRounds;
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)shared;
+    const uint32_t lbase = lds + L::lane_base(l0), rbase = lds + L::kBytes + R::lane_base(r0);
+    if (tiles == 0) return;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(0, lds, i);
+    for (int t = 0; t < tiles; ++t) {
+        const uint32_t stage = (t & 1) * kStage;
+        wait_loads();
+        mend(t, lds + stage);
+        __syncthreads();
+        if (t + 1 < tiles) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load(t + 1, lds + kStage - stage, i);
+        }
+        if (!active) continue;
+        uint32_t lb = lbase + stage, rb = rbase + stage;
+        asm volatile("" : "+v"(lb), "+v"(rb));
+        // Taking a value apart is five and a half vector instructions, an eighth of what its products cost the matrix unit;
+        // they are dealt out between the products of the columns before.
+        Split l[MI], r = split(R::fragment(rb, 0, 0), R::fragment(rb, 0, 1));
+#pragma unroll
+        for (int i = 0; i < MI; ++i) l[i] = split(L::fragment(lb, i, 0), L::fragment(lb, i, 1));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const Split now = r;
+            if (j + 1 < NJ) r = split(R::fragment(rb, j + 1, 0), R::fragment(rb, j + 1, 1));
+            // the smallest first
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(l[i].low, now.high, acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(l[i].high, now.low, acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(l[i].middle, now.middle, acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(l[i].middle, now.high, acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(l[i].high, now.middle, acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) acc[i][j] = mma16(l[i].high, now.high, acc[i][j]);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // the reads
+#pragma unroll
+            for (int i = 0; i < 6 * MI; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);  // two vector ones
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+// Whether some wavefront of the workgroup has a sum that is not finite; clears the sums if so.
+template <int MI, int NJ>
+__device__ __forceinline__ bool start_over(f32x4 (&acc)[MI][NJ])
+{
+    bool finite = true;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(acc[i][j][r]);
+    if (!__syncthreads_or(!finite)) return false;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    return true;
+}
+
 // The same where the loads cannot go past the registers (rows at addresses that are no multiples of 16 bytes): a tile's
 // pieces wait in registers from the middle of one tile to the middle of the next and are then put into LDS.
 //   fetch(t, i)    piece i of LOADS of tile t as it lies in memory; called for one tile after the other
