@@ -1,0 +1,187 @@
+"""A mixture-of-experts layer out of the library's calls, as one would train it and serve it.
+
+Training: the router gives every token k experts, the tokens' rows are multiplied by their experts' weights without being
+copied into order first, and the experts' rows are summed up by token; the gradients go the same way back.  Serving: the
+same with the experts' weights in 4 bits.
+
+    python -m paper_2209_02882_amd.experts          trains a small layer for a few steps, then serves it both ways
+
+The activation between the two products is torch's; everything that goes by expert is the library's.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding
+
+
+class Route(torch.autograd.Function):
+    """(gates, slot, order, offsets) of logits T x E; only the gates have a gradient."""
+
+    @staticmethod
+    def forward(ctx, logits, k):
+        T, E = logits.shape
+        dev = logits.device
+        gates = torch.empty((T, k), device=dev)
+        experts, slot = (torch.empty((T, k), dtype=torch.int32, device=dev) for _ in range(2))
+        order = torch.empty(T * k, dtype=torch.int32, device=dev)
+        offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        workspace = torch.empty(binding.sgap_route_topk_workspace_size(T, E, k), dtype=torch.uint8, device=dev)
+        binding.sgap_route_topk(T, E, k, logits, gates, experts, slot, order, offsets, workspace=workspace)
+        ctx.save_for_backward(logits, gates, experts)
+        ctx.mark_non_differentiable(slot, order, offsets)
+        return gates, slot, order, offsets
+
+    @staticmethod
+    def backward(ctx, dgates, *_):
+        logits, gates, experts = ctx.saved_tensors
+        T, E = logits.shape
+        dlogits = torch.empty_like(logits)
+        binding.sgap_route_topk_grad(T, E, gates.shape[1], logits, gates, experts, dgates.contiguous(), dlogits)
+        return dlogits, None
+
+
+class GroupedMM(torch.autograd.Function):
+    """Rows of x times their expert's weights (E x N x K).  Where they are `gathered`, x has the tokens' rows, row r is
+    x[order[r] // k], and the gradient of x is the sum over a token's rows; else x lies in order already."""
+
+    @staticmethod
+    def forward(ctx, x, weights, offsets, order, slot, gathered):
+        G, N, K = weights.shape
+        k = slot.shape[1]
+        R = order.numel()
+        y = torch.empty((R, N), dtype=x.dtype, device=x.device)
+        gather = {"src": order, "src_div": k} if gathered else {}
+        binding.sgap_grouped_mm(G, R, K, N, offsets, x, weights, y, "nk", **gather)
+        ctx.save_for_backward(x, weights, offsets, order, slot)
+        ctx.gather = gather
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weights, offsets, order, slot = ctx.saved_tensors
+        G, N, K = weights.shape
+        R, dy = order.numel(), dy.contiguous()
+        dx = torch.empty((R, K), dtype=x.dtype, device=x.device)
+        binding.sgap_grouped_mm(G, R, N, K, offsets, dy, weights, dx, "kn")
+        if ctx.gather:
+            rows, dx = dx, torch.empty_like(x)
+            binding.sgap_route_combine(slot.shape[0], slot.shape[1], K, rows, slot, None, dx)
+        dw = torch.empty_like(weights)
+        binding.sgap_grouped_mm_wgrad(G, R, K, N, offsets, x, dy, dw, "nk", **ctx.gather)
+        return dx, dw, None, None, None, None
+
+
+class Combine(torch.autograd.Function):
+    """The experts' rows summed up by token, each times its gate."""
+
+    @staticmethod
+    def forward(ctx, rows, gates, slot, order):
+        T, k = slot.shape
+        out = torch.empty((T, rows.shape[1]), dtype=rows.dtype, device=rows.device)
+        binding.sgap_route_combine(T, k, rows.shape[1], rows, slot, gates, out)
+        ctx.save_for_backward(rows, gates, slot, order)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        rows, gates, slot, order = ctx.saved_tensors
+        T, k = slot.shape
+        drows, dgates = torch.empty_like(rows), torch.empty_like(gates)
+        binding.sgap_route_combine_grad(T, k, rows.shape[1], rows, slot, order, gates, dout.contiguous(), drows, dgates)
+        return drows, dgates, None, None
+
+
+def gated(h):
+    """silu of the first half of the columns times the second."""
+    a, b = h.chunk(2, dim=1)
+    return torch.nn.functional.silu(a) * b
+
+
+def quantise(weights, group_k):
+    """(codes, scales, zeros) in 4 bits of weights E x N x K: group_k neighbours along K share a scale and a zero point."""
+    E, N, K = weights.shape
+    w = weights.float().view(E, N, K // group_k, group_k)
+    low, high = w.amin(3).clamp(max=0), w.amax(3).clamp(min=0)
+    scales = ((high - low) / 15).clamp(min=1e-8).to(weights.dtype)
+    zeros = (-low / scales.float()).round().clamp(0, 15)
+    codes = (w / scales.float()[..., None] + zeros[..., None]).round().clamp(0, 15).view(E, N, K).to(torch.uint8)
+    return codes[..., 0::2] | (codes[..., 1::2] << 4), scales, zeros.to(torch.uint8)
+
+
+class Weights4:
+    """Weights E x N x K in 4 bits, laid out once for sgap_grouped_mm_w4."""
+
+    def __init__(self, weights, group_k=64):
+        self.shape, self.group_k = weights.shape, group_k
+        E, N, K = weights.shape
+        codes, scales, zeros = quantise(weights, group_k)
+        size = binding.sgap_w4_layout_size(E, K, N, group_k, zeros=True)
+        self.data = torch.empty(size, dtype=torch.uint8, device=weights.device)
+        binding.sgap_w4_layout(E, K, N, group_k, codes.contiguous(), scales, zeros, self.data)
+
+    def rows(self, x, offsets, R, **gather):
+        E, N, K = self.shape
+        y = torch.empty((R, N), dtype=x.dtype, device=x.device)
+        binding.sgap_grouped_mm_w4(E, R, K, N, self.group_k, offsets, x, self.data, y, zeros=True, **gather)
+        return y
+
+
+class ExpertLayer(torch.nn.Module):
+    """x (T x width) -> sum over each token's k experts of gate * down(gated(up(x)))."""
+
+    def __init__(self, width, hidden, experts, k, dtype=torch.bfloat16, device="cuda"):
+        super().__init__()
+        self.k = k
+        new = lambda *shape: torch.nn.Parameter((torch.randn(shape, device=device) * shape[-1] ** -0.5).to(dtype))  # noqa: E731
+        self.router, self.up, self.down = new(experts, width), new(experts, 2 * hidden, width), new(experts, width, hidden)
+        self.served = None
+
+    def forward(self, x):
+        gates, slot, order, offsets = Route.apply((x @ self.router.t()).float(), self.k)
+        h = gated(GroupedMM.apply(x, self.up, offsets, order, slot, True))
+        return Combine.apply(GroupedMM.apply(h, self.down, offsets, order, slot, False), gates, slot, order)
+
+    @torch.no_grad()
+    def quantise(self, group_k=64):
+        """From now on serve() has the experts in 4 bits."""
+        self.served = Weights4(self.up, group_k), Weights4(self.down, group_k)
+
+    @torch.no_grad()
+    def serve(self, x):
+        if self.served is None:
+            return self(x)
+        up, down = self.served
+        gates, slot, order, offsets = Route.apply((x @ self.router.t()).float(), self.k)
+        R = order.numel()
+        h = gated(up.rows(x, offsets, R, src=order, src_div=self.k))
+        out = torch.empty_like(x)
+        binding.sgap_route_combine(x.shape[0], self.k, x.shape[1], down.rows(h, offsets, R), slot, gates, out)
+        return out
+
+
+def main(steps=30, tokens=512, width=256, hidden=128, experts=8, k=2):
+    torch.manual_seed(0)
+    layer = ExpertLayer(width, hidden, experts, k)
+    wanted = torch.randn(width, width, device="cuda") * width ** -0.5
+    optimiser = torch.optim.Adam(layer.parameters(), lr=5e-3)
+    x = torch.randn(tokens, width, device="cuda").bfloat16()
+    losses = []
+    for step in range(steps):
+        loss = (layer(x).float() - x.float() @ wanted).square().mean()
+        optimiser.zero_grad()
+        loss.backward()
+        optimiser.step()
+        losses.append(loss.item())
+        if step % 10 == 0 or step == steps - 1:
+            print(f"step {step:3d}: loss {losses[-1]:.4f}", flush=True)
+    x = torch.randn(4, width, device="cuda").bfloat16()
+    full = layer.serve(x).float()
+    layer.quantise()
+    off = (layer.serve(x).float() - full).norm() / full.norm()
+    print(f"4 tokens served with the experts in 4 bits: {100 * off.item():.1f}% off the 16-bit ones")
+    return losses, off.item()
+
+
+if __name__ == "__main__":
+    main()
