@@ -366,17 +366,21 @@ hipError_t by_rows(const GroupedW4Args& a, const W4Sizes& z, hipStream_t s)
     };
     // Wavefronts that share the inner dimension: eight where the workgroups alone would not fill the chip, two where they
     // do several times over, so that a wavefront's start is spread over more blocks.  8 groups of 32 rows by 4,096 x 4,096
-    // (2,048 workgroups): 8 60 us, 4 41.6, 2 35.6; 64 experts for 64 rows (5,632): 4 21.5, 2 20.7; one row by 8,192 x 8,192
-    // (512): 16 14.7, 8 12.6, 4 14.3; 128 rows by 8,192 x 8,192 (768): 8 55, 4 45, 2 48.
+    // (2,048 workgroups): 8 60 us, 4 41.6, 2 35.6; one row by 8,192 x 8,192 (512): 16 14.7, 8 12.6, 4 14.3; 128 rows by
+    // 8,192 x 8,192 (768): 8 55, 4 45, 2 48; 8 experts of 64 (704 that have rows): 4 12.1, 2 15.3.
+    const int64_t used = a.G < a.R ? a.G : a.R;  // groups that may have rows
     const auto waves = [&](int columns, int rows) {
-        const int64_t groups = a.G * ((z.tiles_n * kTileN + columns - 1) / columns) * items(rows);
+        const int64_t groups = used * ((z.tiles_n * kTileN + columns - 1) / columns) * items(rows);
         int w = groups <= 512 ? 8 : groups <= 1024 ? 4 : 2;
         while (w > 1 && w / 2 >= z.blocks_k) w /= 2;
         return w;
     };
     const bool staged = a.ldx % 8 == 0 && (reinterpret_cast<uintptr_t>(a.X) & 15) == 0;
-    // (one row or two: sixteen lanes of a load share a row, and the way through LDS would only be longer)
-    if (most <= 16) return run_w4<T, STEPS, 1, 1>(a, z, waves(16, 16), items(16), staged && most > 2, s);
+    // One row or two: sixteen lanes of a load share a row, and the way through LDS would only be longer.  Two tiles of
+    // columns to a wavefront where that leaves workgroups enough: 64 experts for 64 rows 24.0 us with one, 20.5 with two;
+    // 8 groups of 2 rows by 4,096 x 4,096 21.8 and 17.5; 4,096 columns for one row: 4.7 with one.
+    if (most <= 16 && used * z.tiles_n < 512) return run_w4<T, STEPS, 1, 1>(a, z, waves(16, 16), items(16), staged && most > 2, s);
+    if (most <= 16) return run_w4<T, STEPS, 2, 1>(a, z, waves(32, 16), items(16), staged && most > 2, s);
     if (most <= 32 && staged) return run_w4<T, STEPS, 2, 2>(a, z, waves(32, 32), items(32), staged, s);
     return run_w4<T, STEPS, 2, 3>(a, z, waves(32, 48), items(48), staged, s);
 }
