@@ -1,0 +1,119 @@
+"""Sizes that make the products over groups take each of their tiles, and floats at the ends of their range."""
+import numpy as np
+import pytest
+import torch
+
+from experts_util import E, assert_within, grouped_mm, offsets_of, random
+from paper_2209_02882_amd import binding
+from test_gpu_experts_products import check, check_w4, laid_out, result, w4_inputs
+
+pytestmark = pytest.mark.gpu
+
+HALVES = [torch.float16, torch.bfloat16]
+
+
+# enough rows and columns for 256 x 256 (16-bit types) and 128 x 128 (floats); the rows' gradient has 72 or 200 columns
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("K", [72, 200])
+def test_many_rows_of_many_columns(K, dtype, layout):
+    check([2000, 3111, 0, 1, 2500, 700], K, 4096, dtype, layout, extra=5)
+
+
+# few rows of many weights: the gradient of the weights by 256 x 256
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+def test_many_weights(dtype, layout):
+    check([65, 3, 0, 130, 64, 1, 7, 200, 0, 31, 33, 2], 1048, 1032, dtype, layout, k=2, extra=1)
+
+
+# groups of half a large tile: 128 x 128 for 16-bit types
+@pytest.mark.parametrize("dtype", HALVES)
+def test_many_groups_of_128_rows(dtype):
+    sizes = np.random.default_rng(5).integers(60, 196, 64).tolist()
+    check(sizes, 64, 2048, dtype, "nk", k=1)
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("rows", [1, 2, 5, 17])
+def test_w4_two_tiles_of_columns_to_a_wavefront(rows, dtype):
+    sizes = [rows if g % 3 else 0 for g in range(64)]
+    check_w4(sizes, 256, 205, 64, dtype, True, k=1)
+    check_w4([rows], 128, 8200, 32, dtype, False, given=False)
+    check_w4(sizes, 192, 205, 64, dtype, False, pad=1)
+
+
+def run_f32(X, W, layout):
+    R, K = X.shape
+    N = W.shape[1] if layout == "nk" else W.shape[2]
+    Y = result(R, N, torch.float32)
+    binding.sgap_grouped_mm(1, R, K, N, None, X.cuda(), W.cuda(), Y, layout)
+    return Y
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+def test_floats_that_round_up_to_infinity_in_16_bits(layout):
+    K, N, R = 64, 96, 140
+    X, W = random(1, R, K), random(2, 1, *((N, K) if layout == "nk" else (K, N)), scale=2.0**-9)
+    X[3, 5], X[70, 63] = 3.4e38, -3.4028234e38
+    want, size = grouped_mm(offsets_of([R]), X, W, layout, R)
+    assert_within(run_f32(X, W, layout), want, size * (K + 4) * E)
+    # and the same value among the weights
+    X, W = random(3, R, K, scale=2.0**-9), random(4, 1, *((N, K) if layout == "nk" else (K, N)))
+    W[0, 7, 9] = 3.4e38
+    want, size = grouped_mm(offsets_of([R]), X, W, layout, R)
+    assert_within(run_f32(X, W, layout), want, size * (K + 4) * E)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-20, 1e15])
+def test_floats_far_from_one(scale):
+    X, W = random(5, 130, 72, scale=scale), random(6, 1, 80, 72)
+    want, size = grouped_mm(offsets_of([130]), X, W, "nk", 130)
+    assert_within(run_f32(X, W, "nk"), want, size * 76 * E)
+
+
+def test_floats_under_the_range_of_16_bit_parts():
+    # below 2^-110 the last of the three parts is cut off at the smallest 16-bit number, 2^-133
+    X, W = random(7, 130, 72, scale=2.0**-112), random(8, 1, 80, 72)
+    want, size = grouped_mm(offsets_of([130]), X, W, "nk", 130)
+    cut = 2.0**-133 * W.double().abs().sum(2)
+    assert_within(run_f32(X, W, "nk"), want, size * 76 * E + cut)
+
+
+def test_integers_of_24_bits_are_exact():
+    # one product to a sum: nothing is left out of a value
+    gen = torch.Generator().manual_seed(9)
+    X = torch.zeros(128, 64)
+    X[torch.arange(128), torch.arange(128) % 64] = torch.randint(-2**24, 2**24, (128,), generator=gen).float()
+    W = torch.ones(1, 64, 64)
+    assert torch.equal(run_f32(X, W, "nk").cpu(), X.sum(1, keepdim=True).expand(128, 64))
+
+
+def test_the_same_bits_on_every_call():
+    sizes, K, N = [300, 0, 41, 700], 264, 520
+    offsets, R = offsets_of(sizes).cuda(), 1041
+    for dtype in (torch.float32, *HALVES):
+        X, W, dY = random(1, R, K, dtype=dtype).cuda(), random(2, 4, N, K, dtype=dtype).cuda(), random(3, R, N, dtype=dtype).cuda()
+        seen = None
+        for _ in range(3):
+            Y, dW = torch.empty_like(dY), torch.empty_like(W)
+            binding.sgap_grouped_mm(4, R, K, N, offsets, X, W, Y, "nk")
+            binding.sgap_grouped_mm_wgrad(4, R, K, N, offsets, X, dY, dW, "nk")
+            if seen is not None:
+                assert torch.equal(seen[0], Y) and torch.equal(seen[1], dW)
+            seen = Y, dW
+
+
+@pytest.mark.parametrize("rows", [3, 30])
+def test_w4_sums_that_are_infinite_by_definition(rows):
+    K, N, group_k = 128, 16, 128
+    codes, scales, _ = w4_inputs(1, K, N, group_k, torch.bfloat16, False)
+    scales[:] = 1.0
+    X = torch.zeros(rows, K, dtype=torch.bfloat16)
+    X[1] = 3.0e38
+    Y = result(rows, N, torch.bfloat16)
+    binding.sgap_grouped_mm_w4(1, rows, K, N, group_k, None, X.cuda(), laid_out(1, K, N, group_k, codes, scales, None), Y)
+    got = Y.float().cpu()
+    assert (got[[r for r in range(rows) if r != 1]] == 0).all()
+    # in the order of the inner dimension the running sum passes the largest float, and stays there or is no number
+    assert not torch.isfinite(got[1]).any()
