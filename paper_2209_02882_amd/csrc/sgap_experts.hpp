@@ -161,6 +161,9 @@ hipError_t launch_combine_grad(const CombineArgs& a, hipStream_t s);
 bool grouped_fast_applies(const GroupedArgs& a, int dtype);
 hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s);
+// of those, few rows a group by weights N x K (sgap_grouped_few.hip)
+bool grouped_few_applies(const GroupedArgs& a, int dtype);
+hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
 struct W4Sizes {

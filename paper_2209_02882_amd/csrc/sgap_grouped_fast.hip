@@ -22,7 +22,7 @@ constexpr int kRun = 32, kGradientRun = 16;
 
 // WIDE: rows of X lie further than 32 bits of bytes from its first.
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
-__global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, int64_t column_tiles, int64_t items)
+__global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, int64_t column_tiles, int64_t items, bool apart)
 {
     using Wt = Tile<T, BN, !KN, THREADS>;
     using Xt = Tile<T, BM, true, THREADS>;
@@ -63,10 +63,14 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
             else xo[i] = (uint32_t)r;
         }
         const int tiles = (int)((a.K + Wt::kInner - 1) / Wt::kInner);
+        // APART: where the weights pass once, workgroups begin at different tiles of the inner dimension.  Rows of weights a
+        // power of two apart lie in the same memory channels, and all workgroups would ask for the same ones at a time.
+        const int begin = apart ? __builtin_amdgcn_readfirstlane((int)(item % tiles)) : 0;
+        const auto start_of = [&](int t) { return (int64_t)(t + begin < tiles ? t + begin : t + begin - tiles) * Wt::kInner; };
         // inner values that tile t has
-        const auto left = [&](int t) { return (int)min((int64_t)Wt::kInner, a.K - (int64_t)t * Wt::kInner); };
+        const auto left = [&](int t) { return (int)min((int64_t)Wt::kInner, a.K - start_of(t)); };
         const auto load = [&](int t, uint32_t to, int i) {
-            const int64_t k0 = (int64_t)t * Wt::kInner;
+            const int64_t k0 = start_of(t);
             if (i < Wt::kRounds) {
                 const char* const w = uniform(W + (KN ? k0 * a.N : k0) * (int64_t)sizeof(T));
                 const bool there = (KN ? Wt::major(i) : Wt::minor(i) * Wt::P) < left(t);
@@ -252,9 +256,12 @@ hipError_t run_fast(const GroupedArgs& a, hipStream_t s)
     const int64_t columns = (a.N + BN - 1) / BN, items = columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr);
     if (items > 0x7fffff00LL) return hipErrorInvalidConfiguration;
     constexpr int kLds = 2 * 128 * (BM + BN);
+    // (a row of 4,096 bytes or a multiple: 16 experts for 32 rows, 2,048 x 4,096 bf16, 56.7 us together and 47.7 apart; rows
+    // of 2,000 bytes 29.2 and 32.5)
+    const bool apart = !KN && a.R <= BM * a.G && a.K * (int64_t)sizeof(T) % 4096 == 0;
     static uint64_t allowed = 0;
     if (const hipError_t err = allow_lds(grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS>, kLds, allowed)) return err;
-    grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, columns, items);
+    grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, columns, items, apart);
     return hipGetLastError();
 }
 

@@ -277,6 +277,7 @@ hipError_t wgrad(const GroupedArgs& a, hipStream_t s)
 
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s)
 {
+    if (grouped_few_applies(a, dtype)) return launch_grouped_few(a, dtype, s);
     if (grouped_fast_applies(a, dtype)) return launch_grouped_fast(a, dtype, s);
     switch (dtype) {
         case 0: return by_rows<float>(a, s);

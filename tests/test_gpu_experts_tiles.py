@@ -117,3 +117,23 @@ def test_w4_sums_that_are_infinite_by_definition(rows):
     assert (got[[r for r in range(rows) if r != 1]] == 0).all()
     # in the order of the inner dimension the running sum passes the largest float, and stays there or is no number
     assert not torch.isfinite(got[1]).any()
+
+
+# few rows of few columns: the inner dimension shared by wavefronts, with blocks that are not whole
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("K", [8, 16, 24, 32, 120, 128, 136, 1024, 2056])
+def test_few_rows_by_aligned_weights(K, dtype):
+    for rows in (1, 2, 15, 16):
+        check([rows], K, 88, dtype, "nk", given=False)
+    check([3, 0, 1, 12, 8, 0, 0], K, 40, dtype, "nk", k=2, extra=3, pad=8)
+    check([0, 2, 0], K, 2056, dtype, "nk", extra=1)
+
+
+def test_few_rows_that_are_not_finite_stay_by_themselves():
+    for K in (64, 72):
+        X, W = torch.ones(6, K, dtype=torch.bfloat16), torch.ones(1, 24, K, dtype=torch.bfloat16)
+        X[1, K - 1], X[4, 0] = float("inf"), float("nan")
+        Y = result(6, 24, torch.bfloat16)
+        binding.sgap_grouped_mm(1, 6, K, 24, None, X.cuda(), W.cuda(), Y, "nk")
+        got = Y.float().cpu()
+        assert (got[1] == float("inf")).all() and torch.isnan(got[4]).all() and (got[[0, 2, 3, 5]] == K).all()
