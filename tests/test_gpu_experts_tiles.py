@@ -137,3 +137,12 @@ def test_few_rows_that_are_not_finite_stay_by_themselves():
         binding.sgap_grouped_mm(1, 6, K, 24, None, X.cuda(), W.cuda(), Y, "nk")
         got = Y.float().cpu()
         assert (got[1] == float("inf")).all() and torch.isnan(got[4]).all() and (got[[0, 2, 3, 5]] == K).all()
+
+
+# more rows, but too few tiles for the chip: two times sixteen rows to a wavefront
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("K,N", [(264, 104), (1024, 520)])
+def test_few_tiles_by_aligned_weights(K, N, dtype):
+    for rows in (17, 32, 33, 200):
+        check([rows], K, N, dtype, "nk", given=False)
+    check([40, 0, 33, 1], K, N, dtype, "nk", k=2, extra=40, pad=8)
