@@ -790,6 +790,8 @@ int sgap_route_combine_grad(int64_t T, int64_t k, int64_t D, int dtype, const vo
  * layout's name: K and N change places, and W stays where it is.  K = 0 gives
  * zeros.  Any sizes, strides and element-aligned addresses; multiples of 16
  * bytes are faster.  Y must not overlap X or W.
+ * Floats are multiplied as sums of three bfloat16 numbers, which hold a
+ * float's 24 bits down to 2^-133: a value below 2^-110 counts to within 2^-134.
  */
 typedef enum { SGAP_WEIGHTS_NK = 0, SGAP_WEIGHTS_KN = 1 } sgap_weight_layout;
 int sgap_grouped_mm(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, const int32_t* offsets, const void* X, int64_t ldx,
@@ -804,8 +806,7 @@ int sgap_grouped_mm_wgrad(int64_t G, int64_t R, int64_t K, int64_t N, int dtype,
 /*
  * The same product with weights of 4 bits,
  *   W[g][n, k] = (code[g][n, k] - zero[g][n, k / group_k]) * scale[g][n, k / group_k],
- * for few rows a group: the weights pass once for every 16 (few rows) or 48
- * rows.  No weight is rounded on the way.  sgap_w4_layout puts codes, scales
+ * for few rows a group: the weights pass once for every 16, 32 or 48 rows.  No weight is rounded on the way.  sgap_w4_layout puts codes, scales
  * and zero points into the order in which the product reads them; a program
  * does that once, when it loads its weights, and may free them afterwards.
  *   codes    G x N x K/2 bytes, the code of an even k in the low half

