@@ -161,9 +161,11 @@ hipError_t launch_combine_grad(const CombineArgs& a, hipStream_t s);
 bool grouped_fast_applies(const GroupedArgs& a, int dtype);
 hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s);
-// of those, too few rows or columns for tiles to fill the chip (sgap_grouped_few.hip)
+// of those, too few rows, columns or weights for tiles to fill the chip (sgap_grouped_few.hip)
 bool grouped_few_applies(const GroupedArgs& a, int dtype);
 hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s);
+bool grouped_few_wgrad_applies(const GroupedArgs& a, int dtype);
+hipError_t launch_grouped_few_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
 struct W4Sizes {

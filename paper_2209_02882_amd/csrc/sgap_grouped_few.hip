@@ -252,6 +252,107 @@ __global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int6
     }
 }
 
+// The gradient of few weights from many rows, where tiles of 128 x 128 are too few for the chip: a workgroup has 16 V x 16 V
+// weights, and its wavefronts share the group's rows.  Both operands come as W above does, V columns of P rows to a lane.
+// KN: the gradient's rows are X's columns, otherwise dY's.
+template <typename T, int V, bool KN>
+__global__ __launch_bounds__(512) void grouped_few_wgrad_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n)
+{
+    typedef T row_t __attribute__((ext_vector_type(V)));
+    constexpr int P = Piece<T>::kCount, kStep = 4 * P, S = 4 / V, kBlock = S * kStep, kSide = 16 * V;
+    __shared__ f32x4 part[8][V][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6, place = lane & 15, piece = lane >> 4;
+    const int64_t M = KN ? a.K : a.N, N = KN ? a.N : a.K;
+    const int64_t g = blockIdx.x / (tiles_m * tiles_n), tile = blockIdx.x - g * tiles_m * tiles_n;
+    const int64_t m0 = tile / tiles_n * kSide, n0 = (tile - tile / tiles_n * tiles_n) * kSide;
+    const GroupRows gr = group_rows(a.offsets, g, a.R);
+    const int64_t blocks = (gr.end - gr.first + kBlock - 1) / kBlock;
+    // columns past the last are read from the last, and not stored
+    const int64_t mc = min(m0 + place * V, M - V), nc = min(n0 + place * V, N - V);
+    const T* __restrict__ X = static_cast<const T*>(a.X) + (KN ? mc : nc);
+    const T* __restrict__ dY = static_cast<const T*>(a.Y) + (KN ? nc : mc);
+    struct Block {
+        row_t x[S][P], y[S][P];
+        uint32_t none[S], past;  // rows of X that do not exist, and rows behind the group's last
+    };
+    // what the list says for the rows of the block that is fetched next, one to a lane: asked for a block ahead
+    static_assert(kBlock <= 64, "a lane for every row");
+    int32_t entry = 0;
+    const auto ask = [&](int64_t kb) { entry = a.from.src[min(gr.first + kb * kBlock + lane % kBlock, gr.end - 1)]; };
+    if (a.from.src && wave < blocks) ask(wave);
+    const auto fetch = [&](int64_t kb, Block& b) {
+        const int64_t r0 = gr.first + kb * kBlock + piece * P;
+        int32_t row = 0;
+        if (a.from.src) {
+            row = a.from.row_of(entry);
+            if (kb + waves < blocks) ask(kb + waves);
+        }
+        b.past = 0;
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            b.none[i] = 0;
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const int64_t r = r0 + i * kStep + j, real = min(r, gr.end - 1);
+                if (r > real) b.past |= 1u << (i * P + j);
+                int64_t from = real;
+                if (a.from.src) from = __shfl(row, i * kStep + piece * P + j);
+                if (from < 0 || from >= a.from.rows) b.none[i] |= 1u << j, from = 0;
+                b.y[i][j] = *reinterpret_cast<const row_t*>(dY + real * a.ldy);
+                b.x[i][j] = *reinterpret_cast<const row_t*>(X + from * a.ldx);
+            }
+        }
+    };
+    f32x4 acc[V][V];
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+#pragma unroll
+        for (int f = 0; f < V; ++f) acc[e][f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const auto multiply = [&](int64_t, Block& b) {
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            if (b.none[i] | b.past) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const bool past = b.past >> (i * P + j) & 1;
+                    if (past) b.y[i][j] = row_t{};
+                    if (past || (b.none[i] >> j & 1)) b.x[i][j] = row_t{};
+                }
+            }
+            piece_t<T> x[V], y[V];
+            const auto turn = [&](auto e) {
+                x[e] = column_of<e, T, V>(b.x[i]);
+                y[e] = column_of<e, T, V>(b.y[i]);
+            };
+            [&]<int... e>(std::integer_sequence<int, e...>) {
+                (turn(std::integral_constant<int, e>()), ...);
+            }(std::make_integer_sequence<int, V>());
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+#pragma unroll
+                for (int f = 0; f < V; ++f) acc[e][f] = KN ? mma16(x[e], y[f], acc[e][f]) : mma16(y[e], x[f], acc[e][f]);
+        }
+    };
+    share_blocks<Block>(wave, waves, blocks, fetch, multiply);
+    T* __restrict__ W = static_cast<T*>(const_cast<void*>(a.W)) + g * a.K * a.N;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        __syncthreads();
+#pragma unroll
+        for (int f = 0; f < V; ++f) part[wave][f][lane] = acc[e][f];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * kSide; i += blockDim.x) {
+            // element i: row V * (i / kSide) + e of the tile (rows 4 l + r lie with lane part l), column i % kSide
+            const int m = i / kSide, n = i % kSide, from = (m >> 2) * 16 + n / V;
+            float v = 0.0f;
+            for (int s = 0; s < waves; ++s) v += reinterpret_cast<const float*>(&part[s][n % V][from])[m & 3];
+            const int64_t to = m0 + m * V + e, column = n0 + n;
+            if (to < M && column < N) W[to * N + column] = (T)v;
+        }
+    }
+}
+
 // workgroups that share a group's rows, `rows` each
 unsigned down(const GroupedArgs& a, int rows)
 {
@@ -298,6 +399,26 @@ hipError_t by_columns(const GroupedArgs& a, hipStream_t s)
     return few<T, 2, 1>(a, waves, s);
 }
 
+template <typename T, int V, bool KN>
+hipError_t few_wgrad(const GroupedArgs& a, hipStream_t s)
+{
+    constexpr int kSide = 16 * V;
+    const int64_t tm = ((KN ? a.K : a.N) + kSide - 1) / kSide, tn = ((KN ? a.N : a.K) + kSide - 1) / kSide;
+    if (a.G * tm * tn > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    grouped_few_wgrad_kernel<T, V, KN><<<(unsigned)(a.G * tm * tn), 512, 0, s>>>(a, tm, tn);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
+{
+    // 32 x 32 weights to a workgroup while there is no more than one to a compute unit, then 64 x 64: 8,192 rows, bf16, by
+    // 512 x 512 (256 of the small) 40 us and 48, 1,024 x 1,024 153 and 52; floats 74 and 163, 286 and 177
+    const int64_t workgroups = a.G * ((a.N + 31) / 32) * ((a.K + 31) / 32);
+    if (workgroups <= a.compute_units) return a.weights_kn ? few_wgrad<T, 2, true>(a, s) : few_wgrad<T, 2, false>(a, s);
+    return a.weights_kn ? few_wgrad<T, 4, true>(a, s) : few_wgrad<T, 4, false>(a, s);
+}
+
 }  // namespace
 
 // Where tiles of 64 x 128 are too few for the chip.  Up to sixteen rows a group: up to 256 of them; floats, whose tiles take
@@ -327,6 +448,28 @@ hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s)
         case 0: return by_columns<float>(a, s);
         case 1: return by_columns<half_t>(a, s);
         default: return by_columns<bf16_t>(a, s);
+    }
+}
+
+// Tiles of 128 x 128 and here, us, in brackets how many tiles:
+//   bf16    8,192 rows by 256 x 256 (4) 143, 37; 1,024 x 1,024 (64) 146, 52; 512 rows by the same 14.2, 8.9, 128 rows 8.0, 7.4;
+//           16 groups of 64 rows, 256 x 256 (64) 7.4, 7.3; 8,192 rows by 2,048 x 1,024 (128) 146, 97; 8 groups of 1,024, 512 x 512
+//           (128) 23.1, 24.0; 1,024 rows by 2,048 x 2,048 (256) 25, 42
+//   floats  8,192 rows by 256 x 256 512, 67; 1,024 x 1,024 520, 177; 2,048 x 1,024 519, 322; 8 groups of 1,024, 512 x 512 71, 56, of
+//           128 15.1, 16.8; 1,024 rows by 2,048 x 2,048 73, 98
+bool grouped_few_wgrad_applies(const GroupedArgs& a, int dtype)
+{
+    if (!grouped_fast_applies(a, dtype)) return false;
+    const int64_t tiles = a.G * ((a.N + 127) / 128) * ((a.K + 127) / 128);
+    return tiles <= 64 || (tiles <= 128 && a.R / a.G >= (dtype == 0 ? 1024 : 2048));
+}
+
+hipError_t launch_grouped_few_wgrad(const GroupedArgs& a, int dtype, hipStream_t s)
+{
+    switch (dtype) {
+        case 0: return wgrad_by_size<float>(a, s);
+        case 1: return wgrad_by_size<half_t>(a, s);
+        default: return wgrad_by_size<bf16_t>(a, s);
     }
 }
 

@@ -290,6 +290,7 @@ hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s)
 
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s)
 {
+    if (grouped_few_wgrad_applies(a, dtype)) return launch_grouped_few_wgrad(a, dtype, s);
     if (grouped_fast_applies(a, dtype)) return launch_grouped_wgrad_fast(a, dtype, s);
     switch (dtype) {
         case 0: return wgrad<float>(a, s);

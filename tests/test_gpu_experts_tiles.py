@@ -179,3 +179,12 @@ def test_few_tiles_but_more_workgroups_than_compute_units(K, dtype, layout):
     check([600], K, 520, dtype, layout, given=False)
     check([2, 0, 5, 1, 8, 3, 1], K, 2056, dtype, layout, k=2, extra=3, pad=8)
     check([70, 0, 200, 1, 33], K, 1032, dtype, layout, extra=40)
+
+
+# the gradient of few weights: rows shared by wavefronts, 64 x 64 weights to a workgroup
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+def test_gradient_of_few_weights(dtype, layout):
+    check([300, 0, 71, 1], 520, 264, dtype, layout, k=2, extra=5)
+    check([15, 16, 17, 0, 33], 264, 392, dtype, layout, pad=8)
+    check([2100], 1160, 1032, dtype, layout, given=False)
