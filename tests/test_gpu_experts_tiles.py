@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from experts_util import E, assert_within, grouped_mm, offsets_of, random
+from experts_util import E, assert_within, grouped_mm, grouped_wgrad, offsets_of, random
 from paper_2209_02882_amd import binding
 from test_gpu_experts_products import check, check_w4, laid_out, result, w4_inputs
 
@@ -188,3 +188,34 @@ def test_gradient_of_few_weights(dtype, layout):
     check([300, 0, 71, 1], 520, 264, dtype, layout, k=2, extra=5)
     check([15, 16, 17, 0, 33], 264, 392, dtype, layout, pad=8)
     check([2100], 1160, 1032, dtype, layout, given=False)
+
+
+# many groups of few rows, and columns enough for tiles of 64 x 128
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("K", [8, 136])
+def test_many_groups_of_few_rows_of_many_columns(K, dtype, layout):
+    check([(7 * g) % 6 for g in range(40)], K, 2056, dtype, layout, k=2, extra=3, pad=8)
+
+
+# rows of X that do not exist count as zeros in every kernel: few tiles (88 columns) and many
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("dtype", [torch.float32, *HALVES])
+@pytest.mark.parametrize("N", [88, 89, 2056])
+def test_missing_rows_of_x(N, dtype, layout):
+    sizes, K, x_rows = [70, 0, 33, 200], 136, 60
+    G, R, offsets = len(sizes), sum(sizes), offsets_of(sizes)
+    src = torch.randint(-3, 2 * x_rows + 7, (R,), generator=torch.Generator().manual_seed(3)).int()
+    src[5], src[6] = 2**31 - 1, -2**31
+    X, dY = random(1, x_rows, K, dtype=dtype), random(3, R, N, dtype=dtype)
+    W = random(2, *((G, N, K) if layout == "nk" else (G, K, N)), dtype=dtype, scale=K**-0.5)
+    gone = (src < 0) | (src // 2 >= x_rows)
+    # the plain form: an additional row of zeros for those that do not exist
+    X0, src0 = torch.cat([X, torch.zeros(1, K, dtype=dtype)]), torch.where(gone, 2 * x_rows, src).int()
+    Y, dW = result(R, N, dtype), torch.full_like(W, float("nan")).cuda()
+    binding.sgap_grouped_mm(G, R, K, N, offsets.cuda(), X.cuda(), W.cuda(), Y, layout, src=src.cuda(), src_div=2)
+    want, size = grouped_mm(offsets, X0, W, layout, R, src0, 2)
+    assert_within(Y, want, size * (K + 4) * E)
+    binding.sgap_grouped_mm_wgrad(G, R, K, N, offsets.cuda(), X.cuda(), dY.cuda(), dW, layout, src=src.cuda(), src_div=2)
+    want, size = grouped_wgrad(offsets, X0, dY, layout, src0, 2)
+    assert_within(dW, want, size * (max(sizes) + 4) * E)
