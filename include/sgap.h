@@ -788,8 +788,8 @@ int sgap_route_combine_grad(int64_t T, int64_t k, int64_t D, int dtype, const vo
  *   Y        R x N, rows ldy apart
  * The gradient of the rows that come in is the same call on dY with the other
  * layout's name: K and N change places, and W stays where it is.  K = 0 gives
- * zeros.  Any sizes, strides and element-aligned addresses; multiples of 16
- * bytes are faster.  Y must not overlap X or W.
+ * zeros.  R, K and N up to 2^31 - 65,536, any strides and element-aligned
+ * addresses; multiples of 16 bytes are faster.  Y must not overlap X or W.
  * Floats are multiplied as sums of three bfloat16 numbers, which hold a
  * float's 24 bits down to 2^-133: a value below 2^-110 counts to within 2^-134.
  */

@@ -15,6 +15,8 @@ namespace {
 using sgap::fail_call;
 
 constexpr int64_t kMaxIndex = 2147483646LL;  // row numbers and their ends are 32-bit
+// rows, inner values and columns of a product: its kernels step past the end by up to three tiles
+constexpr int64_t kMaxSteps = 2147483647LL - 65535;
 
 int invalid(const char* what) { return fail_call(SGAP_ERR_INVALID_ARG, what); }
 
@@ -41,7 +43,8 @@ int check_grouped(int64_t G, int64_t R, int64_t K, int64_t N, const int32_t* off
     if (G < 1) return invalid("there must be at least one group");
     if (R < 0 || K < 0 || N < 0 || x_rows < 0) return invalid("negative dimension");
     if (G > (1 << 20)) return invalid("more than 1,048,576 groups");
-    if (R > kMaxIndex || K > kMaxIndex || N > kMaxIndex || x_rows > kMaxIndex) return invalid("dimension exceeds int32 index range");
+    if (R > kMaxSteps || K > kMaxSteps || N > kMaxSteps || x_rows > kMaxIndex)
+        return invalid("dimension exceeds int32 index range: R, K and N are at most 2^31 - 65536");
     if (!offsets && G != 1) return invalid("offsets may be null for one group only");
     if (src_div < 1 || src_div > kMaxIndex) return invalid("src_div must be positive");
     if (!src && src_div != 1) return invalid("src_div needs src");
@@ -155,7 +158,7 @@ static int check_w4(int64_t G, int64_t K, int64_t N, int64_t group_k)
 {
     if (G < 1 || K < 0 || N < 0) return invalid("negative dimension, or no group");
     if (G > (1 << 20)) return invalid("more than 1,048,576 groups");
-    if (K > kMaxIndex || N > kMaxIndex) return invalid("dimension exceeds int32 index range");
+    if (K > kMaxSteps || N > kMaxSteps) return invalid("dimension exceeds int32 index range: K and N are at most 2^31 - 65536");
     if (group_k != 32 && group_k != 64 && (group_k < 128 || group_k % 128)) return invalid("group_k must be 32, 64 or a multiple of 128");
     if (group_k > kMaxIndex || K % group_k) return invalid("K must be a multiple of group_k");
     return SGAP_OK;
