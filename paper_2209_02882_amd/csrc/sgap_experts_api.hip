@@ -32,7 +32,7 @@ int check_route(int64_t T, int64_t E, int64_t k)
     if (T < 0) return invalid("negative number of tokens");
     if (E < 1 || E > SGAP_MAX_EXPERTS) return invalid("the number of experts must be 1 to 1,024");
     if (k < 1 || k > SGAP_MAX_CHOSEN || k > E) return invalid("k must be 1 to 16, and no more than the experts");
-    if (T * k > kMaxIndex) return invalid("dimension exceeds int32 index range");
+    if (T > kMaxIndex / k) return invalid("dimension exceeds int32 index range");
     return SGAP_OK;
 }
 
@@ -103,7 +103,7 @@ static int check_combine(int64_t T, int64_t k, int64_t D, int dtype)
 {
     if (T < 0 || D < 0) return invalid("negative dimension");
     if (k < 1 || k > SGAP_MAX_CHOSEN) return invalid("k must be 1 to 16");
-    if (T * k > kMaxIndex || D > kMaxIndex) return invalid("dimension exceeds int32 index range");
+    if (T > kMaxIndex / k || D > kMaxIndex) return invalid("dimension exceeds int32 index range");
     if (!any_type(dtype)) return invalid("unknown element type");
     return SGAP_OK;
 }
@@ -161,6 +161,8 @@ static int check_w4(int64_t G, int64_t K, int64_t N, int64_t group_k)
     if (K > kMaxSteps || N > kMaxSteps) return invalid("dimension exceeds int32 index range: K and N are at most 2^31 - 65536");
     if (group_k != 32 && group_k != 64 && (group_k < 128 || group_k % 128)) return invalid("group_k must be 32, 64 or a multiple of 128");
     if (group_k > kMaxIndex || K % group_k) return invalid("K must be a multiple of group_k");
+    // a tile of 16 columns by 128 values is 2 KB at most with its scales and zero points: their sizes and places stay in 64 bits
+    if (G * ((N + 15) / 16) > INT64_MAX / 2048 / ((K + 127) / 128 + 1)) return invalid("the laid-out weights are larger than any memory");
     return SGAP_OK;
 }
 
