@@ -627,6 +627,13 @@ def _rows(t, dtype, rows, columns, name):
     return (t.data_ptr() if t.numel() else None), (t.stride(0) if t.shape[0] > 1 else columns)
 
 
+def _bytes(t, name):
+    """(device pointer, bytes) of a contiguous uint8 tensor, or of None."""
+    import torch
+
+    return (None, 0) if t is None else (_dev_ptr(t, torch.uint8, name), t.numel())
+
+
 def sgap_route_topk_workspace_size(T, E, k) -> int:
     size = load().sgap_route_topk_workspace_size(int(T), int(E), int(k))
     if size < 0:
@@ -647,7 +654,7 @@ def sgap_route_topk(T, E, k, logits, gates, experts, slot, order, offsets, renor
 
     dtype = _element_type(logits, "logits")
     ptr, ld = _rows(logits, logits.dtype, T, E, "logits")
-    ws, ws_bytes = _workspace_args(workspace)
+    ws, ws_bytes = _bytes(workspace, "workspace")
     _check(load().sgap_route_topk(
         T, E, k, dtype, ptr, ld, renormalise, _flat(gates, torch.float32, T * k, "gates"),
         _flat(experts, torch.int32, T * k, "experts"), _flat(slot, torch.int32, T * k, "slot"),
@@ -760,7 +767,7 @@ def sgap_w4_layout(G, K, N, group_k, codes, scales, zeros, weights, stream=None)
     if _element_type(scales, "scales") == SGAP_F32:
         raise TypeError("scales must be float16 or bfloat16")
     blocks = K // max(int(group_k), 1)
-    ws, ws_bytes = _workspace_args(weights)
+    ws, ws_bytes = _bytes(weights, "weights")
     _check(load().sgap_w4_layout(
         G, K, N, int(group_k), _flat(codes, torch.uint8, G * N * (K // 2), "codes"), _flat(scales, scales.dtype, G * N * blocks, "scales"),
         None if zeros is None else _flat(zeros, torch.uint8, G * N * blocks, "zeros"), ws, ws_bytes, _stream_ptr(stream)))
@@ -777,6 +784,6 @@ def sgap_grouped_mm_w4(G, R, K, N, group_k, offsets, X, weights, Y, zeros=False,
         _check(st)
     dtype = _element_type(X, "X")
     args = _grouped_args(G, R, K, offsets, X, src, src_div)
-    ws, ws_bytes = _workspace_args(weights)
+    ws, ws_bytes = _bytes(weights, "weights")
     y, ldy = _rows(Y, X.dtype, R, N, "Y")
     _check(load().sgap_grouped_mm_w4(G, R, K, N, dtype, int(group_k), zeros, *args, ws, ws_bytes, y, ldy, _stream_ptr(stream)))

@@ -91,6 +91,13 @@ struct Call {
         *bytes = t->numel();
         return *bytes ? t->data_ptr() : nullptr;
     }
+    // the same, its bytes side by side: a tensor that repeats its elements has less memory than their number says
+    void* whole_workspace(int n, int64_t* bytes)
+    {
+        void* p = workspace(n, bytes);
+        if (ok && arg[n] != Py_None && !tensor(n)->is_contiguous()) ok = false;
+        return p;
+    }
 };
 
 struct Matrix {
@@ -301,7 +308,7 @@ PyObject* route_topk(PyObject*, PyObject* const* arg, Py_ssize_t n)
     int32_t *experts = c.ints(5, T * k), *slot = c.ints(6, T * k), *order = c.ints(7, T * k), *offsets = c.ints(8, E + 1);
     const int renormalise = c.small(9);
     int64_t bytes = 0;
-    void* ws = c.workspace(10, &bytes);
+    void* ws = c.whole_workspace(10, &bytes);
     void* stream = c.stream(11);
     if (!c.ok) return status(kNotTaken);
     return enqueue([&] {
@@ -433,7 +440,7 @@ PyObject* grouped_mm_w4(PyObject*, PyObject* const* arg, Py_ssize_t n)
     if (!c.ok) return status(kNotTaken);
     const int64_t group_k = c.number(4);
     int64_t bytes = 0;
-    const void* weights = c.workspace(7, &bytes);
+    const void* weights = c.whole_workspace(7, &bytes);
     const Rows Y = rows_of(c, 8, m.type, m.R, m.N);
     const int zeros = c.small(9);
     void* stream = c.stream(12);
