@@ -6,11 +6,13 @@ same with the experts' weights in 4 bits.
 
     python -m paper_2209_02882_amd.experts          trains a small layer for a few steps, then serves it both ways
 
-The activation between the two products is torch's; everything that goes by expert is the library's.
+The activation between the two products is torch's; everything that goes by expert is the library's.  The gradients are not
+differentiable themselves: a second derivative raises an error.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -33,6 +35,7 @@ class Route(torch.autograd.Function):
         return gates, slot, order, offsets
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dgates, *_):
         logits, gates, experts = ctx.saved_tensors
         T, E = logits.shape
@@ -58,6 +61,7 @@ class GroupedMM(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weights, offsets, order, slot = ctx.saved_tensors
         G, N, K = weights.shape
@@ -84,6 +88,7 @@ class Combine(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         rows, gates, slot, order = ctx.saved_tensors
         T, k = slot.shape

@@ -1,0 +1,42 @@
+"""The layer of experts itself: what it differentiates, asks for and keeps.  The library's calls are torch's here.  No GPU."""
+import pytest
+import torch
+
+from experts_on_host import on_host
+from paper_2209_02882_amd import experts
+
+
+def layer_and_x(dtype=torch.float32, tokens=12):
+    torch.manual_seed(3)
+    layer = experts.ExpertLayer(16, 8, 4, 2, dtype=dtype, device="cpu")
+    return layer, torch.randn(tokens, 16).to(dtype).requires_grad_()
+
+
+def plain(layer, x):
+    top, chosen = torch.topk(x @ layer.router.t(), layer.k, dim=1)
+    gates, out = torch.softmax(top, dim=1), torch.zeros_like(x)
+    for e in range(layer.up.shape[0]):
+        h = experts.gated(x @ layer.up[e].t()) @ layer.down[e].t()
+        out = out + h * torch.where(chosen == e, gates, torch.zeros_like(gates)).sum(1, keepdim=True)
+    return out
+
+
+def test_the_calls_on_the_host_are_the_layer(monkeypatch):
+    on_host(monkeypatch)
+    layer, x = layer_and_x()
+    inputs = (x, layer.router, layer.up, layer.down)
+    got = torch.autograd.grad(layer(x).square().sum(), inputs)
+    want = torch.autograd.grad(plain(layer, x).square().sum(), inputs)
+    for g, w in zip(got, want):
+        assert (g - w).abs().max() <= 1e-4 * w.abs().max()
+
+
+# the gradients' own calls are not differentiated: a derivative of a gradient is refused, not silently left out
+@pytest.mark.parametrize("wrt", ["x", "router", "up", "down"])
+def test_second_derivatives_are_refused(wrt, monkeypatch):
+    on_host(monkeypatch)
+    layer, x = layer_and_x()
+    loss = layer(x).square().sum()
+    (grad,) = torch.autograd.grad(loss, x if wrt == "x" else getattr(layer, wrt), create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (loss + grad.square().sum()).backward()  # a gradient penalty
