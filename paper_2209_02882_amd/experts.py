@@ -66,13 +66,16 @@ class GroupedMM(torch.autograd.Function):
         x, weights, offsets, order, slot = ctx.saved_tensors
         G, N, K = weights.shape
         R, dy = order.numel(), dy.contiguous()
-        dx = torch.empty((R, K), dtype=x.dtype, device=x.device)
-        binding.sgap_grouped_mm(G, R, N, K, offsets, dy, weights, dx, "kn")
-        if ctx.gather:
-            rows, dx = dx, torch.empty_like(x)
-            binding.sgap_route_combine(slot.shape[0], slot.shape[1], K, rows, slot, None, dx)
-        dw = torch.empty_like(weights)
-        binding.sgap_grouped_mm_wgrad(G, R, K, N, offsets, x, dy, dw, "nk", **ctx.gather)
+        dx = dw = None
+        if ctx.needs_input_grad[0]:
+            dx = torch.empty((R, K), dtype=x.dtype, device=x.device)
+            binding.sgap_grouped_mm(G, R, N, K, offsets, dy, weights, dx, "kn")
+            if ctx.gather:
+                rows, dx = dx, torch.empty_like(x)
+                binding.sgap_route_combine(slot.shape[0], slot.shape[1], K, rows, slot, None, dx)
+        if ctx.needs_input_grad[1]:
+            dw = torch.empty_like(weights)
+            binding.sgap_grouped_mm_wgrad(G, R, K, N, offsets, x, dy, dw, "nk", **ctx.gather)
         return dx, dw, None, None, None, None
 
 

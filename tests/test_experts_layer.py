@@ -40,3 +40,29 @@ def test_second_derivatives_are_refused(wrt, monkeypatch):
     (grad,) = torch.autograd.grad(loss, x if wrt == "x" else getattr(layer, wrt), create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         (loss + grad.square().sum()).backward()  # a gradient penalty
+
+
+# what has no use for a gradient is not charged for one
+@pytest.mark.parametrize("frozen", ["experts", "x", "x and up"])
+def test_gradients_that_nobody_asks_for_are_not_computed(frozen, monkeypatch):
+    calls = on_host(monkeypatch)
+    layer, x = layer_and_x()
+    if frozen == "experts":
+        layer.up.requires_grad_(False)
+        layer.down.requires_grad_(False)
+    if frozen.startswith("x"):
+        x = x.detach()
+    if frozen == "x and up":
+        layer.up.requires_grad_(False)
+    out = layer(x)
+    del calls[:]
+    out.square().sum().backward()
+    made = {name: calls.count(name) for name in set(calls)}
+    want = {"sgap_route_combine_grad": 1, "sgap_route_topk_grad": 1}
+    if frozen == "experts":  # down to x, through both products
+        want |= {"sgap_grouped_mm": 2, "sgap_route_combine": 1}
+    elif frozen == "x":      # the weights of both, and of the rows between them
+        want |= {"sgap_grouped_mm": 1, "sgap_grouped_mm_wgrad": 2}
+    else:                    # nothing below the second product
+        want |= {"sgap_grouped_mm_wgrad": 1}
+    assert made == want
