@@ -145,8 +145,12 @@ class ExpertLayer(torch.nn.Module):
         self.router, self.up, self.down = new(experts, width), new(experts, 2 * hidden, width), new(experts, width, hidden)
         self.served = None
 
+    def logits(self, x):
+        """In 32 bits: in 16, experts within half a unit of one another would be equal, and the first of them chosen."""
+        return x.float() @ self.router.float().t()
+
     def forward(self, x):
-        gates, slot, order, offsets = Route.apply((x @ self.router.t()).float(), self.k)
+        gates, slot, order, offsets = Route.apply(self.logits(x), self.k)
         h = gated(GroupedMM.apply(x, self.up, offsets, order, slot, True))
         return Combine.apply(GroupedMM.apply(h, self.down, offsets, order, slot, False), gates, slot, order)
 
@@ -160,7 +164,7 @@ class ExpertLayer(torch.nn.Module):
         if self.served is None:
             return self(x)
         up, down = self.served
-        gates, slot, order, offsets = Route.apply((x @ self.router.t()).float(), self.k)
+        gates, slot, order, offsets = Route.apply(self.logits(x), self.k)
         R = order.numel()
         h = gated(up.rows(x, offsets, R, src=order, src_div=self.k))
         out = torch.empty_like(x)

@@ -66,3 +66,29 @@ def test_gradients_that_nobody_asks_for_are_not_computed(frozen, monkeypatch):
     else:                    # nothing below the second product
         want |= {"sgap_grouped_mm_wgrad": 1}
     assert made == want
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("serve", [False, True])
+def test_the_choice_is_made_in_32_bits(serve, dtype, monkeypatch):
+    # logits 16, 16 + d, 16 + 2 d, 16 + 3 d with a d of 2^-9, which a 16-bit 16 does not hold: the last two experts are the choice
+    chosen = []
+    calls = on_host(monkeypatch)
+    layer, _ = layer_and_x(dtype)
+    with torch.no_grad():
+        layer.router.fill_(1.0)
+        x = torch.ones(3, 16, dtype=dtype)
+        x[:, 1], x[:, 2] = 2.0**-8, 2.0
+        layer.router[:, 1] = torch.tensor([0.0, 0.5, 1.0, 1.5])
+    route = experts.Route.apply
+
+    def seen(logits, k):
+        chosen.append(logits)
+        return route(logits, k)
+
+    monkeypatch.setattr(experts.Route, "apply", seen)
+    layer.serve(x) if serve else layer(x)
+    assert "sgap_route_topk" in calls
+    want = x.double() @ layer.router.double().t()
+    assert chosen[0].dtype == torch.float32 and torch.equal(chosen[0].double(), want)
+    assert torch.topk(chosen[0], 2)[1].tolist() == [[3, 2]] * 3
