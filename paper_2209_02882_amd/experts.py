@@ -70,6 +70,8 @@ class GroupedMM(torch.autograd.Function):
         if ctx.needs_input_grad[0]:
             dx = torch.empty((R, K), dtype=x.dtype, device=x.device)
             binding.sgap_grouped_mm(G, R, N, K, offsets, dy, weights, dx, "kn")
+            # a pair's row is rounded to x's type, in which the product stores it, and once more the sum of a token's k rows:
+            # half the bytes written and read that rows of floats would be
             if ctx.gather:
                 rows, dx = dx, torch.empty_like(x)
                 binding.sgap_route_combine(slot.shape[0], slot.shape[1], K, rows, slot, None, dx)
