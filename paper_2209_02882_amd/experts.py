@@ -158,7 +158,7 @@ class ExpertLayer(torch.nn.Module):
 
     @torch.no_grad()
     def quantise(self, group_k=64):
-        """From now on serve() has the experts in 4 bits."""
+        """From now on serve() has the experts as they are now, in 4 bits; after further training, quantise again."""
         self.served = Weights4(self.up, group_k), Weights4(self.down, group_k)
 
     @torch.no_grad()
