@@ -50,10 +50,10 @@ struct Columns {
 
 // A work item: a token and 64 * VEC of its columns.  Sums in 32 bits, rounded once.
 template <typename T, int VEC, int KMAX>
-__global__ __launch_bounds__(kCombineThreads) void combine_kernel(CombineArgs a, uint32_t column_items)
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(CombineArgs a, uint32_t column_items, int64_t block0)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * (kCombineThreads / 64) + (threadIdx.x >> 6);
+    const int64_t item = (block0 + blockIdx.x) * (kCombineThreads / 64) + (threadIdx.x >> 6);
     const int64_t t = item / column_items;
     const int64_t c = ((item - t * column_items) * 64 + lane) * VEC;
     if (t >= a.T || c >= a.D) return;
@@ -87,13 +87,13 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(CombineArgs a,
 // WAVES wavefronts share a token's columns.  Behind the tokens' workgroups come those that clear the rows of dZ that
 // no token has.
 template <typename T, int VEC, int KMAX, int WAVES>
-__global__ __launch_bounds__(kCombineThreads) void combine_grad_kernel(CombineArgs a, int64_t token_blocks)
+__global__ __launch_bounds__(kCombineThreads) void combine_grad_kernel(CombineArgs a, int64_t token_blocks, int64_t block0)
 {
     constexpr int kTokens = kCombineThreads / 64 / WAVES;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t rows = a.T * a.k;
-    if (blockIdx.x >= token_blocks) {
-        const int64_t r0 = ((int64_t)blockIdx.x - token_blocks) * kCombineThreads + wave * 64;
+    const int64_t rows = a.T * a.k, block = block0 + blockIdx.x;
+    if (block >= token_blocks) {
+        const int64_t r0 = (block - token_blocks) * kCombineThreads + wave * 64;
         uint64_t clear = __ballot(r0 + lane < rows && a.order[r0 + lane] < 0);
         for (; clear; clear &= clear - 1) {
             T* __restrict__ row = static_cast<T*>(a.out) + (r0 + __builtin_ctzll(clear)) * a.D;
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kCombineThreads) void combine_grad_kernel(CombineAr
         }
         return;
     }
-    const int64_t t = (int64_t)blockIdx.x * kTokens + wave / WAVES;
+    const int64_t t = block * kTokens + wave / WAVES;
     float dot[KMAX], gate[KMAX];
     int64_t slot[KMAX];
     const bool token = t < a.T;
@@ -161,9 +161,9 @@ template <typename T, int VEC, int KMAX>
 hipError_t combine(const CombineArgs& a, hipStream_t s)
 {
     const int64_t columns = (a.D + 64 * VEC - 1) / (64 * VEC), items = a.T * columns;
-    const unsigned grid = (unsigned)((items + kCombineThreads / 64 - 1) / (kCombineThreads / 64));
-    combine_kernel<T, VEC, KMAX><<<grid, kCombineThreads, 0, s>>>(a, (uint32_t)columns);
-    return hipGetLastError();
+    return launch_parts((items + kCombineThreads / 64 - 1) / (kCombineThreads / 64), kCombineThreads, [&](unsigned grid, int64_t block0) {
+        combine_kernel<T, VEC, KMAX><<<grid, kCombineThreads, 0, s>>>(a, (uint32_t)columns, block0);
+    });
 }
 
 template <typename T, int VEC, int KMAX>
@@ -172,12 +172,13 @@ hipError_t combine_grad(const CombineArgs& a, hipStream_t s)
     const int64_t clearing = (a.T * a.k + kCombineThreads - 1) / kCombineThreads;
     // a token's columns go to four wavefronts where tokens are fewer than fill the chip and there are columns for all
     if (a.T < 4096 && a.D >= 2 * 64 * VEC) {
-        combine_grad_kernel<T, VEC, KMAX, 4><<<(unsigned)(a.T + clearing), kCombineThreads, 0, s>>>(a, a.T);
-    } else {
-        const int64_t blocks = (a.T + 3) / 4;
-        combine_grad_kernel<T, VEC, KMAX, 1><<<(unsigned)(blocks + clearing), kCombineThreads, 0, s>>>(a, blocks);
+        combine_grad_kernel<T, VEC, KMAX, 4><<<(unsigned)(a.T + clearing), kCombineThreads, 0, s>>>(a, a.T, 0);
+        return hipGetLastError();
     }
-    return hipGetLastError();
+    const int64_t blocks = (a.T + 3) / 4;
+    return launch_parts(blocks + clearing, kCombineThreads, [&](unsigned grid, int64_t block0) {
+        combine_grad_kernel<T, VEC, KMAX, 1><<<grid, kCombineThreads, 0, s>>>(a, blocks, block0);
+    });
 }
 
 template <typename T, int VEC>

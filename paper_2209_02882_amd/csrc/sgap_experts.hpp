@@ -151,6 +151,20 @@ struct CombineArgs {
     float* __restrict__ dgates;
 };
 
+// A launch has fewer than 2^32 threads: more workgroups go out as several launches, launch(workgroups, block0), in which
+// workgroup b is number block0 + b of all.  (Parts are multiples of 256 workgroups, so that eight dies have whole turns.)
+template <typename F>
+inline hipError_t launch_parts(int64_t workgroups, int threads, F&& launch)
+{
+    const int64_t most = (0xffffffffLL / threads) & ~255LL;
+    for (int64_t block0 = 0; block0 < workgroups; block0 += most) {
+        const int64_t left = workgroups - block0;
+        launch((unsigned)(left < most ? left : most), block0);
+        if (const hipError_t err = hipGetLastError()) return err;
+    }
+    return hipSuccess;
+}
+
 int64_t route_workspace_bytes(int64_t T, int64_t E, int64_t k);
 hipError_t launch_route(const RouteArgs& a, hipStream_t s);
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);

@@ -32,14 +32,14 @@ constexpr int kRun = 32, kGradientRun = 16;
 
 // WIDE: rows of X lie further than 32 bits of bytes from its first.
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
-__global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, int64_t column_tiles, int64_t items, bool apart)
+__global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, int64_t column_tiles, int64_t items, bool apart, int64_t block0)
 {
     using Wt = Tile<T, BN, !KN, THREADS>;
     using Xt = Tile<T, BM, true, THREADS>;
     constexpr int kWaves = THREADS / 64, WN = kWaves / 2, WM = 2;
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     extern __shared__ __align__(16) char lds[];
-    const int64_t item = dealt_item<kRun>(blockIdx.x);
+    const int64_t item = block0 + dealt_item<kRun>(blockIdx.x);
     if (item >= items) return;
     const int64_t tile = item / column_tiles, n0 = (item - tile * column_tiles) * BN;
     const RowTile rows = find_row_tile<BM>(a.offsets, a.G, a.R, tile);
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(THREADS) void grouped_fast_kernel(GroupedArgs a, in
 // The gradient of the weights.  The inner dimension is the group's rows; both operands have their lines contiguous, and
 // the first has the result's contiguous dimension.
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
-__global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n, int64_t items)
+__global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n, int64_t items,
+                                                                       int64_t block0)
 {
     using Lt = Tile<T, BN, false, THREADS>;
     using Rt = Tile<T, BM, false, THREADS>;
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     constexpr int kXAt = KN ? Lt::kBytes : 0, kYAt = KN ? 0 : Lt::kBytes;
     extern __shared__ __align__(16) char lds[];
-    const int64_t item = dealt_item<kGradientRun>(blockIdx.x);
+    const int64_t item = block0 + dealt_item<kGradientRun>(blockIdx.x);
     if (item >= items) return;
     const int64_t per = tiles_m * tiles_n, g = item / per, in = item - g * per;
     const int64_t lines = KN ? a.K : a.N, columns = KN ? a.N : a.K;  // of the result
@@ -258,33 +259,33 @@ __global__ __launch_bounds__(THREADS) void grouped_wgrad_fast_kernel(GroupedArgs
 }
 
 // whole turns of the dies' runs
-unsigned dealt_grid(int64_t items) { return (unsigned)((items + 255) / 256 * 256); }
+int64_t dealt_grid(int64_t items) { return (items + 255) / 256 * 256; }
 
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
 hipError_t run_fast(const GroupedArgs& a, hipStream_t s)
 {
     const int64_t columns = (a.N + BN - 1) / BN, items = columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr);
-    if (items > 0x7fffff00LL) return hipErrorInvalidConfiguration;
     constexpr int kLds = 2 * 128 * (BM + BN);
     // (a row of 4,096 bytes or a multiple: 16 experts for 32 rows, 2,048 x 4,096 bf16, 56.7 us together and 47.7 apart; rows
     // of 2,000 bytes 29.2 and 32.5)
     const bool apart = !KN && a.R <= BM * a.G && a.K * (int64_t)sizeof(T) % 4096 == 0;
     static uint64_t allowed = 0;
     if (const hipError_t err = allow_lds(grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS>, kLds, allowed)) return err;
-    grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, columns, items, apart);
-    return hipGetLastError();
+    return launch_parts(dealt_grid(items), THREADS, [&](unsigned grid, int64_t block0) {
+        grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<grid, THREADS, kLds, s>>>(a, columns, items, apart, block0);
+    });
 }
 
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
 hipError_t run_wgrad_fast(const GroupedArgs& a, hipStream_t s)
 {
     const int64_t tm = ((KN ? a.K : a.N) + BM - 1) / BM, tn = ((KN ? a.N : a.K) + BN - 1) / BN, items = a.G * tm * tn;
-    if (items > 0x7fffff00LL) return hipErrorInvalidConfiguration;
     constexpr int kLds = 2 * 128 * (BM + BN);
     static uint64_t allowed = 0;
     if (const hipError_t err = allow_lds(grouped_wgrad_fast_kernel<T, BM, BN, KN, WIDE, THREADS>, kLds, allowed)) return err;
-    grouped_wgrad_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<dealt_grid(items), THREADS, kLds, s>>>(a, tm, tn, items);
-    return hipGetLastError();
+    return launch_parts(dealt_grid(items), THREADS, [&](unsigned grid, int64_t block0) {
+        grouped_wgrad_fast_kernel<T, BM, BN, KN, WIDE, THREADS><<<grid, THREADS, kLds, s>>>(a, tm, tn, items, block0);
+    });
 }
 
 // Tiles that a compute unit gets, times what one costs: BM x BN products, dearer in small tiles, whose operands are fetched

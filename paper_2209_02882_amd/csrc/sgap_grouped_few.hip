@@ -35,13 +35,13 @@ __device__ __forceinline__ void share_blocks(int wave, int waves, int64_t blocks
 }
 
 template <typename T, int NT, int MT>
-__global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t column_items)
+__global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t column_items, int64_t block0)
 {
     constexpr int P = Piece<T>::kCount, kStep = 4 * P, kBlock = 4 * kStep;
     __shared__ f32x4 part[8][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
-    const int64_t g = blockIdx.x / column_items, n0 = (blockIdx.x - g * column_items) * (NT * kTileN);
+    const int64_t item = block0 + blockIdx.x, g = item / column_items, n0 = (item - g * column_items) * (NT * kTileN);
     const GroupRows gr = group_rows(a.offsets, g, a.R);
     T* __restrict__ Y = static_cast<T*>(a.Y);
     const int64_t blocks = (a.K + kBlock - 1) / kBlock;
@@ -147,7 +147,7 @@ __device__ __forceinline__ piece_t<T> column_of(const T __attribute__((ext_vecto
 // The same by weights K x N.  A lane takes V columns of as many rows of W as it has values of a row of X, and value e of
 // each, put together in registers, is its piece of column tile e: columns n0 + V * (0 .. 15) + e.
 template <typename T, int V, int MT>
-__global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int64_t column_items)
+__global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int64_t column_items, int64_t block0)
 {
     typedef T row_t __attribute__((ext_vector_type(V)));
     // a block: so many steps that their rows of W are 32 registers
@@ -155,7 +155,7 @@ __global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int6
     __shared__ f32x4 part[8][V][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
-    const int64_t g = blockIdx.x / column_items, n0 = (blockIdx.x - g * column_items) * kColumns;
+    const int64_t item = block0 + blockIdx.x, g = item / column_items, n0 = (item - g * column_items) * kColumns;
     const GroupRows gr = group_rows(a.offsets, g, a.R);
     T* __restrict__ Y = static_cast<T*>(a.Y);
     const int64_t blocks = (a.K + kBlock - 1) / kBlock;
@@ -364,18 +364,18 @@ template <typename T, int V, int MT>
 hipError_t few_kn(const GroupedArgs& a, int waves, hipStream_t s)
 {
     const int64_t items = (a.N + V * 16 - 1) / (V * 16);
-    if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    grouped_few_kn_kernel<T, V, MT><<<dim3((unsigned)(a.G * items), down(a, 16 * MT)), 64 * waves, 0, s>>>(a, items);
-    return hipGetLastError();
+    return launch_parts(a.G * items, 64 * waves, [&](unsigned grid, int64_t block0) {
+        grouped_few_kn_kernel<T, V, MT><<<dim3(grid, down(a, 16 * MT)), 64 * waves, 0, s>>>(a, items, block0);
+    });
 }
 
 template <typename T, int NT, int MT>
 hipError_t few(const GroupedArgs& a, int waves, hipStream_t s)
 {
     const int64_t items = (a.N + NT * kTileN - 1) / (NT * kTileN);
-    if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    grouped_few_kernel<T, NT, MT><<<dim3((unsigned)(a.G * items), down(a, 16 * MT)), 64 * waves, 0, s>>>(a, items);
-    return hipGetLastError();
+    return launch_parts(a.G * items, 64 * waves, [&](unsigned grid, int64_t block0) {
+        grouped_few_kernel<T, NT, MT><<<dim3(grid, down(a, 16 * MT)), 64 * waves, 0, s>>>(a, items, block0);
+    });
 }
 
 template <typename T>
@@ -399,12 +399,12 @@ hipError_t by_columns(const GroupedArgs& a, hipStream_t s)
     return few<T, 2, 1>(a, waves, s);
 }
 
+// (no more than 128 tiles of 128 x 128)
 template <typename T, int V, bool KN>
 hipError_t few_wgrad(const GroupedArgs& a, hipStream_t s)
 {
     constexpr int kSide = 16 * V;
     const int64_t tm = ((KN ? a.K : a.N) + kSide - 1) / kSide, tn = ((KN ? a.N : a.K) + kSide - 1) / kSide;
-    if (a.G * tm * tn > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     grouped_few_wgrad_kernel<T, V, KN><<<(unsigned)(a.G * tm * tn), 512, 0, s>>>(a, tm, tn);
     return hipGetLastError();
 }

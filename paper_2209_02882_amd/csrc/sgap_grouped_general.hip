@@ -61,7 +61,7 @@ __device__ __forceinline__ void store_four(T* __restrict__ p, f32x4 v, int64_t c
 // branches, or they would come one after the other: what would pass the end of a row is read from so much further in front
 // and moved down when it has arrived, and what is behind the last row or column is read from the last.
 template <typename T, int BM, bool KN, bool SHORT>
-__global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a, int64_t column_tiles)
+__global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a, int64_t column_tiles, int64_t block0)
 {
     constexpr int BN = 128;
     using Wt = Tile<T, BN, !KN, kThreads>;
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a
     constexpr int WN = BM >= 64 ? 2 : 4, WM = 4 / WN;  // wavefronts along the columns and the rows
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16, P = Wt::P;
     __shared__ __align__(16) char lds[2 * (Wt::kBytes + Xt::kBytes)];
-    const int64_t tile = blockIdx.x / column_tiles, n0 = (blockIdx.x - tile * column_tiles) * BN;
+    const int64_t item = block0 + blockIdx.x, tile = item / column_tiles, n0 = (item - tile * column_tiles) * BN;
     const RowTile rows = find_row_tile<BM>(a.offsets, a.G, a.R, tile);
     if (rows.rows <= 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -152,13 +152,13 @@ __global__ __launch_bounds__(kThreads) void grouped_general_kernel(GroupedArgs a
 
 // A tile of the weights' gradient, 128 x 128, over all rows of its group: the rows of the result are N of N x K, K of K x N.
 template <typename T, bool KN, bool SHORT>
-__global__ __launch_bounds__(kThreads) void grouped_wgrad_general_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n)
+__global__ __launch_bounds__(kThreads) void grouped_wgrad_general_kernel(GroupedArgs a, int64_t tiles_m, int64_t tiles_n, int64_t block0)
 {
     constexpr int B = 128;
     using Bt = Tile<T, B, false, kThreads>;
     constexpr int P = Bt::P;
     __shared__ __align__(16) char lds[4 * Bt::kBytes];
-    const int64_t per = tiles_m * tiles_n, g = blockIdx.x / per, in = blockIdx.x - g * per;
+    const int64_t item = block0 + blockIdx.x, per = tiles_m * tiles_n, g = item / per, in = item - g * per;
     const int64_t lines = KN ? a.K : a.N, columns = KN ? a.N : a.K;
     const int64_t m0 = in / tiles_n * B, n0 = in % tiles_n * B;
     const GroupRows gr = group_rows(a.offsets, g, a.R);
@@ -232,11 +232,11 @@ __global__ __launch_bounds__(kThreads) void grouped_wgrad_general_kernel(Grouped
 template <typename T, int BM, bool SHORT>
 hipError_t general(const GroupedArgs& a, hipStream_t s)
 {
-    const int64_t columns = (a.N + 127) / 128, grid = columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr);
-    if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    if (a.weights_kn) grouped_general_kernel<T, BM, true, SHORT><<<(unsigned)grid, kThreads, 0, s>>>(a, columns);
-    else grouped_general_kernel<T, BM, false, SHORT><<<(unsigned)grid, kThreads, 0, s>>>(a, columns);
-    return hipGetLastError();
+    const int64_t columns = (a.N + 127) / 128;
+    return launch_parts(columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr), kThreads, [&](unsigned grid, int64_t block0) {
+        if (a.weights_kn) grouped_general_kernel<T, BM, true, SHORT><<<grid, kThreads, 0, s>>>(a, columns, block0);
+        else grouped_general_kernel<T, BM, false, SHORT><<<grid, kThreads, 0, s>>>(a, columns, block0);
+    });
 }
 
 // rows of fewer elements than a piece has, or no rows
@@ -262,11 +262,10 @@ template <typename T, bool SHORT>
 hipError_t wgrad_as(const GroupedArgs& a, hipStream_t s)
 {
     const int64_t tm = ((a.weights_kn ? a.K : a.N) + 127) / 128, tn = ((a.weights_kn ? a.N : a.K) + 127) / 128;
-    if (a.G * tm * tn > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const unsigned grid = (unsigned)(a.G * tm * tn);
-    if (a.weights_kn) grouped_wgrad_general_kernel<T, true, SHORT><<<grid, kThreads, 0, s>>>(a, tm, tn);
-    else grouped_wgrad_general_kernel<T, false, SHORT><<<grid, kThreads, 0, s>>>(a, tm, tn);
-    return hipGetLastError();
+    return launch_parts(a.G * tm * tn, kThreads, [&](unsigned grid, int64_t block0) {
+        if (a.weights_kn) grouped_wgrad_general_kernel<T, true, SHORT><<<grid, kThreads, 0, s>>>(a, tm, tn, block0);
+        else grouped_wgrad_general_kernel<T, false, SHORT><<<grid, kThreads, 0, s>>>(a, tm, tn, block0);
+    });
 }
 
 template <typename T>

@@ -291,11 +291,12 @@ __global__ __launch_bounds__(THREADS) void route_few_kernel(RouteArgs a)
 // More tokens: the choice, with the blocks' counts by expert (count[e * stride + b]) and the pairs' ranks within their
 // block (in slot) ...
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, int rows_per_block, uint16_t* count, int stride)
+__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, int rows_per_block, uint16_t* count, int stride,
+                                                                     int64_t block0)
 {
     extern __shared__ __align__(16) char lds[];
     const RouteShared s = route_shared(lds);
-    const int64_t row0 = (int64_t)blockIdx.x * rows_per_block;
+    const int64_t block = block0 + blockIdx.x, row0 = block * rows_per_block;
     const int rows = (int)min((int64_t)rows_per_block, a.T - row0);
     const int pairs = rows * a.k, p = my_pair();
     choose_rows<T, LANES, V, kRouteThreads>(a, s, row0, rows);
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a
     const int rank = rank_pair(s, a.E, pairs);
     __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += kRouteThreads)
-        count[(int64_t)e * stride + blockIdx.x] = (uint16_t)sum_shares<kRouteThreads>(s, a.E, e);
+        count[(int64_t)e * stride + block] = (uint16_t)sum_shares<kRouteThreads>(s, a.E, e);
     __syncthreads();
     if (p >= pairs) return;
     const int e = s.expert[p];
@@ -331,10 +332,11 @@ __global__ __launch_bounds__(256) void route_scan_kernel(const uint16_t* count, 
 // blocks before this one, and all of them.
 template <bool SUM>
 __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a, int rows_per_block, const uint16_t* count,
-                                                                    const int32_t* summed, const int32_t* total, int blocks, int stride)
+                                                                    const int32_t* summed, const int32_t* total, int blocks, int stride,
+                                                                    int64_t block0)
 {
     __shared__ int32_t all[kMaxExperts], before[kMaxExperts], start[kMaxExperts + 1], wave_total[kRouteThreads / 64];
-    const int mine = blockIdx.x;
+    const int mine = (int)(block0 + blockIdx.x);
     if constexpr (SUM) {
         const int sub = threadIdx.x & 15;
         for (int e = threadIdx.x >> 4; e < a.E; e += kRouteThreads / 16) {
@@ -380,11 +382,11 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a,
 
 // dl_e = p_e ([e chosen] dg_e - sum of g dg) with p over all experts, or, renormalised, the same over the chosen ones alone.
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kGradThreads) void route_grad_kernel(RouteGradArgs a)
+__global__ __launch_bounds__(kGradThreads) void route_grad_kernel(RouteGradArgs a, int64_t block0)
 {
     constexpr int kGroups = kGradThreads / LANES;
     const int sub = threadIdx.x & (LANES - 1);
-    const int64_t t = (int64_t)blockIdx.x * kGroups + threadIdx.x / LANES;
+    const int64_t t = (block0 + blockIdx.x) * kGroups + threadIdx.x / LANES;
     if (t >= a.T) return;
     int expert = -1;
     float gate = 0.0f, dgate = 0.0f;
@@ -430,19 +432,18 @@ __global__ __launch_bounds__(kGradThreads) void route_grad_kernel(RouteGradArgs 
 }
 
 template <typename F, typename T>
-bool by_experts(int E, F&& f, T)
+hipError_t by_experts(int E, F&& f, T)
 {
-    if (E <= 16) f.template operator()<T, 16, 1>();
-    else if (E <= 32) f.template operator()<T, 16, 2>();
-    else if (E <= 64) f.template operator()<T, 16, 4>();
-    else if (E <= 128) f.template operator()<T, 16, 8>();
-    else if (E <= 256) f.template operator()<T, 16, 16>();
-    else if (E <= 512) f.template operator()<T, 64, 8>();
-    else f.template operator()<T, 64, 16>();
-    return true;
+    if (E <= 16) return f.template operator()<T, 16, 1>();
+    if (E <= 32) return f.template operator()<T, 16, 2>();
+    if (E <= 64) return f.template operator()<T, 16, 4>();
+    if (E <= 128) return f.template operator()<T, 16, 8>();
+    if (E <= 256) return f.template operator()<T, 16, 16>();
+    if (E <= 512) return f.template operator()<T, 64, 8>();
+    return f.template operator()<T, 64, 16>();
 }
 template <typename F>
-bool by_type(int dtype, int E, F&& f)
+hipError_t by_type(int dtype, int E, F&& f)
 {
     switch (dtype) {
         case 0: return by_experts(E, f, 0.0f);
@@ -462,13 +463,14 @@ struct RouteFew {
     const RouteArgs& a;
     hipStream_t s;
     template <typename T, int LANES, int V>
-    void operator()() const
+    hipError_t operator()() const
     {
         // a pass of the small block's groups of lanes, and a pair to a thread
         if (a.T <= kFewThreads / LANES && a.T * a.k <= kFewThreads)
             route_few_kernel<T, LANES, V, kFewThreads><<<1, kFewThreads, route_shared_bytes(kFewThreads, a.E), s>>>(a);
         else
             route_few_kernel<T, LANES, V, kRouteThreads><<<1, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(a);
+        return hipGetLastError();
     }
 };
 
@@ -496,20 +498,24 @@ struct RouteChoose {
     const RouteCounts& c;
     hipStream_t s;
     template <typename T, int LANES, int V>
-    void operator()() const
+    hipError_t operator()() const
     {
-        route_choose_kernel<T, LANES, V><<<c.blocks, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(
-            a, c.rows, static_cast<uint16_t*>(a.workspace), c.stride);
+        return launch_parts(c.blocks, kRouteThreads, [&](unsigned grid, int64_t block0) {
+            route_choose_kernel<T, LANES, V><<<grid, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(
+                a, c.rows, static_cast<uint16_t*>(a.workspace), c.stride, block0);
+        });
     }
 };
 struct RouteGrad {
     const RouteGradArgs& a;
     hipStream_t s;
     template <typename T, int LANES, int V>
-    void operator()() const
+    hipError_t operator()() const
     {
         constexpr int kGroups = kGradThreads / LANES;
-        route_grad_kernel<T, LANES, V><<<(unsigned)((a.T + kGroups - 1) / kGroups), kGradThreads, 0, s>>>(a);
+        return launch_parts((a.T + kGroups - 1) / kGroups, kGradThreads, [&](unsigned grid, int64_t block0) {
+            route_grad_kernel<T, LANES, V><<<grid, kGradThreads, 0, s>>>(a, block0);
+        });
     }
 };
 
@@ -525,28 +531,22 @@ int64_t route_workspace_bytes(int64_t T, int64_t E, int64_t k)
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s)
 {
-    if (route_in_one(a.T, a.k)) {
-        by_type(a.dtype, a.E, RouteFew{a, s});
-        return hipGetLastError();
-    }
+    if (route_in_one(a.T, a.k)) return by_type(a.dtype, a.E, RouteFew{a, s});
     const RouteCounts c = route_counts(a.T, a.E, a.k);
     char* const at = static_cast<char*>(a.workspace);
     const uint16_t* const count = reinterpret_cast<const uint16_t*>(at);
     int32_t *summed = reinterpret_cast<int32_t*>(at + c.summed_at), *total = reinterpret_cast<int32_t*>(at + c.total_at);
-    by_type(a.dtype, a.E, RouteChoose{a, c, s});
-    if (c.each) {
-        route_place_kernel<true><<<c.blocks, kRouteThreads, 0, s>>>(a, c.rows, count, nullptr, nullptr, c.blocks, c.stride);
-    } else {
-        route_scan_kernel<<<(a.E + 3) / 4, 256, 0, s>>>(count, summed, total, c.blocks, c.stride, a.E);
-        route_place_kernel<false><<<c.blocks, kRouteThreads, 0, s>>>(a, c.rows, count, summed, total, c.blocks, c.stride);
-    }
-    return hipGetLastError();
+    if (const hipError_t err = by_type(a.dtype, a.E, RouteChoose{a, c, s})) return err;
+    if (!c.each) route_scan_kernel<<<(a.E + 3) / 4, 256, 0, s>>>(count, summed, total, c.blocks, c.stride, a.E);
+    return launch_parts(c.blocks, kRouteThreads, [&](unsigned grid, int64_t block0) {
+        if (c.each) route_place_kernel<true><<<grid, kRouteThreads, 0, s>>>(a, c.rows, count, nullptr, nullptr, c.blocks, c.stride, block0);
+        else route_place_kernel<false><<<grid, kRouteThreads, 0, s>>>(a, c.rows, count, summed, total, c.blocks, c.stride, block0);
+    });
 }
 
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s)
 {
-    by_type(a.dtype, a.E, RouteGrad{a, s});
-    return hipGetLastError();
+    return by_type(a.dtype, a.E, RouteGrad{a, s});
 }
 
 }  // namespace sgap

@@ -128,7 +128,7 @@ constexpr int kMostWaves = 8;
 // take 16 lanes to one turn.  For rows at addresses that are multiples of 16 bytes; others load as the unit wants them.
 template <typename T, int STEPS, int NT, int MT, bool ZEROS, bool STAGED>
 __global__ __launch_bounds__(64 * kMostWaves) void grouped_w4_kernel(GroupedW4Args a, W4Sizes z, int64_t column_items,
-                                                                              int64_t blocks, bool tail)
+                                                                              int64_t blocks, bool tail, int64_t block0)
 {
     using Block = W4Block<T, STEPS, NT, ZEROS>;
     constexpr int kPer = Block::kPer, kRowBytes = 2 * kBlockK, kStaged = MT * 16 * kRowBytes;
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void grouped_w4_kernel(GroupedW4Ar
     f32x4(*const part)[64] = reinterpret_cast<f32x4(*)[64]>(lds);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
-    const int64_t g = blockIdx.x / column_items, item = blockIdx.x - g * column_items;
+    const int64_t at0 = block0 + blockIdx.x, g = at0 / column_items, item = at0 - g * column_items;
     const int64_t tile0 = item * NT;
     const uint8_t* __restrict__ tiles = a.weights + g * z.tiles_n * z.blocks_k * kTileBytes;
     const T* __restrict__ scales = reinterpret_cast<const T*>(a.weights + z.scales_at) + g * z.tiles_n * z.scales_k * kTileN;
@@ -331,16 +331,16 @@ template <typename T, int STEPS, int NT, int MT, bool ZEROS, bool STAGED>
 hipError_t launch_as(const GroupedW4Args& a, const W4Sizes& z, int waves, int row_items, hipStream_t s)
 {
     const int64_t items = (z.tiles_n + NT - 1) / NT;
-    if (a.G * items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)(a.G * items), (unsigned)row_items);
     // whole blocks, and one that is not; without a row of X there is nothing to read
     const int64_t blocks = a.from.rows > 0 ? a.K / kBlockK : 0;
     const bool tail = a.from.rows > 0 && a.K % kBlockK;
     static uint64_t allowed = 0;
     constexpr int kEach = STAGED ? MT * 4096 : 1024;
     if (const hipError_t err = allow_lds(grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED>, kMostWaves * kEach, allowed)) return err;
-    grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED><<<grid, 64 * waves, waves * kEach, s>>>(a, z, items, blocks, tail);
-    return hipGetLastError();
+    return launch_parts(a.G * items, 64 * waves, [&](unsigned grid, int64_t block0) {
+        grouped_w4_kernel<T, STEPS, NT, MT, ZEROS, STAGED><<<dim3(grid, (unsigned)row_items), 64 * waves, waves * kEach, s>>>(
+            a, z, items, blocks, tail, block0);
+    });
 }
 
 template <typename T, int STEPS, int NT, int MT>
@@ -420,8 +420,11 @@ hipError_t launch_w4_layout(int64_t G, int64_t K, int64_t N, int group_k, const 
     return hipGetLastError();
 }
 
-hipError_t launch_grouped_w4(const GroupedW4Args& a, int dtype, hipStream_t s)
+hipError_t launch_grouped_w4(const GroupedW4Args& args, int dtype, hipStream_t s)
 {
+    GroupedW4Args a = args;
+    // nothing to multiply: zeros, whatever the groups are (they take no memory here, and might be more than can be launched)
+    if (a.K == 0) a.G = 1, a.offsets = nullptr;
     const W4Sizes z = w4_sizes(a.G, a.K, a.N, a.group_k, a.zeros);
     return dtype == 1 ? by_scale<half_t>(a, z, s) : by_scale<bf16_t>(a, z, s);
 }
