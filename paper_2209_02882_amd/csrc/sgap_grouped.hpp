@@ -81,4 +81,61 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
 }
 
+// Sums of floats over a long inner dimension: what a run of tiles sums up is added to the total of the runs before, so that a
+// sum's error grows with the length of a run (512 values) and the number of runs, not with their product.  Root mean square
+// of the result's error, with and without: 3,384 values through registers 4.0e-7, 1.0e-6; 262,144 rows of a gradient shared by
+// eight wavefronts 4.3e-7, 3.2e-6 (4.8e-6 in a library's product), where 1,024 x 1,024 weights then take 5.5 ms, 5.0 without.
+// TILES: tiles of the inner dimension to a run.  ASIDE: the totals wait in scratch memory, for kernels whose registers the sums
+// and what is multiplied fill; they are read and written once a run.
+template <bool LONG, int MI, int NJ, int TILES, bool ASIDE = false>
+struct Runs {
+    typedef __attribute__((address_space(5))) f32x4 aside_t;
+    f32x4 total[LONG ? MI : 1][LONG ? NJ : 1];
+    bool any = false;
+    __device__ __forceinline__ Runs()
+    {
+        if constexpr (LONG && !ASIDE) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) total[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+    // total i, j from where the compiler cannot see that it might be a register
+    __device__ __forceinline__ aside_t* aside()
+    {
+        aside_t* p = (aside_t*)&total[0][0];
+        asm volatile("" : "+s"(p));
+        return p;
+    }
+    // after tile t
+    __device__ __forceinline__ void end_of(int t, f32x4 (&acc)[MI][NJ])
+    {
+        if constexpr (LONG) {
+            if ((t + 1) % TILES) return;
+            aside_t* const kept = ASIDE ? aside() : nullptr;
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    if (ASIDE) kept[i * NJ + j] = any ? kept[i * NJ + j] + acc[i][j] : acc[i][j];
+                    else total[i][j] += acc[i][j];
+                    acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+            any = true;
+        }
+    }
+    __device__ __forceinline__ void finish(f32x4 (&acc)[MI][NJ])
+    {
+        if constexpr (LONG) {
+            if (ASIDE && !any) return;
+            aside_t* const kept = ASIDE ? aside() : nullptr;
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j] += ASIDE ? kept[i * NJ + j] : total[i][j];
+        }
+    }
+};
+
 }  // namespace sgap

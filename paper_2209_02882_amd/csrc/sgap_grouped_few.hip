@@ -82,6 +82,8 @@ __global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        Runs<sizeof(T) == 4, NT, MT, 512 / kBlock> runs;
+        int done = 0;
         const auto multiply = [&](int64_t kb, Block& b) {
             if ((kb + 1) * kBlock > a.K) {
 #pragma unroll
@@ -99,8 +101,10 @@ __global__ __launch_bounds__(512) void grouped_few_kernel(GroupedArgs a, int64_t
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = mma16(b.x[mt][i], b.w[nt][i], acc[nt][mt]);
+            runs.end_of(done++, acc);
         };
         share_blocks<Block>(wave, waves, blocks, fetch, multiply);
+        runs.finish(acc);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -202,6 +206,8 @@ __global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int6
         for (int e = 0; e < V; ++e)
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) acc[e][mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        Runs<sizeof(T) == 4, V, MT, 512 / kBlock, (V * MT > 4)> runs;
+        int done = 0;
         const auto multiply = [&](int64_t kb, Block& b) {
             if ((kb + 1) * kBlock > a.K) {
 #pragma unroll
@@ -224,8 +230,10 @@ __global__ __launch_bounds__(512) void grouped_few_kn_kernel(GroupedArgs a, int6
                     (tile(std::integral_constant<int, e>()), ...);
                 }(std::make_integer_sequence<int, V>());
             }
+            runs.end_of(done++, acc);
         };
         share_blocks<Block>(wave, waves, blocks, fetch, multiply);
+        runs.finish(acc);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             __syncthreads();
@@ -262,7 +270,8 @@ __global__ __launch_bounds__(512) void grouped_few_wgrad_kernel(GroupedArgs a, i
     constexpr int P = Piece<T>::kCount, kStep = 4 * P, S = 4 / V, kBlock = S * kStep, kSide = 16 * V;
     __shared__ f32x4 part[8][V][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int waves = blockDim.x >> 6, place = lane & 15, piece = lane >> 4;
+    constexpr int waves = 8;
+    const int place = lane & 15, piece = lane >> 4;
     const int64_t M = KN ? a.K : a.N, N = KN ? a.N : a.K;
     const int64_t g = blockIdx.x / (tiles_m * tiles_n), tile = blockIdx.x - g * tiles_m * tiles_n;
     const int64_t m0 = tile / tiles_n * kSide, n0 = (tile - tile / tiles_n * tiles_n) * kSide;
@@ -309,6 +318,8 @@ __global__ __launch_bounds__(512) void grouped_few_wgrad_kernel(GroupedArgs a, i
     for (int e = 0; e < V; ++e)
 #pragma unroll
         for (int f = 0; f < V; ++f) acc[e][f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    Runs<sizeof(T) == 4, V, V, 512 / kBlock, (V > 2)> runs;
+    int done = 0;
     const auto multiply = [&](int64_t, Block& b) {
 #pragma unroll
         for (int i = 0; i < S; ++i) {
@@ -333,8 +344,10 @@ __global__ __launch_bounds__(512) void grouped_few_wgrad_kernel(GroupedArgs a, i
 #pragma unroll
                 for (int f = 0; f < V; ++f) acc[e][f] = KN ? mma16(x[e], y[f], acc[e][f]) : mma16(y[e], x[f], acc[e][f]);
         }
+        runs.end_of(done++, acc);
     };
     share_blocks<Block>(wave, waves, blocks, fetch, multiply);
+    runs.finish(acc);
     T* __restrict__ W = static_cast<T*>(const_cast<void*>(a.W)) + g * a.K * a.N;
 #pragma unroll
     for (int e = 0; e < V; ++e) {

@@ -323,37 +323,7 @@ __device__ __forceinline__ bool start_over(f32x4 (&acc)[MI][NJ])
     return true;
 }
 
-// Sums of floats over a long inner dimension: what a run of tiles sums up is added to the total of the runs before, so that a
-// sum's error grows with the length of a run (512 values) and the number of runs, not with their product.  3,384 values: 1.0e-6
-// of the result's size without, 4.0e-7 with, at the same time.  (Products of parts, whose instruction sums up 32 values at
-// once, have 4.9e-7 over 1,024 values without and 3.4e-7 with, but there the totals' registers cost a fifth of the time.)
-template <bool LONG, int MI, int NJ>
-struct Runs {
-    static constexpr int kTiles = 16;
-    f32x4 total[LONG ? MI : 1][LONG ? NJ : 1] = {};
-    // after tile t
-    __device__ __forceinline__ void end_of(int t, f32x4 (&acc)[MI][NJ])
-    {
-        if constexpr (LONG) {
-            if ((t + 1) % kTiles) return;
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) total[i][j] += acc[i][j], acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-    }
-    __device__ __forceinline__ void finish(f32x4 (&acc)[MI][NJ])
-    {
-        if constexpr (LONG) {
-#pragma unroll
-            for (int i = 0; i < MI; ++i)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] += total[i][j];
-        }
-    }
-};
-
-// The same where the loads cannot go past the registers (rows at addresses that are no multiples of 16 bytes): a tile's
+// multiply_tiles where the loads cannot go past the registers (rows at addresses that are no multiples of 16 bytes): a tile's
 // pieces wait in registers from the middle of one tile to the middle of the next and are then put into LDS.
 //   fetch(t, i)    piece i of LOADS of tile t as it lies in memory; called for one tile after the other
 //   mend(t, i, v)  what of it belongs there, looked at when it has arrived
@@ -365,7 +335,7 @@ __device__ __forceinline__ void multiply_tiles_staged(char* shared, int tiles, F
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)shared;
     if (tiles == 0) return;
     piece_t<T> fl[2][MI], fr[2][NJ], coming[kLoads];
-    Runs<sizeof(T) == 4, MI, NJ> runs;
+    Runs<sizeof(T) == 4, MI, NJ, 512 / L::kInner> runs;
     const uint32_t lbase = lds + L::lane_base(l0), rbase = lds + L::kBytes + R::lane_base(r0);
     uint32_t lb, rb;
     const auto at = [&](uint32_t stage) {
