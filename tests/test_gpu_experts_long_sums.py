@@ -71,3 +71,16 @@ def test_gradient_of_few_weights_from_many_rows(R, K, N, layout):
 def test_rows_at_odd_addresses(layout):
     assert product_off(300, 65_533, 515, layout) <= by_runs(65_533, 1)
     assert gradient_off(65_533, 259, 131, layout) <= by_runs(65_533, 1)
+
+
+# rows, columns and weights enough for tiles: parts of 16 bits
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("R,K,N", [(2_048, 4_096, 2_048), (2_000, 65_536, 2_040), (4_096, 16_384, 1_024)])
+def test_many_rows_by_long_weights(R, K, N, layout):
+    assert product_off(R, K, N, layout) <= by_parts(K)
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+@pytest.mark.parametrize("R,K,N", [(16_384, 2_048, 2_048), (65_536, 2_048, 2_048), (150_001, 1_032, 2_048)])
+def test_gradient_of_many_weights_from_many_rows(R, K, N, layout):
+    assert gradient_off(R, K, N, layout) <= by_parts(R)
