@@ -99,6 +99,14 @@ int sgap_debug_group_seg_reduce(const float* in, const int32_t* span, float* out
  *     takes the matrix by four neighbouring rows together, 0 if entry by
  *     entry, -1 on bad arguments (rowptr and colidx in host memory; the device
  *     looks at the same rows of its own).
+ *   sgap_debug_grouped_plan: which kernel sgap_grouped_mm, or with `gradient`
+ *     sgap_grouped_mm_wgrad, takes such a call to (aligned: X, W and Y at
+ *     16-byte addresses; given_offsets: offsets not null).  plan[0]: 0 tiles
+ *     loaded past the registers, 1 wavefronts that share the inner dimension,
+ *     2 tiles through registers; plan[1], plan[2]: rows and columns of a
+ *     workgroup's part of the result; plan[3]: 1 where X is addressed in 64
+ *     bits; plan[4]: 1 where workgroups begin at different places of the inner
+ *     dimension; plan[5]: 1 where rows are read element by element.
  */
 int64_t sgap_debug_tile_deal(int64_t tiles, int grid, int block, int64_t* out_tiles, int64_t capacity);
 int sgap_debug_plan_nnz_serial(int group_size, int lanes_per_row, int cols_per_lane, int64_t nnz_hint,
@@ -117,6 +125,9 @@ int sgap_debug_spmm_teams(int64_t M, int64_t K, int64_t N, int64_t nnz_hint, con
 int sgap_debug_mttkrp_teams(int64_t I, int64_t J, int group_size, int strategy, int schedule, int64_t nnz_hint);
 int sgap_debug_sddmm_quads(int64_t M, int64_t K, int64_t J, int group_size, int64_t nnz_hint, const int32_t* rowptr,
                            const int32_t* colidx);
+int sgap_debug_grouped_plan(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, int given_offsets, int64_t ldx,
+                            int64_t x_rows, int64_t ldy, int layout, int gradient, int aligned, int compute_units,
+                            int* plan);
 
 /*
  * Streaming kernels over n fp32 elements (16-byte aligned device buffers):

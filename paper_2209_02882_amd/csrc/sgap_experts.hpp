@@ -171,15 +171,26 @@ hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);
 hipError_t launch_combine_grad(const CombineArgs& a, hipStream_t s);
 // dtype as in sgap.h
-// rows that are multiples of 16 bytes at 16-byte addresses (sgap_grouped_fast.hip); every other call: sgap_grouped_general.hip
+// Which kernel a product over groups, or the gradient of its weights, takes.
+struct GroupedPlan {
+    enum Way {
+        kTiles,     // rows that are multiples of 16 bytes at 16-byte addresses: sgap_grouped_fast.hip
+        kFew,       // of those, too few rows, columns or weights for tiles to fill the chip: sgap_grouped_few.hip
+        kRegisters  // every other call: sgap_grouped_general.hip
+    } way;
+    int rows, columns;  // of a workgroup's part of the result
+    bool wide;          // kTiles: X is longer than 4 GiB
+    bool apart;         // kTiles: workgroups begin at different places of the inner dimension
+    bool short_rows;    // kRegisters: rows of fewer elements than 16 bytes hold
+};
+GroupedPlan plan_grouped(const GroupedArgs& a, int dtype, bool gradient);
+// the parts of that
 bool grouped_fast_applies(const GroupedArgs& a, int dtype);
-hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s);
-hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s);
-// of those, too few rows, columns or weights for tiles to fill the chip (sgap_grouped_few.hip)
-bool grouped_few_applies(const GroupedArgs& a, int dtype);
-hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s);
-bool grouped_few_wgrad_applies(const GroupedArgs& a, int dtype);
-hipError_t launch_grouped_few_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
+GroupedPlan plan_grouped_fast(const GroupedArgs& a, int dtype, bool gradient);
+hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, bool gradient, const GroupedPlan& p, hipStream_t s);
+bool grouped_few_applies(const GroupedArgs& a, int dtype, bool gradient);
+GroupedPlan plan_grouped_few(const GroupedArgs& a, int dtype, bool gradient);
+hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, bool gradient, const GroupedPlan& p, hipStream_t s);
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s);
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s);
 struct W4Sizes {

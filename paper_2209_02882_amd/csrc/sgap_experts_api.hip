@@ -2,6 +2,7 @@
 #include <climits>
 
 #include "../../include/sgap.h"
+#include "../../include/sgap_debug.h"
 #include "sgap_experts.hpp"
 
 namespace sgap {
@@ -152,6 +153,26 @@ int sgap_grouped_mm_wgrad(int64_t G, int64_t R, int64_t K, int64_t N, int dtype,
     const sgap::GroupedArgs a{G, R, K, N, offsets, {src, src_div, x_rows}, X, ldx, dW, const_cast<void*>(dY), lddy,
                               layout == SGAP_WEIGHTS_KN, sgap::device_compute_units()};
     return launched(sgap::launch_grouped_wgrad(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int sgap_debug_grouped_plan(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, int given_offsets, int64_t ldx, int64_t x_rows,
+                            int64_t ldy, int layout, int gradient, int aligned, int compute_units, int* plan)
+{
+    if (!any_type(dtype) || G < 1 || R < 0 || K < 0 || N < 0 || x_rows < 0 || R > kMaxSteps || K > kMaxSteps || N > kMaxSteps ||
+        x_rows > kMaxIndex || ldx < K || ldy < N || (layout != SGAP_WEIGHTS_NK && layout != SGAP_WEIGHTS_KN) || compute_units < 1 || !plan)
+        return invalid("bad arguments");
+    // only the addresses' alignment and whether there are offsets are looked at
+    void* const at = reinterpret_cast<void*>(aligned ? 0x1000 : 0x1004);
+    const int32_t* const offsets = given_offsets ? static_cast<const int32_t*>(at) : nullptr;
+    const sgap::GroupedArgs a{G, R, K, N, offsets, {nullptr, 1, x_rows}, at, ldx, at, at, ldy, layout == SGAP_WEIGHTS_KN, compute_units};
+    const sgap::GroupedPlan p = sgap::plan_grouped(a, dtype, gradient != 0);
+    plan[0] = (int)p.way;
+    plan[1] = p.rows;
+    plan[2] = p.columns;
+    plan[3] = p.wide ? 1 : 0;
+    plan[4] = p.apart ? 1 : 0;
+    plan[5] = p.short_rows ? 1 : 0;
+    return SGAP_OK;
 }
 
 static int check_w4(int64_t G, int64_t K, int64_t N, int64_t group_k)

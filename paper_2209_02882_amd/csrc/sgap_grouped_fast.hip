@@ -267,13 +267,10 @@ __global__ __launch_bounds__(THREADS, kWavesToSimd<T>) void grouped_wgrad_fast_k
 int64_t dealt_grid(int64_t items) { return (items + 255) / 256 * 256; }
 
 template <typename T, int BM, int BN, bool KN, bool WIDE, int THREADS>
-hipError_t run_fast(const GroupedArgs& a, hipStream_t s)
+hipError_t run_fast(const GroupedArgs& a, bool apart, hipStream_t s)
 {
     const int64_t columns = (a.N + BN - 1) / BN, items = columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr);
     constexpr int kLds = 2 * 128 * (BM + BN);
-    // (a row of 4,096 bytes or a multiple: 16 experts for 32 rows, 2,048 x 4,096 bf16, 56.7 us together and 47.7 apart; rows
-    // of 2,000 bytes 29.2 and 32.5)
-    const bool apart = !KN && a.R <= BM * a.G && a.K * (int64_t)sizeof(T) % 4096 == 0;
     static uint64_t allowed = 0;
     if (const hipError_t err = allow_lds(grouped_fast_kernel<T, BM, BN, KN, WIDE, THREADS>, kLds, allowed)) return err;
     return launch_parts(dealt_grid(items), THREADS, [&](unsigned grid, int64_t block0) {
@@ -300,57 +297,21 @@ double turns(int64_t tiles, int compute_units, int BM, int BN, double rate)
     return (double)((tiles + compute_units - 1) / compute_units) * BM * BN / rate;
 }
 
-// 256 x 256, 128 x 128 or 64 x 128, whichever leaves the least to the unit that has most.  A group has a last tile that
-// is not full: 0.6 of a tile more than its rows in the mean.  16 groups, 16,384 rows, 4,096 x 2,048 bf16: 317 us with
-// 256 x 256, 372 with 128 x 128; 64 groups, 8,192 rows, 1,024 x 2,048: 101 and 86.  Floats have the two
-// small ones: the instruction's six products of parts leave no registers for the large.
 template <typename T, bool KN, bool WIDE>
-hipError_t by_size(const GroupedArgs& a, hipStream_t s)
-{
-    constexpr bool kHalf = sizeof(T) == 2;
-    const auto tiles = [&](int BM, int BN) {
-        const double down = a.G == 1 ? (double)((a.R + BM - 1) / BM) : (double)a.R / BM + 0.6 * (double)a.G;
-        return (int64_t)(down * (double)((a.N + BN - 1) / BN));
-    };
-    const double large = turns(tiles(256, 256), a.compute_units, 256, 256, 1.0);
-    const double middle = turns(tiles(128, 128), a.compute_units, 128, 128, kHalf ? 0.7 : 1.0);
-    const double small = turns(tiles(64, 128), a.compute_units, 64, 128, kHalf ? 0.55 : 0.8);
-    if constexpr (kHalf) {
-        if (large <= std::min(middle, small)) return run_fast<T, 256, 256, KN, WIDE, 512>(a, s);
-    }
-    if (middle <= small) return run_fast<T, 128, 128, KN, WIDE, 256>(a, s);
-    return run_fast<T, 64, 128, KN, WIDE, 256>(a, s);
-}
-
-template <typename T, bool KN, bool WIDE>
-hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
+hipError_t by_size(const GroupedArgs& a, bool gradient, const GroupedPlan& p, hipStream_t s)
 {
     if constexpr (sizeof(T) == 2) {
-        if (a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 192) return run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s);
+        if (p.rows == 256) return gradient ? run_wgrad_fast<T, 256, 256, KN, WIDE, 512>(a, s) : run_fast<T, 256, 256, KN, WIDE, 512>(a, p.apart, s);
     }
-    return run_wgrad_fast<T, 128, 128, KN, WIDE, 256>(a, s);
+    if (gradient) return run_wgrad_fast<T, 128, 128, KN, WIDE, 256>(a, s);
+    return p.rows == 128 ? run_fast<T, 128, 128, KN, WIDE, 256>(a, p.apart, s) : run_fast<T, 64, 128, KN, WIDE, 256>(a, p.apart, s);
 }
 
 template <typename T>
-hipError_t by_layout(const GroupedArgs& a, bool gradient, hipStream_t s)
+hipError_t by_layout(const GroupedArgs& a, bool gradient, const GroupedPlan& p, hipStream_t s)
 {
-    // bytes of X from its first row to the end of its last
-    const bool wide = a.from.rows * a.ldx * (int64_t)sizeof(T) > 0xffffffffLL;
-    if (gradient) {
-        if (wide) return a.weights_kn ? wgrad_by_size<T, true, true>(a, s) : wgrad_by_size<T, false, true>(a, s);
-        return a.weights_kn ? wgrad_by_size<T, true, false>(a, s) : wgrad_by_size<T, false, false>(a, s);
-    }
-    if (wide) return a.weights_kn ? by_size<T, true, true>(a, s) : by_size<T, false, true>(a, s);
-    return a.weights_kn ? by_size<T, true, false>(a, s) : by_size<T, false, false>(a, s);
-}
-
-hipError_t by_type(const GroupedArgs& a, int dtype, bool gradient, hipStream_t s)
-{
-    switch (dtype) {
-        case 0: return by_layout<float>(a, gradient, s);
-        case 1: return by_layout<half_t>(a, gradient, s);
-        default: return by_layout<bf16_t>(a, gradient, s);
-    }
+    if (p.wide) return a.weights_kn ? by_size<T, true, true>(a, gradient, p, s) : by_size<T, false, true>(a, gradient, p, s);
+    return a.weights_kn ? by_size<T, true, false>(a, gradient, p, s) : by_size<T, false, false>(a, gradient, p, s);
 }
 
 bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -366,7 +327,43 @@ bool grouped_fast_applies(const GroupedArgs& a, int dtype)
            aligned(a.X) && aligned(a.W) && aligned(a.Y);
 }
 
-hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, hipStream_t s) { return by_type(a, dtype, false, s); }
-hipError_t launch_grouped_wgrad_fast(const GroupedArgs& a, int dtype, hipStream_t s) { return by_type(a, dtype, true, s); }
+// 256 x 256, 128 x 128 or 64 x 128, whichever leaves the least to the unit that has most.  A group has a last tile that
+// is not full: 0.6 of a tile more than its rows in the mean.  16 groups, 16,384 rows, 4,096 x 2,048 bf16: 317 us with
+// 256 x 256, 372 with 128 x 128; 64 groups, 8,192 rows, 1,024 x 2,048: 101 and 86.  Floats have the two
+// small ones: the instruction's six products of parts leave no registers for the large.
+GroupedPlan plan_grouped_fast(const GroupedArgs& a, int dtype, bool gradient)
+{
+    const bool half = dtype != 0;
+    const int64_t size = half ? 2 : 4;
+    GroupedPlan p = {GroupedPlan::kTiles, 128, 128, false, false, false};
+    // bytes of X from its first row to the end of its last
+    p.wide = a.from.rows * a.ldx * size > 0xffffffffLL;
+    if (gradient) {
+        if (half && a.G * ((a.N + 255) / 256) * ((a.K + 255) / 256) >= 192) p.rows = p.columns = 256;
+        return p;
+    }
+    const auto tiles = [&](int BM, int BN) {
+        const double down = a.G == 1 ? (double)((a.R + BM - 1) / BM) : (double)a.R / BM + 0.6 * (double)a.G;
+        return (int64_t)(down * (double)((a.N + BN - 1) / BN));
+    };
+    const double large = turns(tiles(256, 256), a.compute_units, 256, 256, 1.0);
+    const double middle = turns(tiles(128, 128), a.compute_units, 128, 128, half ? 0.7 : 1.0);
+    const double small = turns(tiles(64, 128), a.compute_units, 64, 128, half ? 0.55 : 0.8);
+    if (half && large <= std::min(middle, small)) p.rows = p.columns = 256;
+    else if (middle > small) p.rows = 64;
+    // (a row of 4,096 bytes or a multiple: 16 experts for 32 rows, 2,048 x 4,096 bf16, 56.7 us together and 47.7 apart; rows
+    // of 2,000 bytes 29.2 and 32.5)
+    p.apart = !a.weights_kn && a.R <= p.rows * a.G && a.K * size % 4096 == 0;
+    return p;
+}
+
+hipError_t launch_grouped_fast(const GroupedArgs& a, int dtype, bool gradient, const GroupedPlan& p, hipStream_t s)
+{
+    switch (dtype) {
+        case 0: return by_layout<float>(a, gradient, p, s);
+        case 1: return by_layout<half_t>(a, gradient, p, s);
+        default: return by_layout<bf16_t>(a, gradient, p, s);
+    }
+}
 
 }  // namespace sgap

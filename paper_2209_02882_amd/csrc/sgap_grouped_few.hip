@@ -392,24 +392,17 @@ hipError_t few(const GroupedArgs& a, int waves, hipStream_t s)
 }
 
 template <typename T>
-hipError_t by_columns(const GroupedArgs& a, hipStream_t s)
+hipError_t by_plan(const GroupedArgs& a, const GroupedPlan& p, hipStream_t s)
 {
-    const int64_t used = a.G < a.R ? a.G : a.R, tiles = used * ((a.N + 15) / 16);
-    const int64_t blocks = (a.K * (int64_t)sizeof(T) + 255) / 256, mean = (a.R + a.G - 1) / a.G, most = a.G == 1 ? mean : 2 * mean;
+    const int64_t blocks = (a.K * (int64_t)sizeof(T) + 255) / 256;
     int waves = 8;
     while (waves > 1 && waves / 2 >= blocks) waves /= 2;
-    // More columns to a workgroup where the narrow ones are more than one to a compute unit, so that rows of X are read less
-    // often.  bf16: one group, inner dimension 4,096, by 16 and by 32 columns: 512 rows by 512 columns 27.2, 19.4; 128 by 4,096
-    // 53.3, 38.3; 32 by 4,096 (256 workgroups) 16.3, 21.2.  Weights K x N, 32 and 64 columns: 128 by 4,096 36.3, 22.0; 32 experts
-    // for 64 rows, 2,048 by 1,024 50.1, 30.6; 512 rows by 512 (256) 16.2, 21.2.  128 columns are never better.
     if (a.weights_kn) {
-        const bool narrow = used * ((a.N + 31) / 32) * down(a, most > 16 ? 32 : 16) <= a.compute_units;
-        if (most > 16) return narrow ? few_kn<T, 2, 2>(a, waves, s) : few_kn<T, 4, 2>(a, waves, s);
-        return narrow ? few_kn<T, 2, 1>(a, waves, s) : few_kn<T, 4, 1>(a, waves, s);
+        if (p.rows > 16) return p.columns == 32 ? few_kn<T, 2, 2>(a, waves, s) : few_kn<T, 4, 2>(a, waves, s);
+        return p.columns == 32 ? few_kn<T, 2, 1>(a, waves, s) : few_kn<T, 4, 1>(a, waves, s);
     }
-    if (most > 16) return tiles * down(a, 32) <= a.compute_units ? few<T, 1, 2>(a, waves, s) : few<T, 2, 2>(a, waves, s);
-    if (tiles < 1024) return few<T, 1, 1>(a, waves, s);
-    return few<T, 2, 1>(a, waves, s);
+    if (p.rows > 16) return p.columns == 16 ? few<T, 1, 2>(a, waves, s) : few<T, 2, 2>(a, waves, s);
+    return p.columns == 16 ? few<T, 1, 1>(a, waves, s) : few<T, 2, 1>(a, waves, s);
 }
 
 // (no more than 128 tiles of 128 x 128)
@@ -423,16 +416,11 @@ hipError_t few_wgrad(const GroupedArgs& a, hipStream_t s)
 }
 
 template <typename T>
-hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
+hipError_t wgrad_by_plan(const GroupedArgs& a, const GroupedPlan& p, hipStream_t s)
 {
-    // 32 x 32 weights to a workgroup while there is no more than one to a compute unit, then 64 x 64: 8,192 rows, bf16, by
-    // 512 x 512 (256 of the small) 40 us and 48, 1,024 x 1,024 153 and 52; floats 74 and 163, 286 and 177
-    const int64_t workgroups = a.G * ((a.N + 31) / 32) * ((a.K + 31) / 32);
-    if (workgroups <= a.compute_units) return a.weights_kn ? few_wgrad<T, 2, true>(a, s) : few_wgrad<T, 2, false>(a, s);
+    if (p.rows == 32) return a.weights_kn ? few_wgrad<T, 2, true>(a, s) : few_wgrad<T, 2, false>(a, s);
     return a.weights_kn ? few_wgrad<T, 4, true>(a, s) : few_wgrad<T, 4, false>(a, s);
 }
-
-}  // namespace
 
 // Where tiles of 64 x 128 are too few for the chip.  Up to sixteen rows a group: up to 256 of them; floats, whose tiles take
 // longer, 512, and by weights K x N, which they have to turn round, 1,024.  More rows: 96 and 128; floats 128 and 192.
@@ -445,7 +433,7 @@ hipError_t wgrad_by_size(const GroupedArgs& a, hipStream_t s)
 //   floats  64 groups of 4, 1,024 x 2,048 (1,024) 132, 132, K x N 135, 110; one group, 4,096: 1,024 rows by 1,024 (128) 172, 162;
 //           8 groups, 1,024 rows, 2,048 x 1,024 (160) 90, 98, K x N 94, 68; 16 groups, 1,024 rows, 1,024 x 1,024 (192) K x N
 //           50.5, 42.7; one group, 2,048 rows by 1,024 (256) K x N 176, 219
-bool grouped_few_applies(const GroupedArgs& a, int dtype)
+bool few_rows_apply(const GroupedArgs& a, int dtype)
 {
     if (!grouped_fast_applies(a, dtype)) return false;
     const int64_t mean = (a.R + a.G - 1) / a.G, used = a.G < a.R ? a.G : a.R;  // groups that may have rows
@@ -455,34 +443,54 @@ bool grouped_few_applies(const GroupedArgs& a, int dtype)
     return tiles <= (floats ? (a.weights_kn ? 192 : 128) : a.weights_kn ? 128 : 96);
 }
 
-hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, hipStream_t s)
-{
-    switch (dtype) {
-        case 0: return by_columns<float>(a, s);
-        case 1: return by_columns<half_t>(a, s);
-        default: return by_columns<bf16_t>(a, s);
-    }
-}
-
 // Tiles of 128 x 128 and here, us, in brackets how many tiles:
 //   bf16    8,192 rows by 256 x 256 (4) 143, 37; 1,024 x 1,024 (64) 146, 52; 512 rows by the same 14.2, 8.9, 128 rows 8.0, 7.4;
 //           16 groups of 64 rows, 256 x 256 (64) 7.4, 7.3; 8,192 rows by 2,048 x 1,024 (128) 146, 97; 8 groups of 1,024, 512 x 512
 //           (128) 23.1, 24.0; 1,024 rows by 2,048 x 2,048 (256) 25, 42
 //   floats  8,192 rows by 256 x 256 512, 67; 1,024 x 1,024 520, 177; 2,048 x 1,024 519, 322; 8 groups of 1,024, 512 x 512 71, 56, of
 //           128 15.1, 16.8; 1,024 rows by 2,048 x 2,048 73, 98
-bool grouped_few_wgrad_applies(const GroupedArgs& a, int dtype)
+bool few_weights_apply(const GroupedArgs& a, int dtype)
 {
     if (!grouped_fast_applies(a, dtype)) return false;
     const int64_t tiles = a.G * ((a.N + 127) / 128) * ((a.K + 127) / 128);
     return tiles <= 64 || (tiles <= 128 && a.R / a.G >= (dtype == 0 ? 1024 : 2048));
 }
 
-hipError_t launch_grouped_few_wgrad(const GroupedArgs& a, int dtype, hipStream_t s)
+}  // namespace
+
+bool grouped_few_applies(const GroupedArgs& a, int dtype, bool gradient)
+{
+    return gradient ? few_weights_apply(a, dtype) : few_rows_apply(a, dtype);
+}
+
+GroupedPlan plan_grouped_few(const GroupedArgs& a, int dtype, bool gradient)
+{
+    GroupedPlan p = {GroupedPlan::kFew, 16, 16, false, false, false};
+    if (gradient) {
+        // 32 x 32 weights to a workgroup while there is no more than one to a compute unit, then 64 x 64: 8,192 rows, bf16, by
+        // 512 x 512 (256 of the small) 40 us and 48, 1,024 x 1,024 153 and 52; floats 74 and 163, 286 and 177
+        p.rows = p.columns = a.G * ((a.N + 31) / 32) * ((a.K + 31) / 32) <= a.compute_units ? 32 : 64;
+        return p;
+    }
+    const int64_t used = a.G < a.R ? a.G : a.R, tiles = used * ((a.N + 15) / 16);
+    const int64_t mean = (a.R + a.G - 1) / a.G, most = a.G == 1 ? mean : 2 * mean;
+    if (most > 16) p.rows = 32;
+    // More columns to a workgroup where the narrow ones are more than one to a compute unit, so that rows of X are read less
+    // often.  bf16: one group, inner dimension 4,096, by 16 and by 32 columns: 512 rows by 512 columns 27.2, 19.4; 128 by 4,096
+    // 53.3, 38.3; 32 by 4,096 (256 workgroups) 16.3, 21.2.  Weights K x N, 32 and 64 columns: 128 by 4,096 36.3, 22.0; 32 experts
+    // for 64 rows, 2,048 by 1,024 50.1, 30.6; 512 rows by 512 (256) 16.2, 21.2.  128 columns are never better.
+    if (a.weights_kn) p.columns = used * ((a.N + 31) / 32) * down(a, p.rows) <= a.compute_units ? 32 : 64;
+    else if (most > 16) p.columns = tiles * down(a, 32) <= a.compute_units ? 16 : 32;
+    else p.columns = tiles < 1024 ? 16 : 32;
+    return p;
+}
+
+hipError_t launch_grouped_few(const GroupedArgs& a, int dtype, bool gradient, const GroupedPlan& p, hipStream_t s)
 {
     switch (dtype) {
-        case 0: return wgrad_by_size<float>(a, s);
-        case 1: return wgrad_by_size<half_t>(a, s);
-        default: return wgrad_by_size<bf16_t>(a, s);
+        case 0: return gradient ? wgrad_by_plan<float>(a, p, s) : by_plan<float>(a, p, s);
+        case 1: return gradient ? wgrad_by_plan<half_t>(a, p, s) : by_plan<half_t>(a, p, s);
+        default: return gradient ? wgrad_by_plan<bf16_t>(a, p, s) : by_plan<bf16_t>(a, p, s);
     }
 }
 

@@ -239,23 +239,11 @@ hipError_t general(const GroupedArgs& a, hipStream_t s)
     });
 }
 
-// rows of fewer elements than a piece has, or no rows
 template <typename T>
-bool short_rows(const GroupedArgs& a)
+hipError_t by_rows(const GroupedArgs& a, const GroupedPlan& p, hipStream_t s)
 {
-    return a.K < Piece<T>::kCount || a.N < Piece<T>::kCount || a.from.rows == 0;
-}
-
-template <typename T>
-hipError_t by_rows(const GroupedArgs& a, hipStream_t s)
-{
-    if (short_rows<T>(a)) return general<T, 32, true>(a, s);
-    // Tiles no longer than a group is in the mean (an empty half of a tile costs as much as a full one), and shorter ones
-    // where there are not enough for the chip.
-    if (a.R <= 48 * a.G) return general<T, 32, false>(a, s);
-    const int64_t columns = (a.N + 127) / 128;
-    if ((a.R / 128 + a.G / 2) * columns < 3 * a.compute_units) return general<T, 64, false>(a, s);
-    return general<T, 128, false>(a, s);
+    if (p.short_rows) return general<T, 32, true>(a, s);
+    return p.rows == 32 ? general<T, 32, false>(a, s) : p.rows == 64 ? general<T, 64, false>(a, s) : general<T, 128, false>(a, s);
 }
 
 template <typename T, bool SHORT>
@@ -269,32 +257,49 @@ hipError_t wgrad_as(const GroupedArgs& a, hipStream_t s)
 }
 
 template <typename T>
-hipError_t wgrad(const GroupedArgs& a, hipStream_t s)
+hipError_t wgrad(const GroupedArgs& a, const GroupedPlan& p, hipStream_t s)
 {
-    return short_rows<T>(a) ? wgrad_as<T, true>(a, s) : wgrad_as<T, false>(a, s);
+    return p.short_rows ? wgrad_as<T, true>(a, s) : wgrad_as<T, false>(a, s);
 }
 
 }  // namespace
 
+GroupedPlan plan_grouped(const GroupedArgs& a, int dtype, bool gradient)
+{
+    if (grouped_few_applies(a, dtype, gradient)) return plan_grouped_few(a, dtype, gradient);
+    if (grouped_fast_applies(a, dtype)) return plan_grouped_fast(a, dtype, gradient);
+    GroupedPlan p = {GroupedPlan::kRegisters, 128, 128, false, false, false};
+    const int64_t piece = dtype == 0 ? 4 : 8;
+    p.short_rows = a.K < piece || a.N < piece || a.from.rows == 0;  // or no rows
+    if (gradient) return p;
+    // Tiles no longer than a group is in the mean (an empty half of a tile costs as much as a full one), and shorter ones
+    // where there are not enough for the chip.
+    if (p.short_rows || a.R <= 48 * a.G) p.rows = 32;
+    else if ((a.R / 128 + a.G / 2) * ((a.N + 127) / 128) < 3 * a.compute_units) p.rows = 64;
+    return p;
+}
+
 hipError_t launch_grouped_mm(const GroupedArgs& a, int dtype, hipStream_t s)
 {
-    if (grouped_few_applies(a, dtype)) return launch_grouped_few(a, dtype, s);
-    if (grouped_fast_applies(a, dtype)) return launch_grouped_fast(a, dtype, s);
+    const GroupedPlan p = plan_grouped(a, dtype, false);
+    if (p.way == GroupedPlan::kFew) return launch_grouped_few(a, dtype, false, p, s);
+    if (p.way == GroupedPlan::kTiles) return launch_grouped_fast(a, dtype, false, p, s);
     switch (dtype) {
-        case 0: return by_rows<float>(a, s);
-        case 1: return by_rows<half_t>(a, s);
-        default: return by_rows<bf16_t>(a, s);
+        case 0: return by_rows<float>(a, p, s);
+        case 1: return by_rows<half_t>(a, p, s);
+        default: return by_rows<bf16_t>(a, p, s);
     }
 }
 
 hipError_t launch_grouped_wgrad(const GroupedArgs& a, int dtype, hipStream_t s)
 {
-    if (grouped_few_wgrad_applies(a, dtype)) return launch_grouped_few_wgrad(a, dtype, s);
-    if (grouped_fast_applies(a, dtype)) return launch_grouped_wgrad_fast(a, dtype, s);
+    const GroupedPlan p = plan_grouped(a, dtype, true);
+    if (p.way == GroupedPlan::kFew) return launch_grouped_few(a, dtype, true, p, s);
+    if (p.way == GroupedPlan::kTiles) return launch_grouped_fast(a, dtype, true, p, s);
     switch (dtype) {
-        case 0: return wgrad<float>(a, s);
-        case 1: return wgrad<half_t>(a, s);
-        default: return wgrad<bf16_t>(a, s);
+        case 0: return wgrad<float>(a, p, s);
+        case 1: return wgrad<half_t>(a, p, s);
+        default: return wgrad<bf16_t>(a, p, s);
     }
 }
 
