@@ -211,7 +211,7 @@ __device__ __forceinline__ void multiply_tiles(char* shared, int tiles, F&& load
 }
 
 // Eight floats as three times eight 16-bit ones, x = high + middle + low: eight bits of x's 24 each, rounded to nearest, so
-// that the middle one is at most 2^-9 of x and the low one 2^-17.
+// that the middle one is at most 2^-8 of x and the low one 2^-17.
 struct Split {
     piece_t<bf16_t> high, middle, low;
 };
@@ -243,8 +243,8 @@ __device__ __forceinline__ Split split(piece_t<float> x, piece_t<float> y)
 }
 
 // Products of floats on the 16-bit matrix instruction, which makes sixteen times as many in the same time as the one for
-// floats: of the nine products of the parts the six that count, and what is left out (middle x low and low x low) is
-// under 2^-25 of a product, less than the rounding of a float.  The two half tiles are the instruction's 32 inner values.
+// floats: of the nine products of the parts the six that count, and what is left out (middle x low twice and low x low) is
+// 2^-24 of a product at most, no more than the rounding of a float.  The two half tiles are the instruction's 32 inner values.
 // The six products of 32 inner values are summed up by themselves and then added: one rounding of the sum for 32 values, where
 // the matrix instruction's own additions to it would be six.  Root mean square of the result's
 // error over 1,024, 16,384 and 65,536 values: 1.2e-7, 4.3e-7 and 8.5e-7 (six additions: 4.8e-7, 2.1e-6 and 4.5e-6; a library's

@@ -230,3 +230,14 @@ def test_integers_of_24_bits_are_exact(layout):
     X[torch.arange(R), torch.arange(R) % K] = torch.randint(-2**24, 2**24, (R,), generator=torch.Generator().manual_seed(9)).float()
     W = torch.ones(1, *((N, K) if layout == "nk" else (K, N)))
     assert torch.equal(product(X, W, layout).cpu(), X.sum(1, keepdim=True).expand(R, N))
+
+
+@LAYOUTS
+def test_the_products_of_parts_that_are_left_out(layout):
+    # 1 + 2^-8 - 2^-17 is 1, 2^-8 and -2^-17: what its square leaves out, middle x low twice and low x low, is 2^-24 of it.  Six
+    # products of parts are added, each sum rounded by 2^-23 at most.
+    K, value = 64, 1 + 2.0**-8 - 2.0**-17
+    X, W = torch.zeros(R, K), torch.full((1, N, K) if layout == "nk" else (1, K, N), value)
+    X[torch.arange(R), torch.arange(R) % K] = value
+    got = product(X, W, layout).double().cpu()
+    assert float((got - value**2).abs().max()) <= (1.1 * 2.0**-24 + 6 * 2.0**-23) * value**2
