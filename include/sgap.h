@@ -790,8 +790,11 @@ int sgap_route_combine_grad(int64_t T, int64_t k, int64_t D, int dtype, const vo
  * layout's name: K and N change places, and W stays where it is.  K = 0 gives
  * zeros.  R, K and N up to 2^31 - 65,536, any strides and element-aligned
  * addresses; multiples of 16 bytes are faster.  Y must not overlap X or W.
- * Floats are multiplied as sums of three bfloat16 numbers, which hold a
- * float's 24 bits down to 2^-133: a value below 2^-110 counts to within 2^-134.
+ * Floats: calls of many rows and columns (or, for the weights' gradient, many
+ * weights) whose rows are multiples of 16 bytes at 16-byte addresses multiply
+ * them as sums of three bfloat16 numbers, which hold a float's 24 bits down to
+ * 2^-133: there a value below 2^-110 counts to within 2^-134, and a product to
+ * within 2^-24 of itself.  Other calls use the matrix instruction for floats.
  */
 typedef enum { SGAP_WEIGHTS_NK = 0, SGAP_WEIGHTS_KN = 1 } sgap_weight_layout;
 int sgap_grouped_mm(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, const int32_t* offsets, const void* X, int64_t ldx,
