@@ -809,9 +809,14 @@ int sgap_grouped_mm_wgrad(int64_t G, int64_t R, int64_t K, int64_t N, int dtype,
 /*
  * The same product with weights of 4 bits,
  *   W[g][n, k] = (code[g][n, k] - zero[g][n, k / group_k]) * scale[g][n, k / group_k],
- * for few rows a group: the weights pass once for every 16, 32 or 48 rows.  No weight is rounded on the way.  sgap_w4_layout puts codes, scales
- * and zero points into the order in which the product reads them; a program
- * does that once, when it loads its weights, and may free them afterwards.
+ * for few rows a group: the weights pass once for every 16, 32 or 48 rows.  No
+ * weight is rounded on the way, but what is summed up (in 32 bits) is (16 +
+ * code) * x less (16 + zero) * x: the rounding of a result goes with the sum of
+ * |x| * (32 + code + zero) * scale, and weights that are all zero give a result
+ * of that size times 2^-24 or so, not always zero.  sgap_w4_layout puts codes,
+ * scales and zero points into the order in which the product reads them; a
+ * program does that once, when it loads its weights, and may free them
+ * afterwards.
  *   codes    G x N x K/2 bytes, the code of an even k in the low half
  *   scales   G x N x K/group_k elements of 16 bits, of the type that the
  *            products are asked for
