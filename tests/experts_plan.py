@@ -8,6 +8,8 @@ from paper_2209_02882_amd import binding
 
 TILES, FEW, REGISTERS = 0, 1, 2
 Plan = namedtuple("Plan", "way rows columns wide apart short")
+# sizes of groups, K, N: with X beyond 4 GiB these take every tile that such an X is multiplied by
+BEYOND_4_GIB = [([200, 0, 360], 136, 4_104), ([3_000, 1, 2_500], 1_032, 4_096), ([512, 300, 0, 700, 1_100, 5, 900, 579], 136, 1_032)]
 DTYPES = {torch.float32: binding.SGAP_F32, torch.float16: binding.SGAP_F16, torch.bfloat16: binding.SGAP_BF16}
 
 

@@ -4,7 +4,7 @@ import ctypes
 import pytest
 import torch
 
-from experts_plan import FEW, REGISTERS, TILES, plan
+from experts_plan import BEYOND_4_GIB, DTYPES, FEW, REGISTERS, TILES, plan
 from paper_2209_02882_amd import binding
 
 F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
@@ -62,3 +62,19 @@ def test_bad_arguments():
     for change in (dict(G=0), dict(R=-1), dict(dtype=3), dict(ldx=7), dict(ldy=7), dict(layout=2), dict(units=0), dict(plan=None),
                    dict(K=2**31 - 1, ldx=2**31)):
         assert ask(*{**args, **change}.values()) == binding.SGAP_ERR_INVALID_ARG
+
+
+def test_sizes_that_take_every_tile_beyond_4_gib():
+    seen = set()
+    for sizes, K, N in BEYOND_4_GIB:
+        for dtype in DTYPES:
+            for layout in ("nk", "kn"):
+                for gradient in (False, True):
+                    p = plan(len(sizes), sum(sizes), K, N, dtype, layout, gradient, ldx=2**16 + 8, x_rows=36_000)
+                    if p.way == TILES:
+                        assert p.wide
+                        seen.add((dtype, layout, gradient, p.rows))
+    want = {(dtype, layout, False, rows) for dtype in DTYPES for layout in ("nk", "kn") for rows in (64, 128)}
+    want |= {(dtype, layout, True, 128) for dtype in DTYPES for layout in ("nk", "kn")}
+    want |= {(dtype, layout, gradient, 256) for dtype in (F16, BF16) for layout in ("nk", "kn") for gradient in (False, True)}
+    assert seen == want
