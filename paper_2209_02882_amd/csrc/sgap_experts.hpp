@@ -165,7 +165,7 @@ inline hipError_t launch_parts(int64_t workgroups, int threads, F&& launch)
     return hipSuccess;
 }
 
-int64_t route_workspace_bytes(int64_t T, int64_t E, int64_t k);
+int64_t route_workspace_bytes(int64_t T, int64_t E);
 hipError_t launch_route(const RouteArgs& a, hipStream_t s);
 hipError_t launch_route_grad(const RouteGradArgs& a, hipStream_t s);
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s);

@@ -65,7 +65,7 @@ extern "C" {
 int64_t sgap_route_topk_workspace_size(int64_t T, int64_t E, int64_t k)
 {
     if (check_route(T, E, k) != SGAP_OK) return -1;
-    return sgap::route_workspace_bytes(T, E, k);
+    return sgap::route_workspace_bytes(T, E);
 }
 
 int sgap_route_topk(int64_t T, int64_t E, int64_t k, int dtype, const void* logits, int64_t ld_logits, int renormalise,
@@ -78,7 +78,7 @@ int sgap_route_topk(int64_t T, int64_t E, int64_t k, int dtype, const void* logi
     if (ld_logits < E) return invalid("ld_logits is less than a row");
     if (!offsets) return invalid("offsets must not be null");
     if (T > 0 && (!logits || !gates || !experts || !slot || !order)) return invalid("logits and the results must not be null");
-    const int64_t need = sgap::route_workspace_bytes(T, E, k);
+    const int64_t need = sgap::route_workspace_bytes(T, E);
     if (need > 0 && (!workspace || workspace_bytes < need))
         return invalid("the workspace is smaller than sgap_route_topk_workspace_size says");
     if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 15)) return invalid("the workspace must be 16-byte aligned");

@@ -27,7 +27,9 @@ constexpr int kFewThreads = 256;     // a few tokens: a start and barriers that 
 constexpr int kGradThreads = 256;
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxChosen = 16;
-constexpr int kBlockPairs = 1024;  // pairs of a block at most
+constexpr int kBlockRows = 64;     // tokens of a block: a pass of its groups of sixteen lanes
+constexpr int kBlockPairs = 1024;  // pairs of a block at most, one to a thread
+static_assert(kBlockRows * kMaxChosen <= kBlockPairs && kBlockPairs <= kRouteThreads, "");
 
 // Ordered like the floats: NaN above everything (as a sort has it), -infinity, which is never chosen, 0.  -0 is +0.
 __device__ __forceinline__ uint32_t order_key(float x)
@@ -291,13 +293,12 @@ __global__ __launch_bounds__(THREADS) void route_few_kernel(RouteArgs a)
 // More tokens: the choice, with the blocks' counts by expert (count[e * stride + b]) and the pairs' ranks within their
 // block (in slot) ...
 template <typename T, int LANES, int V>
-__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, int rows_per_block, uint16_t* count, int stride,
-                                                                     int64_t block0)
+__global__ __launch_bounds__(kRouteThreads) void route_choose_kernel(RouteArgs a, uint16_t* count, int stride, int64_t block0)
 {
     extern __shared__ __align__(16) char lds[];
     const RouteShared s = route_shared(lds);
-    const int64_t block = block0 + blockIdx.x, row0 = block * rows_per_block;
-    const int rows = (int)min((int64_t)rows_per_block, a.T - row0);
+    const int64_t block = block0 + blockIdx.x, row0 = block * kBlockRows;
+    const int rows = (int)min((int64_t)kBlockRows, a.T - row0);
     const int pairs = rows * a.k, p = my_pair();
     choose_rows<T, LANES, V, kRouteThreads>(a, s, row0, rows);
     __syncthreads();
@@ -331,7 +332,7 @@ __global__ __launch_bounds__(256) void route_scan_kernel(const uint16_t* count, 
 // ... and every pair into its place.  SUM: sixteen lanes sum up the counts of an expert, eight to a load: those of the
 // blocks before this one, and all of them.
 template <bool SUM>
-__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a, int rows_per_block, const uint16_t* count,
+__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a, const uint16_t* count,
                                                                     const int32_t* summed, const int32_t* total, int blocks, int stride,
                                                                     int64_t block0)
 {
@@ -369,8 +370,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(RouteArgs a,
     block_offsets<kRouteThreads>(all, start, a.E, wave_total);
     if (mine == 0)
         for (int e = threadIdx.x; e <= a.E; e += kRouteThreads) a.offsets[e] = start[e];
-    const int64_t p = (int64_t)mine * rows_per_block * a.k + threadIdx.x;
-    if ((int)threadIdx.x >= rows_per_block * a.k || p >= a.T * a.k) return;
+    const int64_t p = (int64_t)mine * kBlockRows * a.k + threadIdx.x;
+    if ((int)threadIdx.x >= kBlockRows * a.k || p >= a.T * a.k) return;
     const int e = a.experts[p];
     if (e >= 0) {
         const int at = start[e] + before[e] + a.slot[p];
@@ -452,21 +453,15 @@ hipError_t by_type(int dtype, int E, F&& f)
     }
 }
 
-// Rows of a block: 64, a pass of its groups of sixteen lanes; a thread has one pair at most.
-int rows_per_block(int64_t T, int k)
-{
-    const int most = kBlockPairs / k;
-    return most < 64 ? most : 64;
-}
-
 struct RouteFew {
     const RouteArgs& a;
     hipStream_t s;
     template <typename T, int LANES, int V>
     hipError_t operator()() const
     {
-        // a pass of the small block's groups of lanes, and a pair to a thread
-        if (a.T <= kFewThreads / LANES && a.T * a.k <= kFewThreads)
+        // a pass of the small block's groups of lanes: their pairs are one to a thread, as k is no more than LANES
+        static_assert(LANES >= kMaxChosen, "");
+        if (a.T <= kFewThreads / LANES)
             route_few_kernel<T, LANES, V, kFewThreads><<<1, kFewThreads, route_shared_bytes(kFewThreads, a.E), s>>>(a);
         else
             route_few_kernel<T, LANES, V, kRouteThreads><<<1, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(a);
@@ -476,15 +471,14 @@ struct RouteFew {
 
 // Where the counts lie in the workspace.
 struct RouteCounts {
-    int rows, blocks, stride;        // rows of a block; blocks, and as many in whole loads
+    int blocks, stride;              // blocks, and as many in whole loads
     int64_t summed_at, total_at, bytes;
     bool each;                       // each block sums them up for itself: no more than 128 KB of them
 };
-RouteCounts route_counts(int64_t T, int64_t E, int k)
+RouteCounts route_counts(int64_t T, int64_t E)
 {
     RouteCounts c;
-    c.rows = rows_per_block(T, k);
-    c.blocks = (int)((T + c.rows - 1) / c.rows);
+    c.blocks = (int)((T + kBlockRows - 1) / kBlockRows);
     c.stride = (c.blocks + 7) / 8 * 8;
     c.each = E * c.stride <= 65536;
     c.summed_at = (E * c.stride * 2 + 15) / 16 * 16;
@@ -502,7 +496,7 @@ struct RouteChoose {
     {
         return launch_parts(c.blocks, kRouteThreads, [&](unsigned grid, int64_t block0) {
             route_choose_kernel<T, LANES, V><<<grid, kRouteThreads, route_shared_bytes(kRouteThreads, a.E), s>>>(
-                a, c.rows, static_cast<uint16_t*>(a.workspace), c.stride, block0);
+                a, static_cast<uint16_t*>(a.workspace), c.stride, block0);
         });
     }
 };
@@ -520,27 +514,27 @@ struct RouteGrad {
 };
 
 // One workgroup for all tokens: as many as a block of more has.
-bool route_in_one(int64_t T, int k) { return T <= 64 && T * k <= kBlockPairs; }
+bool route_in_one(int64_t T) { return T <= kBlockRows; }
 
 }  // namespace
 
-int64_t route_workspace_bytes(int64_t T, int64_t E, int64_t k)
+int64_t route_workspace_bytes(int64_t T, int64_t E)
 {
-    return route_in_one(T, (int)k) ? 0 : route_counts(T, E, (int)k).bytes;
+    return route_in_one(T) ? 0 : route_counts(T, E).bytes;
 }
 
 hipError_t launch_route(const RouteArgs& a, hipStream_t s)
 {
-    if (route_in_one(a.T, a.k)) return by_type(a.dtype, a.E, RouteFew{a, s});
-    const RouteCounts c = route_counts(a.T, a.E, a.k);
+    if (route_in_one(a.T)) return by_type(a.dtype, a.E, RouteFew{a, s});
+    const RouteCounts c = route_counts(a.T, a.E);
     char* const at = static_cast<char*>(a.workspace);
     const uint16_t* const count = reinterpret_cast<const uint16_t*>(at);
     int32_t *summed = reinterpret_cast<int32_t*>(at + c.summed_at), *total = reinterpret_cast<int32_t*>(at + c.total_at);
     if (const hipError_t err = by_type(a.dtype, a.E, RouteChoose{a, c, s})) return err;
     if (!c.each) route_scan_kernel<<<(a.E + 3) / 4, 256, 0, s>>>(count, summed, total, c.blocks, c.stride, a.E);
     return launch_parts(c.blocks, kRouteThreads, [&](unsigned grid, int64_t block0) {
-        if (c.each) route_place_kernel<true><<<grid, kRouteThreads, 0, s>>>(a, c.rows, count, nullptr, nullptr, c.blocks, c.stride, block0);
-        else route_place_kernel<false><<<grid, kRouteThreads, 0, s>>>(a, c.rows, count, summed, total, c.blocks, c.stride, block0);
+        if (c.each) route_place_kernel<true><<<grid, kRouteThreads, 0, s>>>(a, count, nullptr, nullptr, c.blocks, c.stride, block0);
+        else route_place_kernel<false><<<grid, kRouteThreads, 0, s>>>(a, count, summed, total, c.blocks, c.stride, block0);
     });
 }
 
