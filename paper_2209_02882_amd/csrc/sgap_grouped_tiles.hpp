@@ -136,6 +136,7 @@ __device__ __forceinline__ void multiply_tiles_as(uint32_t lds, int tiles, F&& l
     constexpr int kLoads = L::kRounds + R::kRounds;
     using frag = decltype(L::fragment(0u, 0, 0));
     frag fl[2][MI], fr[2][NJ];
+    Runs<L::P == 4, MI, NJ, 512 / L::kInner, true> runs;  // floats: only where sums are not finite, and time counts less
     const uint32_t lbase = lds + L::lane_base(l0), rbase = lds + L::kBytes + R::lane_base(r0);
     uint32_t lb, rb;
     const auto at = [&](uint32_t stage) {
@@ -190,6 +191,7 @@ __device__ __forceinline__ void multiply_tiles_as(uint32_t lds, int tiles, F&& l
 #pragma unroll
             for (int i = j * kLoads / NJ; i < (j + 1) * kLoads / NJ; ++i) load(t + 2, lds + stage, i);
         });
+        runs.end_of(t, acc);
     }
     for (; t < tiles; ++t) {
         const uint32_t stage = (t & 1) * kStage;
@@ -198,7 +200,9 @@ __device__ __forceinline__ void multiply_tiles_as(uint32_t lds, int tiles, F&& l
         meet(t + 1);
         at(kStage - stage);
         half(1, [](int) {});  // behind the last tile the fragments that are read are not used
+        runs.end_of(t, acc);
     }
+    runs.finish(acc);
 }
 template <typename L, typename R, int MI, int NJ, typename F, typename M>
 __device__ __forceinline__ void multiply_tiles(char* shared, int tiles, F&& load, M&& mend, int l0, int r0, bool active,

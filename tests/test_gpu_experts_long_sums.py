@@ -84,3 +84,28 @@ def test_many_rows_by_long_weights(R, K, N, layout):
 @pytest.mark.parametrize("R,K,N", [(16_384, 2_048, 2_048), (65_536, 2_048, 2_048), (150_001, 1_032, 2_048)])
 def test_gradient_of_many_weights_from_many_rows(R, K, N, layout):
     assert gradient_off(R, K, N, layout) <= by_parts(R)
+
+
+# a tile with a sum that is not finite goes by the instruction for floats: its other sums are no worse for it
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+def test_long_sums_beside_one_that_is_infinite(layout):
+    R, K, N = 2_048, 65_536, 2_048
+    X, W = normal(1, R, K), normal(2, *((1, N, K) if layout == "nk" else (1, K, N)))
+    X[5, 7] = float("inf")
+    Y = torch.empty(R, N, device="cuda")
+    binding.sgap_grouped_mm(1, R, K, N, None, X, W, Y, layout)
+    w = W[0].t().contiguous() if layout == "nk" else W[0]
+    assert torch.isinf(Y[5]).all()
+    assert off(Y[6:70], torch.mm(X[6:70].double(), w.double())) <= by_runs(K, 1)
+
+
+@pytest.mark.parametrize("layout", ["nk", "kn"])
+def test_long_gradients_beside_one_that_is_infinite(layout):
+    R, K, N = 65_536, 2_048, 2_048
+    X, dY = normal(1, R, K), normal(2, R, N)
+    dY[100, 5] = float("inf")
+    dW = torch.empty((1, N, K) if layout == "nk" else (1, K, N), device="cuda")
+    binding.sgap_grouped_mm_wgrad(1, R, K, N, None, X, dY, dW, layout)
+    got = dW[0] if layout == "nk" else dW[0].t()
+    assert torch.isinf(got[5]).all()
+    assert off(got[6:70], torch.mm(dY[:, 6:70].double().t().contiguous(), X.double())) <= by_runs(R, 1)
