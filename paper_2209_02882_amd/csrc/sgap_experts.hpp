@@ -151,8 +151,8 @@ struct CombineArgs {
     float* __restrict__ dgates;
 };
 
-// A launch has fewer than 2^32 threads: more workgroups go out as several launches, launch(workgroups, block0), in which
-// workgroup b is number block0 + b of all.  (Parts are multiples of 256 workgroups, so that eight dies have whole turns.)
+// A launch has fewer than 2^32 threads (a larger grid is cut off to what is left over 2^32, mostly without an error): more
+// workgroups go out as several launches, launch(workgroups, block0), in which workgroup b is number block0 + b of all.  (Parts are multiples of 256 workgroups, so that eight dies have whole turns.)
 template <typename F>
 inline hipError_t launch_parts(int64_t workgroups, int threads, F&& launch)
 {

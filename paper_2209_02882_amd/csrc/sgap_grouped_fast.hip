@@ -7,7 +7,7 @@
 // rows are many: what is lost to them is the reads of LDS between them, a tile's first wait and its store, and the part of
 // every group's last tile that has no rows.  16 groups, 16,384 rows, 4,096 by 2,048, bf16 (275 GF each): the product 315 us
 // (870 TF/s), the gradient of X 313 us, of W 350 us; one group of 8,192 rows, 4,096 by 8,192: 1,310 TF/s, where the library's
-// product reaches 1,540.  Floats, 4,096 rows in 8 groups, 1,024 by 1,024, in parts of 16 bits: 90, 104 and 72 us, 8.6 GF each.
+// product reaches 1,540.  Floats, 4,096 rows in 8 groups, 1,024 by 1,024, in parts of 16 bits: 90, 91 and 75 us, 8.6 GF each.
 // Bound by the weights' bytes where rows are few: 16 experts for 32 rows, 2,048 by 4,096, bf16: 47.6 us, 5.0 TB/s.
 #include <algorithm>
 #include <type_traits>
@@ -351,8 +351,9 @@ GroupedPlan plan_grouped_fast(const GroupedArgs& a, int dtype, bool gradient)
     const double small = turns(tiles(64, 128), a.compute_units, 64, 128, half ? 0.55 : 0.8);
     if (half && large <= std::min(middle, small)) p.rows = p.columns = 256;
     else if (middle > small) p.rows = 64;
-    // (a row of 4,096 bytes or a multiple: 16 experts for 32 rows, 2,048 x 4,096 bf16, 56.7 us together and 47.7 apart; rows
-    // of 2,000 bytes 29.2 and 32.5)
+    // (16 experts for 32 rows, 4,096 columns, bf16, together and apart: rows of 4,096 bytes 66.4 us, 54.1, 8,192 122.6, 88.3,
+    // 12,288 146.8, 133.3, 16,384 189.0, 176.0; floats, 8,192 columns, 150, 127, 241, 237, 359, 342, 462, 456.  Rows of 512 to 2,560
+    // bytes, 4,112, 5,120, 6,144, 8,208 and 10,240: within 6 % of one another, either way.)
     p.apart = !a.weights_kn && a.R <= p.rows * a.G && a.K * size % 4096 == 0;
     return p;
 }

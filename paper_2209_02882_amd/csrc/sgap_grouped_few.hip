@@ -430,9 +430,9 @@ hipError_t wgrad_by_plan(const GroupedArgs& a, const GroupedPlan& p, hipStream_t
 //           63, 52; 16 experts for 32 rows, 2,048 x 4,096 (512) 47, 60, K x N 50, 57;
 //           8 groups, 512 rows, 2,048 x 1,024 (96) 32.6, 24.7; 1,024 rows by 1,024 (128) 42.4, 71; K x N 42.7, 41.1, 64 groups,
 //           2,048 rows, 1,024 x 256 (128) 18.7, 12.6, 16 groups, 1,024 rows, 1,024 x 1,024 (192) 19.5, 22.6
-//   floats  64 groups of 4, 1,024 x 2,048 (1,024) 132, 132, K x N 135, 110; one group, 4,096: 1,024 rows by 1,024 (128) 172, 162;
-//           8 groups, 1,024 rows, 2,048 x 1,024 (160) 90, 98, K x N 94, 68; 16 groups, 1,024 rows, 1,024 x 1,024 (192) K x N
-//           50.5, 42.7; one group, 2,048 rows by 1,024 (256) K x N 176, 219
+//   floats  64 groups of 4, 1,024 x 2,048 (1,024) 131, 139, K x N 131, 111; one group, 4,096: 1,024 rows by 1,024 (128) 174, 168;
+//           8 groups, 1,024 rows, 2,048 x 1,024 (160) 81, 96, K x N 83, 66; 16 groups, 1,024 rows, 1,024 x 1,024 (192) K x N
+//           44.0, 41.7; one group, 2,048 rows by 1,024 (256) K x N 170, 237
 bool few_rows_apply(const GroupedArgs& a, int dtype)
 {
     if (!grouped_fast_applies(a, dtype)) return false;
@@ -447,8 +447,8 @@ bool few_rows_apply(const GroupedArgs& a, int dtype)
 //   bf16    8,192 rows by 256 x 256 (4) 143, 37; 1,024 x 1,024 (64) 146, 52; 512 rows by the same 14.2, 8.9, 128 rows 8.0, 7.4;
 //           16 groups of 64 rows, 256 x 256 (64) 7.4, 7.3; 8,192 rows by 2,048 x 1,024 (128) 146, 97; 8 groups of 1,024, 512 x 512
 //           (128) 23.1, 24.0; 1,024 rows by 2,048 x 2,048 (256) 25, 42
-//   floats  8,192 rows by 256 x 256 512, 67; 1,024 x 1,024 520, 177; 2,048 x 1,024 519, 322; 8 groups of 1,024, 512 x 512 71, 56, of
-//           128 15.1, 16.8; 1,024 rows by 2,048 x 2,048 73, 98
+//   floats  8,192 rows by 256 x 256 504, 66; 1,024 x 1,024 519, 195; 2,048 x 1,024 526, 368; 8 groups of 1,024, 512 x 512 70, 55, of
+//           128 14.4, 15.5; 1,024 rows by 2,048 x 2,048 76, 101
 bool few_weights_apply(const GroupedArgs& a, int dtype)
 {
     if (!grouped_fast_applies(a, dtype)) return false;
@@ -468,7 +468,7 @@ GroupedPlan plan_grouped_few(const GroupedArgs& a, int dtype, bool gradient)
     GroupedPlan p = {GroupedPlan::kFew, 16, 16, false, false, false};
     if (gradient) {
         // 32 x 32 weights to a workgroup while there is no more than one to a compute unit, then 64 x 64: 8,192 rows, bf16, by
-        // 512 x 512 (256 of the small) 40 us and 48, 1,024 x 1,024 153 and 52; floats 74 and 163, 286 and 177
+        // 512 x 512 (256 of the small) 40 us and 48, 1,024 x 1,024 153 and 52; floats 70 and 175, 266 and 195
         p.rows = p.columns = a.G * ((a.N + 31) / 32) * ((a.K + 31) / 32) <= a.compute_units ? 32 : 64;
         return p;
     }
