@@ -1,8 +1,8 @@
 """Binding of libsgap.so: argument marshalling only.
 
 sgap_spmm_csr_ex, sgap_spmm_csr_cfg, sgap_sddmm_csr, sgap_sddmm_csr_windows, sgap_ttm_csf, sgap_mttkrp_csf_ex and the
-calls of a mixture of experts (sgap_route_*, sgap_grouped_*) go through a small native module (csrc/sgap_python.cpp), which reads the tensors and calls the library in a few hundred
-nanoseconds; what it does not take (another type, a wrong length, a number that is no int) goes through ctypes and the
+calls of a mixture of experts (sgap_route_*, sgap_grouped_*, sgap_embed*, sgap_f8_*) go through a small native module
+(csrc/sgap_python.cpp), which reads the tensors and calls the library in a few hundred nanoseconds; what it does not take (another type, a wrong length, a number that is no int) goes through ctypes and the
 checks below, which say what is wrong.  The other calls, and all of them where that module has not been built, go
 through ctypes: about 8 us of host time each.
 
@@ -69,6 +69,15 @@ EXPORTS = {
     "sgap_w4_layout_size": (_i64, [_i64, _i64, _i64, _i64, _int]),
     "sgap_w4_layout": (_int, [_i64, _i64, _i64, _i64, _p, _p, _p, _p, _i64, _p]),
     "sgap_grouped_mm_w4": (_int, [_i64, _i64, _i64, _i64, _int, _i64, _int, _p, _p, _i64, _i64, _p, _i64, _p, _i64, _p, _i64, _p]),
+    "sgap_route_balance_workspace_size": (_i64, [_i64, _i64, _i64, _i64]),
+    "sgap_route_balance": (_int, [_i64, _i64, _i64, _i64, _int, _p, _i64, _p, _p, _p, _p, _p, _p, _i64, _p]),
+    "sgap_route_balance_grad": (_int, [_i64, _i64, _i64, _i64, _int, _p, _i64, _p, _p, _p, _p, _p, _int, _p, _i64, _p]),
+    "sgap_embed": (_int, [_i64, _i64, _i64, _int, _p, _p, _i64, ctypes.c_float, _p, _i64, _p]),
+    "sgap_embed_grad_workspace_size": (_i64, [_i64, _i64, _i64]),
+    "sgap_embed_grad": (_int, [_i64, _i64, _i64, _int, _p, _p, _i64, ctypes.c_float, _int, _int, _p, _i64, _p, _i64, _p]),
+    "sgap_f8_rows": (_int, [_i64, _i64, _int, _p, _i64, _p, _p, _p]),
+    "sgap_f8_weights": (_int, [_i64, _i64, _i64, _int, _p, _p, _p, _p, _p, _p]),
+    "sgap_grouped_mm_f8": (_int, [_i64, _i64, _i64, _i64, _int, _p, _p, _p, _i64, _p, _i64, _p, _p, _p, _i64, _p]),
     "sgap_status_string": (ctypes.c_char_p, [_int]),
     "sgap_last_error": (ctypes.c_char_p, []),
     "sgap_version": (_int, []),
@@ -788,3 +797,159 @@ def sgap_grouped_mm_w4(G, R, K, N, group_k, offsets, X, weights, Y, zeros=False,
     ws, ws_bytes = _bytes(weights, "weights")
     y, ldy = _rows(Y, X.dtype, R, N, "Y")
     _check(load().sgap_grouped_mm_w4(G, R, K, N, dtype, int(group_k), zeros, *args, ws, ws_bytes, y, ldy, _stream_ptr(stream)))
+
+
+def sgap_route_balance_workspace_size(T, E, k, S) -> int:
+    size = load().sgap_route_balance_workspace_size(int(T), int(E), int(k), int(S))
+    if size < 0:
+        raise SgapError(SGAP_ERR_INVALID_ARG, load().sgap_last_error().decode())
+    return size
+
+
+def sgap_route_balance(T, E, k, S, logits, experts, segments, loss, counts, rows, workspace=None, stream=None) -> None:
+    """The balance loss over S sequences of tokens (segments None: one of all), each expert's pairs and the tokens that chose, from
+    a router's logits and choice (see include/sgap.h).  `workspace`: a CUDA uint8 tensor of sgap_route_balance_workspace_size bytes."""
+    st = (_native or _load_native()).route_balance(T, E, k, S, logits, experts, segments, loss, counts, rows, workspace, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(logits, "logits")
+    ptr, ld = _rows(logits, logits.dtype, T, E, "logits")
+    ws, ws_bytes = _bytes(workspace, "workspace")
+    _check(load().sgap_route_balance(
+        T, E, k, S, dtype, ptr, ld, _flat(experts, torch.int32, T * k, "experts"),
+        None if segments is None else _flat(segments, torch.int32, S + 1, "segments"), _flat(loss, torch.float32, 1, "loss"),
+        _flat(counts, torch.int32, S * E, "counts"), _flat(rows, torch.int32, S, "rows"), ws, ws_bytes, _stream_ptr(stream)))
+
+
+def sgap_route_balance_grad(T, E, k, S, logits, experts, segments, counts, rows, dloss, dlogits, accumulate=False, stream=None) -> None:
+    """dlogits from the gradient of the balance loss, or added to what is there (see include/sgap.h)."""
+    accumulate = int(bool(accumulate))
+    st = (_native or _load_native()).route_balance_grad(T, E, k, S, logits, experts, segments, counts, rows, dloss, dlogits, accumulate,
+                                                        stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(logits, "logits")
+    ptr, ld = _rows(logits, logits.dtype, T, E, "logits")
+    dptr, ldd = _rows(dlogits, logits.dtype, T, E, "dlogits")
+    _check(load().sgap_route_balance_grad(
+        T, E, k, S, dtype, ptr, ld, _flat(experts, torch.int32, T * k, "experts"),
+        None if segments is None else _flat(segments, torch.int32, S + 1, "segments"), _flat(counts, torch.int32, S * E, "counts"),
+        _flat(rows, torch.int32, S, "rows"), _flat(dloss, torch.float32, 1, "dloss"), accumulate, dptr, ldd, _stream_ptr(stream)))
+
+
+def sgap_embed(T, V, D, ids, weights, out, scale=1.0, stream=None) -> None:
+    """out[t] = scale * weights[ids[t]]; an id outside 0 .. V gives zeros (see include/sgap.h)."""
+    scale = float(scale)
+    st = (_native or _load_native()).embed(T, V, D, ids, weights, out, scale, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(weights, "weights")
+    w, ldw = _rows(weights, weights.dtype, V, D, "weights")
+    o, ldo = _rows(out, weights.dtype, T, D, "out")
+    _check(load().sgap_embed(T, V, D, dtype, _flat(ids, torch.int32, T, "ids"), w, ldw, scale, o, ldo, _stream_ptr(stream)))
+
+
+def sgap_embed_grad_workspace_size(T, V, D) -> int:
+    size = load().sgap_embed_grad_workspace_size(int(T), int(V), int(D))
+    if size < 0:
+        raise SgapError(SGAP_ERR_INVALID_ARG, load().sgap_last_error().decode())
+    return size
+
+
+def sgap_embed_grad(T, V, D, ids, dout, dweights, scale=1.0, accumulate=False, workspace=None, stream=None) -> None:
+    """dweights[v] = scale * the sum of dout[t] over the tokens with ids[t] = v, or that added to what is there; dweights has
+    dout's type or float32 (see include/sgap.h).  `workspace`: a CUDA uint8 tensor of sgap_embed_grad_workspace_size bytes."""
+    scale, accumulate = float(scale), int(bool(accumulate))
+    st = (_native or _load_native()).embed_grad(T, V, D, ids, dout, dweights, scale, accumulate, workspace, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype, grad_dtype = _element_type(dout, "dout"), _element_type(dweights, "dweights")
+    d, ldd = _rows(dout, dout.dtype, T, D, "dout")
+    w, ldw = _rows(dweights, dweights.dtype, V, D, "dweights")
+    ws, ws_bytes = _bytes(workspace, "workspace")
+    _check(load().sgap_embed_grad(T, V, D, dtype, _flat(ids, torch.int32, T, "ids"), d, ldd, scale, accumulate, grad_dtype, w, ldw, ws,
+                                  ws_bytes, _stream_ptr(stream)))
+
+
+SGAP_F8_BLOCK = 128
+SGAP_MAX_SEQUENCES = 65536
+
+
+def _f8_blocks(n):
+    return (n + SGAP_F8_BLOCK - 1) // SGAP_F8_BLOCK
+
+
+def sgap_f8_rows(R, K, X, codes, scales, stream=None) -> None:
+    """The rows of X in 8 bits: codes (torch.float8_e4m3fn, R rows of 128 * ceil(K / 128)) and scales (float32, R x ceil(K / 128))
+    (see include/sgap.h)."""
+    st = (_native or _load_native()).f8_rows(R, K, X, codes, scales, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(X, "X")
+    ptr, ld = _rows(X, X.dtype, R, K, "X")
+    blocks = _f8_blocks(K)
+    _check(load().sgap_f8_rows(R, K, dtype, ptr, ld, _flat(codes, torch.float8_e4m3fn, R * blocks * SGAP_F8_BLOCK, "codes"),
+                               _flat(scales, torch.float32, R * blocks, "scales"), _stream_ptr(stream)))
+
+
+def sgap_f8_weights(G, K, N, W, codes, scales, codes_t=None, scales_t=None, stream=None) -> None:
+    """Weights G x N x K in 8 bits: codes (torch.float8_e4m3fn, G x N rows of 128 * ceil(K / 128)), scales (float32, G x ceil(N /
+    128) x ceil(K / 128)), and, if they are given, the same of the transposed matrices (see include/sgap.h)."""
+    st = (_native or _load_native()).f8_weights(G, K, N, W, codes, scales, codes_t, scales_t, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(W, "W")
+    nb, kb = _f8_blocks(N), _f8_blocks(K)
+    _check(load().sgap_f8_weights(
+        G, K, N, dtype, _flat(W, W.dtype, G * N * K, "W"), _flat(codes, torch.float8_e4m3fn, G * N * kb * SGAP_F8_BLOCK, "codes"),
+        _flat(scales, torch.float32, G * nb * kb, "scales"),
+        None if codes_t is None else _flat(codes_t, torch.float8_e4m3fn, G * K * nb * SGAP_F8_BLOCK, "codes_t"),
+        None if scales_t is None else _flat(scales_t, torch.float32, G * nb * kb, "scales_t"), _stream_ptr(stream)))
+
+
+def sgap_grouped_mm_f8(G, R, K, N, offsets, X, x_scales, W, w_scales, Y, src=None, src_div=1, stream=None) -> None:
+    """sgap_grouped_mm with rows and weights (G x N x K) in 8 bits, as sgap_f8_rows and sgap_f8_weights put them; Y is float32,
+    float16 or bfloat16 (see include/sgap.h)."""
+    st = (_native or _load_native()).grouped_mm_f8(G, R, K, N, offsets, X, x_scales, W, w_scales, Y, src, src_div, stream)
+    if st == 0:
+        return
+    if st > 0:
+        _check(st)
+    import torch
+
+    dtype = _element_type(Y, "Y")
+    nb, kb = _f8_blocks(N), _f8_blocks(K)
+    if not isinstance(X, torch.Tensor) or X.dim() != 2:
+        raise ValueError("X must be a matrix of codes")
+    x_rows = X.shape[0]
+    y, ldy = _rows(Y, Y.dtype, R, N, "Y")
+    _check(load().sgap_grouped_mm_f8(
+        G, R, K, N, dtype, None if offsets is None else _flat(offsets, torch.int32, G + 1, "offsets"),
+        _flat(X, torch.float8_e4m3fn, x_rows * kb * SGAP_F8_BLOCK, "X"), _flat(x_scales, torch.float32, x_rows * kb, "x_scales"), x_rows,
+        None if src is None else _flat(src, torch.int32, R, "src"), int(src_div),
+        _flat(W, torch.float8_e4m3fn, G * N * kb * SGAP_F8_BLOCK, "W"), _flat(w_scales, torch.float32, G * nb * kb, "w_scales"), y, ldy,
+        _stream_ptr(stream)))

@@ -15,6 +15,7 @@ SOURCES = [
     "sgap_nnz_serial.hip", "sgap_nnz_serial_lc1_2.hip", "sgap_nnz_serial_lc4_8.hip",
     "sgap_nnz_serial_lc16_32.hip", "sgap_nnz_serial_lc64.hip",
     "sgap_experts_api.hip", "sgap_route.hip", "sgap_combine.hip", "sgap_grouped_general.hip", "sgap_grouped_fast.hip", "sgap_grouped_few.hip", "sgap_w4.hip",
+    "sgap_tokens_api.hip", "sgap_embed.hip", "sgap_balance.hip", "sgap_f8.hip", "sgap_grouped_f8.hip",
 ]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -7,46 +7,13 @@
 //
 // 8,192 tokens of 4 rows of 2,048 columns, bf16: 26.3 us, 6.4 TB/s of the 168 MB that the call names (part of Z comes out of
 // the last-level cache); the gradient 57 us, 5.3 TB/s of its 302 MB.  A copy reaches 5.6 TB/s.
-#include "sgap_experts.hpp"
+#include "sgap_columns.hpp"
 
 namespace sgap {
 
 namespace {
 
 constexpr int kCombineThreads = 256;
-
-// the first column of the piece that starts at column c < D of a row of at least a piece's columns
-template <int VEC>
-__device__ __forceinline__ int64_t piece_first(int64_t c, int64_t D)
-{
-    return VEC == 1 || c + VEC <= D ? c : D - VEC;
-}
-
-template <typename T, int VEC>
-struct Columns {
-    float v[VEC];
-    __device__ __forceinline__ void load(const T* p)
-    {
-        if constexpr (VEC == 1) {
-            v[0] = (float)*p;
-        } else {
-            const piece_t<T> x = load_piece(p);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = (float)x[i];
-        }
-    }
-    __device__ __forceinline__ void store(T* p) const
-    {
-        if constexpr (VEC == 1) {
-            *p = (T)v[0];
-        } else {
-            piece_t<T> x;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = (T)v[i];
-            store_piece(p, x);
-        }
-    }
-};
 
 // A work item: a token and 64 * VEC of its columns.  Sums in 32 bits, rounded once.
 template <typename T, int VEC, int KMAX>

@@ -57,6 +57,13 @@ struct Call {
     }
     int32_t* ints(int n, int64_t count) { return static_cast<int32_t*>(data(n, at::kInt, count)); }
     float* floats(int n, int64_t count) { return static_cast<float*>(data(n, at::kFloat, count)); }
+    uint8_t* codes(int n, int64_t count) { return static_cast<uint8_t*>(data(n, at::kFloat8_e4m3fn, count)); }
+    // a Python float
+    float real(int n)
+    {
+        if (!PyFloat_CheckExact(arg[n])) return ok = false, 0.0f;
+        return (float)PyFloat_AS_DOUBLE(arg[n]);
+    }
     int64_t length(int n)
     {
         const at::Tensor* t = tensor(n);
@@ -451,6 +458,160 @@ PyObject* grouped_mm_w4(PyObject*, PyObject* const* arg, Py_ssize_t n)
     });
 }
 
+// T, E, k, S, logits, experts, segments or None, loss, counts, rows, workspace, stream
+PyObject* route_balance(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 12) return status(kNotTaken);
+    const int64_t T = c.number(0), E = c.number(1), k = c.number(2), S = c.number(3);
+    if (!sizes_ok(c, {T, E, k, S})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 4);
+    const Rows logits = rows_of(c, 4, type, T, E);
+    const int32_t *experts = c.ints(5, T * k), *segments = arg[6] == Py_None ? nullptr : c.ints(6, S + 1);
+    float* loss = c.floats(7, 1);
+    int32_t *counts = c.ints(8, S * E), *rows = c.ints(9, S);
+    int64_t bytes = 0;
+    void* ws = c.whole_workspace(10, &bytes);
+    void* stream = c.stream(11);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_route_balance(T, E, k, S, element_type(type), logits.data, logits.ld, experts, segments, loss, counts, rows, ws, bytes,
+                                  stream);
+    });
+}
+
+// T, E, k, S, logits, experts, segments or None, counts, rows, dloss, dlogits, accumulate, stream
+PyObject* route_balance_grad(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 13) return status(kNotTaken);
+    const int64_t T = c.number(0), E = c.number(1), k = c.number(2), S = c.number(3);
+    if (!sizes_ok(c, {T, E, k, S})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 4);
+    const Rows logits = rows_of(c, 4, type, T, E), dlogits = rows_of(c, 10, type, T, E);
+    const int32_t *experts = c.ints(5, T * k), *segments = arg[6] == Py_None ? nullptr : c.ints(6, S + 1);
+    const int32_t *counts = c.ints(7, S * E), *rows = c.ints(8, S);
+    const float* dloss = c.floats(9, 1);
+    const int accumulate = c.small(11);
+    void* stream = c.stream(12);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_route_balance_grad(T, E, k, S, element_type(type), logits.data, logits.ld, experts, segments, counts, rows, dloss,
+                                       accumulate, dlogits.data, dlogits.ld, stream);
+    });
+}
+
+// T, V, D, ids, weights, out, scale, stream
+PyObject* embed(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 8) return status(kNotTaken);
+    const int64_t T = c.number(0), V = c.number(1), D = c.number(2);
+    if (!sizes_ok(c, {T, V, D})) return status(kNotTaken);
+    const int32_t* ids = c.ints(3, T);
+    const at::ScalarType type = type_of(c, 4);
+    const Rows weights = rows_of(c, 4, type, V, D), out = rows_of(c, 5, type, T, D);
+    const float scale = c.real(6);
+    void* stream = c.stream(7);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] { return sgap_embed(T, V, D, element_type(type), ids, weights.data, weights.ld, scale, out.data, out.ld, stream); });
+}
+
+// T, V, D, ids, dout, dweights, scale, accumulate, workspace, stream
+PyObject* embed_grad(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 10) return status(kNotTaken);
+    const int64_t T = c.number(0), V = c.number(1), D = c.number(2);
+    if (!sizes_ok(c, {T, V, D})) return status(kNotTaken);
+    const int32_t* ids = c.ints(3, T);
+    const at::ScalarType type = type_of(c, 4), grad_type = type_of(c, 5);
+    const Rows dout = rows_of(c, 4, type, T, D), dweights = rows_of(c, 5, grad_type, V, D);
+    const float scale = c.real(6);
+    const int accumulate = c.small(7);
+    int64_t bytes = 0;
+    void* ws = c.whole_workspace(8, &bytes);
+    void* stream = c.stream(9);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_embed_grad(T, V, D, element_type(type), ids, dout.data, dout.ld, scale, accumulate, element_type(grad_type),
+                               dweights.data, dweights.ld, ws, bytes, stream);
+    });
+}
+
+int64_t f8_blocks(int64_t n) { return (n + SGAP_F8_BLOCK - 1) / SGAP_F8_BLOCK; }
+
+// R, K, X, codes, scales, stream
+PyObject* f8_rows(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 6) return status(kNotTaken);
+    const int64_t R = c.number(0), K = c.number(1);
+    if (!sizes_ok(c, {R, K})) return status(kNotTaken);
+    const at::ScalarType type = type_of(c, 2);
+    const Rows X = rows_of(c, 2, type, R, K);
+    uint8_t* codes = c.codes(3, R * f8_blocks(K) * SGAP_F8_BLOCK);
+    float* scales = c.floats(4, R * f8_blocks(K));
+    void* stream = c.stream(5);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] { return sgap_f8_rows(R, K, element_type(type), X.data, X.ld, codes, scales, stream); });
+}
+
+// what G matrices of N rows of whole blocks of K values have, if that is a number
+bool f8_sizes_ok(Call& c, int64_t G, int64_t N, int64_t K)
+{
+    __int128 bytes = (__int128)G * (N + SGAP_F8_BLOCK) * (f8_blocks(K) + 1) * SGAP_F8_BLOCK;
+    if (bytes > INT64_MAX / 8) c.ok = false;
+    return c.ok;
+}
+
+// G, K, N, W, codes, scales, codes_t or None, scales_t or None, stream
+PyObject* f8_weights(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 9) return status(kNotTaken);
+    const int64_t G = c.number(0), K = c.number(1), N = c.number(2);
+    if (!sizes_ok(c, {G, K, N}) || !f8_sizes_ok(c, G, N, K)) return status(kNotTaken);
+    const int64_t nb = f8_blocks(N), kb = f8_blocks(K);
+    const at::ScalarType type = type_of(c, 3);
+    const void* W = c.data(3, type, G * N * K);
+    uint8_t* codes = c.codes(4, G * N * kb * SGAP_F8_BLOCK);
+    float* scales = c.floats(5, G * nb * kb);
+    uint8_t* codes_t = arg[6] == Py_None ? nullptr : c.codes(6, G * K * nb * SGAP_F8_BLOCK);
+    float* scales_t = arg[7] == Py_None ? nullptr : c.floats(7, G * nb * kb);
+    void* stream = c.stream(8);
+    if (!c.ok || (arg[6] == Py_None) != (arg[7] == Py_None)) return status(kNotTaken);
+    return enqueue([&] { return sgap_f8_weights(G, K, N, element_type(type), W, codes, scales, codes_t, scales_t, stream); });
+}
+
+// G, R, K, N, offsets or None, X, x_scales, W, w_scales, Y, src or None, src_div, stream
+PyObject* grouped_mm_f8(PyObject*, PyObject* const* arg, Py_ssize_t n)
+{
+    Call c{arg};
+    if (n != 13) return status(kNotTaken);
+    const int64_t G = c.number(0), R = c.number(1), K = c.number(2), N = c.number(3);
+    if (!sizes_ok(c, {G, R, K, N}) || !f8_sizes_ok(c, G, N, K)) return status(kNotTaken);
+    const int64_t nb = f8_blocks(N), kb = f8_blocks(K);
+    const int32_t* offsets = arg[4] == Py_None ? nullptr : c.ints(4, G + 1);
+    const at::Tensor* x = c.tensor(5);
+    if (!x || x->dim() != 2) return status(kNotTaken);
+    const int64_t x_rows = x->size(0);
+    const uint8_t* X = c.codes(5, x_rows * kb * SGAP_F8_BLOCK);
+    const float* x_scales = c.floats(6, x_rows * kb);
+    const uint8_t* W = c.codes(7, G * N * kb * SGAP_F8_BLOCK);
+    const float* w_scales = c.floats(8, G * nb * kb);
+    const at::ScalarType type = type_of(c, 9);
+    const Rows Y = rows_of(c, 9, type, R, N);
+    const int32_t* src = arg[10] == Py_None ? nullptr : c.ints(10, R);
+    const int64_t src_div = c.number(11);
+    void* stream = c.stream(12);
+    if (!c.ok) return status(kNotTaken);
+    return enqueue([&] {
+        return sgap_grouped_mm_f8(G, R, K, N, element_type(type), offsets, X, x_scales, x_rows, src, src_div, W, w_scales, Y.data, Y.ld,
+                                  stream);
+    });
+}
+
 PyMethodDef kMethods[] = {
     {"spmm_csr_ex", (PyCFunction)(void (*)())spmm_csr_ex, METH_FASTCALL, nullptr},
     {"spmm_csr_cfg", (PyCFunction)(void (*)())spmm_csr_cfg, METH_FASTCALL, nullptr},
@@ -464,6 +625,13 @@ PyMethodDef kMethods[] = {
     {"grouped_mm", (PyCFunction)(void (*)())grouped_mm, METH_FASTCALL, nullptr},
     {"grouped_mm_wgrad", (PyCFunction)(void (*)())grouped_mm_wgrad, METH_FASTCALL, nullptr},
     {"grouped_mm_w4", (PyCFunction)(void (*)())grouped_mm_w4, METH_FASTCALL, nullptr},
+    {"route_balance", (PyCFunction)(void (*)())route_balance, METH_FASTCALL, nullptr},
+    {"route_balance_grad", (PyCFunction)(void (*)())route_balance_grad, METH_FASTCALL, nullptr},
+    {"embed", (PyCFunction)(void (*)())embed, METH_FASTCALL, nullptr},
+    {"embed_grad", (PyCFunction)(void (*)())embed_grad, METH_FASTCALL, nullptr},
+    {"f8_rows", (PyCFunction)(void (*)())f8_rows, METH_FASTCALL, nullptr},
+    {"f8_weights", (PyCFunction)(void (*)())f8_weights, METH_FASTCALL, nullptr},
+    {"grouped_mm_f8", (PyCFunction)(void (*)())grouped_mm_f8, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
