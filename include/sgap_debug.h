@@ -107,6 +107,10 @@ int sgap_debug_group_seg_reduce(const float* in, const int32_t* span, float* out
  *     workgroup's part of the result; plan[3]: 1 where X is addressed in 64
  *     bits; plan[4]: 1 where workgroups begin at different places of the inner
  *     dimension; plan[5]: 1 where rows are read element by element.
+ *   sgap_debug_f8_plan: the same of sgap_grouped_mm_f8.  plan[0]: 1 tiles, 0
+ *     wavefronts that share the inner dimension; plan[1], plan[2]: rows and
+ *     columns of a workgroup's part of the result; plan[3]: 1 where gathered
+ *     rows are addressed in 64 bits.
  */
 int64_t sgap_debug_tile_deal(int64_t tiles, int grid, int block, int64_t* out_tiles, int64_t capacity);
 int sgap_debug_plan_nnz_serial(int group_size, int lanes_per_row, int cols_per_lane, int64_t nnz_hint,
@@ -128,6 +132,8 @@ int sgap_debug_sddmm_quads(int64_t M, int64_t K, int64_t J, int group_size, int6
 int sgap_debug_grouped_plan(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, int given_offsets, int64_t ldx,
                             int64_t x_rows, int64_t ldy, int layout, int gradient, int aligned, int compute_units,
                             int* plan);
+int sgap_debug_f8_plan(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, int given_offsets, int given_src,
+                       int64_t x_rows, int compute_units, int* plan);
 
 /*
  * Streaming kernels over n fp32 elements (16-byte aligned device buffers):

@@ -97,6 +97,7 @@ EXPORTS = {
     "sgap_debug_mttkrp_teams": (_int, [_i64, _i64, _int, _int, _int, _i64]),
     "sgap_debug_sddmm_quads": (_int, [_i64, _i64, _i64, _int, _i64, _p, _p]),
     "sgap_debug_grouped_plan": (_int, [_i64, _i64, _i64, _i64, _int, _int, _i64, _i64, _i64, _int, _int, _int, _int, _p]),
+    "sgap_debug_f8_plan": (_int, [_i64, _i64, _i64, _i64, _int, _int, _int, _i64, _int, _p]),
     "sgap_copy_f32": (_int, [_p, _p, _i64, _p]),
     "sgap_stream_f32": (_int, [_p, _p, _i64, _int, _p]),
 }

@@ -11,6 +11,7 @@
 //   numbers  the codes as bfloat16, which holds them all, and its matrix instruction: exact products, added in 32 bits, at 3.5
 //            times the matrix unit's time.  For results of floats, and for few rows, where the weights' bytes are the bound.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "sgap_grouped_tiles.hpp"
@@ -22,10 +23,10 @@ namespace {
 
 typedef int Codes __attribute__((ext_vector_type(8)));  // 32 codes of a row or column: a lane's share of a block
 
-// A * B over a block on a 16 x 16 tile; lanes and results as mma16's.  (Scales of the instruction's own: 2^0.)
+// A * B over a block on a 16 x 16 tile; lanes and results as mma16's.  (Without scales of the instruction's own.)
 __device__ __forceinline__ f32x4 mma_block(Codes a, Codes b)
 {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
 }
 
 typedef int HalfCodes __attribute__((ext_vector_type(4)));
@@ -186,29 +187,184 @@ __global__ __launch_bounds__(512) void grouped_f8_few_kernel(GroupedF8Args a, in
     }
 }
 
-// Work items are dealt to the eight dies (workgroup b runs on die b % 8) in runs of neighbours, which share rows of X or weights
-// in the die's L2.
-constexpr int kRun = 32;
+// Work items are dealt to the eight dies (workgroup b runs on die b % 8) in runs of neighbours, which share rows of X and weights
+// in the die's L2: bands of eight rows of tiles, and down and up in a band by columns, so that a run is a patch of 8 x 4.
+constexpr int kRun = 32, kBand = 8;
 __device__ __forceinline__ int64_t dealt(uint32_t b)
 {
     const uint32_t die = b & 7, at = b >> 3;
     return (int64_t)((at / kRun) * 8 + die) * kRun + at % kRun;
 }
 
-// Many rows: tiles of BM rows by BN columns, a block of the inner dimension at a time, by loads straight into LDS; two stages.
-// FAR: rows of X lie further than 32 bits of bytes from its first.  Results of floats go by numbers, others by codes.
-template <typename T, int BM, int BN, bool FAR, int THREADS>
-__global__ __launch_bounds__(THREADS) void grouped_f8_tiles_kernel(GroupedF8Args a, int64_t column_tiles, int64_t items, bool wide, int64_t block0)
+// The rows' scales of a block, put into LDS beside the tiles, a float to a lane.
+__device__ __forceinline__ void load_scale(uint32_t lds, const void* base, uint32_t offset)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "m0", "memory");
+}
+__device__ __forceinline__ void load_scale(uint32_t lds, const void* from)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(lds), "v"(from) : "m0", "memory");
+}
+
+// What comes before it in the program is done before what comes after it, where these are made or used.
+__device__ __forceinline__ void tie(f32x4& made, f32x4& added, Codes& next) { asm volatile("" : "+v"(made), "+v"(added), "+v"(next) : : "memory"); }
+__device__ __forceinline__ void tie(f32x4& made, f32x4& added, Numbers& next)
+{
+    asm volatile("" : "+v"(made), "+v"(added), "+v"(next.piece[0]), "+v"(next.piece[1]), "+v"(next.piece[2]), "+v"(next.piece[3]) : : "memory");
+}
+
+// Until no more than N of this wavefront's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_but()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+
+// acc += the products of `blocks` blocks.  STAGES of a block's tiles; the loads of a block have the STAGES - 1 before it to
+// arrive in, its fragments the products before them, and a product is added to the result while the next ones are made.
+// A block has two halves.  In the first the columns' fragments stay and half of the rows' pass, while those of the other half are
+// read; then one barrier says that everyone has read the stage, which is filled next, and that the other one is full; in the
+// second half the rows' fragments stay, and each of the columns' makes place for the next block's as soon as it has been used:
+// so there are always products to make while the next block's first fragments are read, which all wavefronts do at a time.
+//   load(t, stage, i)   starts load i of LOADS of block t; every wavefront has so many
+//   ACTIVE: this wavefront has products to make
+template <typename T, int MI, int NJ, int STAGES, int LOADS, bool ACTIVE, typename F>
+__device__ __forceinline__ void multiply_blocks(uint32_t lds, uint32_t stage_bytes, int blocks, F&& load, const float* w_scales, uint32_t wbase,
+                                                uint32_t xbase, uint32_t sbase, f32x4 (&acc)[MI][NJ])
+{
+    constexpr int H = NJ / 2;
+    static_assert(NJ % 2 == 0, "");
+    // (the same in every lane, and nobody writes them)
+    const __attribute__((address_space(4))) float* const w_scale = (const __attribute__((address_space(4))) float*)w_scales;
+    typedef __attribute__((address_space(3))) HalfCodes lds_piece;
+    typedef __attribute__((address_space(3))) float lds_float;
+    const auto fragment = [](uint32_t base, int i) {
+        return operand<T>(join(*(const lds_piece*)(uintptr_t)(base + i * 2048), *(const lds_piece*)(uintptr_t)((base ^ 64) + i * 2048)));
+    };
+    const auto scale = [](uint32_t base, int j) { return *(const lds_float*)(uintptr_t)(base + j * 64); };
+    operand_t<T> w[MI], x[2], held[H];
+    f32x4 p[H];  // of the columns before, made and not yet added
+    float s[H], held_s[H];
+#pragma unroll
+    for (int i = 0; i < H; ++i) p[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < H; ++j) held_s[j] = 0.0f;
+#pragma unroll
+    for (int b = 0; b < STAGES; ++b) {
+        if (b >= blocks) break;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) load(b, lds + b * stage_bytes, i);
+    }
+    float sw = w_scale[0];
+    // (also until the compiler's own loads have arrived)
+    if (blocks >= STAGES) wait_but<(STAGES - 1) * LOADS>();
+    else wait_loads();
+    __syncthreads();
+    if constexpr (ACTIVE) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) w[i] = fragment(wbase, i);
+        x[0] = fragment(xbase, 0);
+        s[0] = scale(sbase, 0);
+    }
+    const auto add = [&](f32x4& to, const f32x4& made, float by) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) to[r] = __builtin_fmaf(made[r], by, to[r]);
+    };
+    uint32_t other = 0;
+    for (int t = 0; t < blocks; ++t) {
+        const uint32_t stage = other;
+        other = other == (STAGES - 1) * stage_bytes ? 0 : other + stage_bytes;
+        uint32_t xb = xbase + stage, sb = sbase + stage;
+        asm volatile("" : "+v"(xb), "+v"(sb));  // made anew each time, not kept in registers
+        const float sw_next = w_scale[t + 1 < blocks ? t + 1 : t];
+        f32x4 q[MI];
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+            if constexpr (ACTIVE) {
+                if (j + 1 < H) {
+                    x[(j + 1) & 1] = fragment(xb, j + 1);
+                    s[j + 1] = scale(sb, j + 1);
+                }
+                held[j] = fragment(xb, H + j);
+                s[j] *= sw;
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const f32x4 made = mma_block(w[i], x[j & 1]);
+                    // the last columns of the block before, then the rows before
+                    f32x4& to = j == 0 ? acc[MI - 1][H + i % H] : acc[i][j - 1];
+                    if (j == 0 && i < H) add(to, p[i], held_s[i]);
+                    if (j > 0) add(to, q[i], s[j - 1]);
+                    q[i] = made;
+                    tie(q[i], to, w[(i + 1) % MI]);
+                }
+            }
+        }
+        if constexpr (ACTIVE) {
+#pragma unroll
+            for (int j = 0; j < H; ++j) held_s[j] = scale(sb, H + j) * sw;
+        }
+        if (STAGES > 2 && t + STAGES <= blocks) wait_but<(STAGES - 2) * LOADS>();
+        else wait_loads();
+        __syncthreads();
+        uint32_t wn = wbase + other, xn = xbase + other;
+        asm volatile("" : "+v"(wn), "+v"(xn));
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+#pragma unroll
+            for (int j = 0; j < H; ++j) {
+                constexpr int kSteps = MI * H;
+                if (t + STAGES < blocks) {
+#pragma unroll
+                    for (int l = (i * H + j) * LOADS / kSteps; l < (i * H + j + 1) * LOADS / kSteps; ++l) load(t + STAGES, lds + stage, l);
+                }
+                if constexpr (ACTIVE) {
+                    const f32x4 made = mma_block(w[i], held[j]);
+                    // the last rows of the first half, then the columns before
+                    f32x4& to = i == 0 ? acc[j % MI][H - 1] : acc[i - 1][H + j];
+                    if (i == 0) add(to, q[j % MI], s[H - 1]);
+                    else add(to, p[j], held_s[j]);
+                    p[j] = made;
+                    tie(p[j], to, held[(j + 1) % H]);
+                }
+            }
+            if constexpr (ACTIVE) {
+                if (i == 0) {
+                    // (where there are more columns than rows to a half)
+#pragma unroll
+                    for (int r = H; r < MI; ++r) add(acc[r][H - 1], q[r], s[H - 1]);
+                }
+                w[i] = fragment(wn, i);  // behind the last block: not used
+                if (i == (MI > 1 ? MI - 2 : 0)) {
+                    x[0] = fragment(xn, 0);
+                    s[0] = scale(sbase + other, 0);
+                }
+            }
+        }
+        sw = sw_next;
+    }
+    if constexpr (ACTIVE) {
+#pragma unroll
+        for (int j = 0; j < H; ++j) add(acc[MI - 1][H + j], p[j], held_s[j]);
+    }
+}
+
+// Many rows: tiles of BM rows by BN columns, a block of the inner dimension at a time, by loads straight into LDS.
+// FAR: rows are gathered that lie further than 32 bits of bytes from X's first.  Results of floats go by numbers, others by codes.
+// (Two wavefronts to a SIMD: with more registers than that leaves, the compiler has the matrix unit write to those that no vector
+// instruction reads, and waits for each product: 64 x 128 tiles took 0.68 us a block.)
+template <typename T, int BM, int BN, int STAGES, bool FAR, int THREADS>
+__global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8Args a, int64_t column_tiles, int64_t items, int64_t block0)
 {
     using Wt = Tile<uint8_t, BN, true, THREADS>;
     using Xt = Tile<uint8_t, BM, true, THREADS>;
     constexpr int kWaves = THREADS / 64, WN = kWaves / 2, WM = 2;
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
-    constexpr uint32_t kStage = Wt::kBytes + Xt::kBytes;
+    constexpr uint32_t kStage = Wt::kBytes + Xt::kBytes + BM * 4;
     extern __shared__ __align__(16) char lds_bytes[];
     const int64_t item = block0 + dealt(blockIdx.x);
     if (item >= items) return;
-    const int64_t tile = item / column_tiles, n0 = (item - tile * column_tiles) * BN;
+    const int64_t band = item / (kBand * column_tiles), in = item - band * (kBand * column_tiles);
+    const int64_t tile = band * kBand + in % kBand, n0 = in / kBand * BN;
     const RowTile rows = find_row_tile<BM>(a.offsets, a.G, a.R, tile);
     if (rows.rows <= 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -220,79 +376,88 @@ __global__ __launch_bounds__(THREADS) void grouped_f8_tiles_kernel(GroupedF8Args
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (rows.g < a.G) {
+        // columns and rows past the last are read from the last, and not stored; a row of X that does not exist is read
+        // from row 0, and zeros are stored
         const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_bytes;
         const uint8_t* const W = uniform(a.W + (rows.g * a.N + n0) * pitch);
+        // of X a byte's place, or, FAR, the row
         uint32_t wo[Wt::kRounds], xo[Xt::kRounds];
-        const uint8_t* xp[Xt::kRounds];
 #pragma unroll
         for (int i = 0; i < Wt::kRounds; ++i) wo[i] = (uint32_t)(min((int64_t)Wt::major(i), a.N - 1 - n0) * pitch + Wt::minor(i) * 16);
+        // rows of X from the first of the tile on, or, gathered, from X's
+        const int64_t x_first = a.from.src ? 0 : rows.first;
+        const uint8_t* const X = uniform(a.X + x_first * pitch);
+        const float* const xs = uniform(a.x_scales + x_first * blocks);
+        const auto row = [&](int i) {
+            const int64_t r = a.from.src ? a.from.row(rows.first + min(i, rows.rows - 1)) : min(i, rows.rows - 1);
+            return r < 0 ? 0 : r;
+        };
 #pragma unroll
         for (int i = 0; i < Xt::kRounds; ++i) {
-            int64_t r = a.from.row(rows.first + min(Xt::major(i), rows.rows - 1));
-            r = (r < 0 ? 0 : r) * pitch + Xt::minor(i) * 16;
-            if constexpr (FAR) xp[i] = a.X + r;
-            else xo[i] = (uint32_t)r;
+            const int64_t r = row(Xt::major(i));
+            xo[i] = FAR ? (uint32_t)r : (uint32_t)(r * pitch + Xt::minor(i) * 16);
         }
-        // scales: of the lane's row in each of its tiles, of the wavefront's columns
-        const float* sx[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int64_t r = a.from.row(rows.first + min(wm + 16 * j + (lane & 15), rows.rows - 1));
-            sx[j] = a.x_scales + (r < 0 ? 0 : r) * blocks;
-        }
+        // a wavefront loads the scales of 64 rows (where there are more wavefronts than that, some the same ones)
+        const int scales0 = wave * 64 % BM;
+        const int64_t scale_row = row(scales0 + lane);
+        const uint32_t so = FAR ? (uint32_t)scale_row : (uint32_t)(scale_row * blocks * 4);
         const float* const sw = uniform(a.w_scales + (rows.g * f8_blocks(a.N) + min(n0 + wn, a.N - 1) / kF8Block) * blocks);
-        const auto load = [&](int64_t t, uint32_t to) {
-            const uint8_t* const w = uniform(W + t * kF8Block);
-#pragma unroll
-            for (int i = 0; i < Wt::kRounds; ++i) Wt::load(to, i, w, wo[i]);
-#pragma unroll
-            for (int i = 0; i < Xt::kRounds; ++i) {
-                if constexpr (FAR) Xt::load(to + Wt::kBytes, i, xp[i] + t * kF8Block);
-                else Xt::load(to + Wt::kBytes, i, uniform(a.X + t * kF8Block), xo[i]);
+        constexpr int kLoads = Wt::kRounds + Xt::kRounds + 1;
+        const auto load = [&](int t, uint32_t to, int i) {
+            const int r = i - Wt::kRounds;
+            if (i < Wt::kRounds) {
+                Wt::load(to, i, uniform(W + (int64_t)t * kF8Block), wo[i]);
+            } else if (r < Xt::kRounds) {
+                if constexpr (FAR) Xt::load(to + Wt::kBytes, r, X + (int64_t)xo[r] * pitch + Xt::minor(r) * 16 + (int64_t)t * kF8Block);
+                else Xt::load(to + Wt::kBytes, r, uniform(X + (int64_t)t * kF8Block), xo[r]);
+            } else {
+                const uint32_t at = __builtin_amdgcn_readfirstlane(to + Wt::kBytes + Xt::kBytes + scales0 * 4);
+                if constexpr (FAR) load_scale(at, xs + (int64_t)so * blocks + t);
+                else load_scale(at, uniform(xs + t), so);
             }
         };
         const uint32_t wbase = lds + Wt::lane_base(wn), xbase = lds + Wt::kBytes + Xt::lane_base(wm);
-        const auto fragment = [&](uint32_t base, int i) {
-            typedef __attribute__((address_space(3))) HalfCodes lds_piece;
-            return join(*(const lds_piece*)(uintptr_t)(base + i * 2048), *(const lds_piece*)(uintptr_t)((base ^ 64) + i * 2048));
-        };
-        load(0, lds);
-        for (int64_t t = 0; t < blocks; ++t) {
-            const uint32_t stage = (t & 1) * kStage;
-            float s[NJ];
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) s[j] = sx[j][t] * sw[t];
-            wait_loads();
-            __syncthreads();
-            if (t + 1 < blocks) load(t + 1, lds + kStage - stage);
-            if (wm < rows.rows) {
-                operand_t<T> w[MI];
-#pragma unroll
-                for (int i = 0; i < MI; ++i) w[i] = operand<T>(fragment(wbase + stage, i));
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const operand_t<T> x = operand<T>(fragment(xbase + stage, j));
-#pragma unroll
-                    for (int i = 0; i < MI; ++i) {
-                        const f32x4 p = mma_block(w[i], x);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(p[r], s[j], acc[i][j][r]);
-                    }
-                }
-            }
-            __syncthreads();
-        }
+        const uint32_t sbase = lds + Wt::kBytes + Xt::kBytes + (wm + (lane & 15)) * 4;
+        if (wm < rows.rows) multiply_blocks<T, MI, NJ, STAGES, kLoads, true>(lds, kStage, (int)blocks, load, sw, wbase, xbase, sbase, acc);
+        else multiply_blocks<T, MI, NJ, STAGES, kLoads, false>(lds, kStage, (int)blocks, load, sw, wbase, xbase, sbase, acc);
     }
+    // Through LDS, each wavefront its own part, so that rows leave in whole lines: 16-byte chunk c of row r at place c ^ (r & 7).
+    constexpr int kColumns = BN / WN, kRows = BM / WM, P = Piece<T>::kCount, kChunks = kColumns / P;
+    static_assert(kRows * kColumns * (int)sizeof(T) * kWaves <= STAGES * (int)kStage && kChunks >= 8, "");
+    typedef __attribute__((address_space(3))) char lds_char;
+    typedef T out4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) out4 lds_out4;
+    typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
+    lds_char* const part = (lds_char*)lds_bytes + wave * (kRows * kColumns * (int)sizeof(T));
+    __syncthreads();  // everyone has read what lies there
+    const int real_rows = min(rows.rows - wm, kRows);
+    if (real_rows <= 0) return;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-        const int m = wm + 16 * j + (lane & 15);
-        if (m >= rows.rows) continue;
-        const bool real = rows.g < a.G && (!a.from.src || a.from.row(rows.first + m) >= 0);
-        T* __restrict__ y = static_cast<T*>(a.Y) + (rows.first + m) * a.ldy;
+        const int m = 16 * j + (lane & 15);
+        const bool real = rows.g < a.G && m < real_rows && (!a.from.src || a.from.row(rows.first + wm + m) >= 0);
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
-            const int64_t n = n0 + wn + 16 * i + 4 * (lane >> 4);
-            if (n < a.N) store4(y, n, a.N, wide, real ? acc[i][j] : f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+            const int n = 16 * i + 4 * (lane >> 4);
+            out4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = (T)(real ? acc[i][j][r] : 0.0f);
+            *(lds_out4*)(part + m * (kColumns * (int)sizeof(T)) + (((n / P) ^ (m & 7)) * P + n % P) * (int)sizeof(T)) = o;
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    constexpr int kAtOnce = 64 / kChunks;  // rows
+    const int chunk = lane % kChunks;
+    const int64_t n = n0 + wn + chunk * P;
+    T* __restrict__ y = static_cast<T*>(a.Y) + (rows.first + wm) * a.ldy + n;
+    for (int m = lane / kChunks; m < real_rows; m += kAtOnce) {
+        const piece_t<T> v = *(const lds_piece*)(part + m * (kColumns * (int)sizeof(T)) + (chunk ^ (m & 7)) * 16);
+        if (n + P <= a.N) {
+            store_piece(y + m * a.ldy, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (n + i < a.N) y[m * a.ldy + i] = v[i];
         }
     }
 }
@@ -309,38 +474,84 @@ hipError_t run_few(const GroupedF8Args& a, bool wide, hipStream_t s)
     });
 }
 
-template <typename T, int BM, int BN, bool FAR, int THREADS>
-hipError_t run_tiles(const GroupedF8Args& a, bool wide, hipStream_t s)
+template <typename T, int BM, int BN, int STAGES, bool FAR, int THREADS>
+hipError_t run_tiles(const GroupedF8Args& a, hipStream_t s)
 {
-    const int64_t columns = (a.N + BN - 1) / BN, items = columns * most_row_tiles(a.G, a.R, BM, a.offsets != nullptr);
-    constexpr int kLds = 2 * 128 * (BM + BN);
+    const int64_t columns = (a.N + BN - 1) / BN, bands = (most_row_tiles(a.G, a.R, BM, a.offsets != nullptr) + kBand - 1) / kBand;
+    const int64_t items = columns * bands * kBand;
+    constexpr int kLds = STAGES * (128 * (BM + BN) + BM * 4);
     static uint64_t allowed = 0;
-    if (const hipError_t err = allow_lds(grouped_f8_tiles_kernel<T, BM, BN, FAR, THREADS>, kLds, allowed)) return err;
+    if (const hipError_t err = allow_lds(grouped_f8_tiles_kernel<T, BM, BN, STAGES, FAR, THREADS>, kLds, allowed)) return err;
     return launch_parts((items + 255) / 256 * 256, THREADS, [&](unsigned grid, int64_t block0) {
-        grouped_f8_tiles_kernel<T, BM, BN, FAR, THREADS><<<grid, THREADS, kLds, s>>>(a, columns, items, wide, block0);
+        grouped_f8_tiles_kernel<T, BM, BN, STAGES, FAR, THREADS><<<grid, THREADS, kLds, s>>>(a, columns, items, block0);
     });
 }
 
 template <typename T>
-hipError_t grouped_f8(GroupedF8Args a, hipStream_t s)
+hipError_t grouped_f8(const GroupedF8Args& a, const GroupedF8Plan& p, hipStream_t s)
 {
-    if (a.from.rows == 0) a.K = 0;  // no row of X: zeros, and nothing is read
-    // 128 lines of an operand have to lie within 32 bits of bytes
-    constexpr int64_t kLongest = 1 << 22;
+    // (the address and the row's length that stores of four results ask for)
     const bool wide = a.ldy % 4 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & (4 * sizeof(T) - 1)) == 0;
-    const bool far = a.from.rows * f8_blocks(a.K) * kF8Block > 0xffffffffLL;
-    if (a.K == 0 || a.K > kLongest || a.R / a.G < 64) return run_few<T, 1, 1, 4>(a, wide, s);
-    return far ? run_tiles<T, 128, 128, true, 256>(a, wide, s) : run_tiles<T, 128, 128, false, 256>(a, wide, s);
+    if (!p.tiles) return p.rows == 16 ? run_few<T, 1, 1, 4>(a, wide, s) : run_few<T, 2, 2, 2>(a, wide, s);
+    if constexpr (sizeof(T) == 2) {
+        if (p.rows == 256) return run_tiles<T, 256, 256, 2, false, 512>(a, s);
+    }
+    if (p.far) return run_tiles<T, 128, 128, 2, true, 256>(a, s);
+    return p.rows == 128 ? run_tiles<T, 128, 128, 2, false, 256>(a, s) : run_tiles<T, 64, 128, 2, false, 256>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_grouped_f8(const GroupedF8Args& a, int dtype, hipStream_t s)
+// The least of what the kernels are reckoned to take, in us.  With tiles, a compute unit has n of them: a tile costs so much a
+// block of the inner dimension and so much besides, and the only one of a unit more a block.  A group has a last tile that is not
+// full: 0.6 of a tile more than its rows in the mean.  With few rows: the weights pass once for 16 or 32 rows.
+// Measured (us; few rows 16, 32; tiles of 64, 128, 256 rows), inner dimension by columns, 16-bit results:
+//   1 row, 4,096 x 4,096                      6.2  10.5  16.8  25.5  40.7
+//   32 rows, 8,192 x 8,192                   40.2  25.2  53.4  59.1  76.0
+//   64 groups, 64 rows, 2,048 x 1,408        23.3  43.9  17.4  21.0  28.4
+//   256 rows, 4,096 x 4,096                  77.1  51.0  20.6  27.7  51.6
+//   2,048 rows, 4,096 x 4,096                 572   381  62.2  48.1  67.4
+//   64 groups, 8,192 rows, 2,048 x 1,408      406   386  60.3  66.1  68.9
+//   16 groups, 16,384 rows, 2,048 x 4,096   2,177 1,982   262   219   192
+GroupedF8Plan plan_grouped_f8(const GroupedF8Args& a, int dtype)
 {
+    const bool half = dtype != 0;
+    const double blocks = (double)f8_blocks(a.K), used = a.offsets ? (double)std::min(a.G, std::max<int64_t>(a.R, 1)) : 1.0;
+    const double rows = (double)a.R / used, bytes = 2.5 + used * (double)a.K * (double)a.N / 5.7e6;  // the weights', once
+    GroupedF8Plan p = {false, false, 16, 16};
+    p.far = a.from.src && a.from.rows * f8_blocks(a.K) * kF8Block > 1ll << 32;
+    double few = bytes;
+    if (rows > 16) {
+        few = 2.5 + std::ceil(rows / 32) * (bytes - 2.5) * 2.0;
+        p.rows = p.columns = 32;
+    }
+    // 128 lines of an operand have to lie within 32 bits of bytes
+    constexpr int64_t kLongest = 1 << 22;
+    if (a.K == 0 || a.K > kLongest) return p;
+    const auto tiles = [&](int BM, int BN, double block, double only, double besides) {
+        const double down = used == 1 ? std::ceil((double)a.R / BM) : (double)a.R / BM + 0.6 * used;
+        const double n = std::ceil(down * std::ceil((double)a.N / BN) / a.compute_units);
+        return std::max(std::max(n * (block * blocks + besides), only * blocks + 4.0), bytes);
+    };
+    const double small = p.far ? 1e30 : half ? tiles(64, 128, 0.48, 0.58, 0.4) : tiles(64, 128, 0.6, 0.92, 0.4);
+    const double middle = half ? tiles(128, 128, 0.72, 0.88, 1.4) : tiles(128, 128, 1.02, 1.3, 1.4);
+    const double large = half && !p.far ? tiles(256, 256, 1.67, 1.67, 9.0) : 1e30;
+    const double least = std::min(std::min(small, middle), large);
+    if (few < (used > 1 ? 0.8 : 1.0) * least) return p;
+    p.tiles = true;
+    p.rows = small <= least ? 64 : middle <= least ? 128 : 256;
+    p.columns = p.rows == 256 ? 256 : 128;
+    return p;
+}
+
+hipError_t launch_grouped_f8(GroupedF8Args a, int dtype, hipStream_t s)
+{
+    if (a.from.rows == 0) a.K = 0;  // no row of X: zeros, and nothing is read
+    const GroupedF8Plan p = plan_grouped_f8(a, dtype);
     switch (dtype) {
-        case 0: return grouped_f8<float>(a, s);
-        case 1: return grouped_f8<half_t>(a, s);
-        default: return grouped_f8<bf16_t>(a, s);
+        case 0: return grouped_f8<float>(a, p, s);
+        case 1: return grouped_f8<half_t>(a, p, s);
+        default: return grouped_f8<bf16_t>(a, p, s);
     }
 }
 

@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "../../include/sgap.h"
+#include "../../include/sgap_debug.h"
 #include "sgap_tokens.hpp"
 
 namespace sgap {
@@ -187,6 +188,23 @@ int sgap_grouped_mm_f8(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, co
     if (loose(X) || loose(W)) return invalid("codes must be 16-byte aligned");
     const sgap::GroupedF8Args a{G, R, K, N, offsets, {src, src_div, x_rows}, X, x_scales, W, w_scales, Y, ldy, sgap::device_compute_units()};
     return launched(sgap::launch_grouped_f8(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int sgap_debug_f8_plan(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, int given_offsets, int given_src, int64_t x_rows,
+                       int compute_units, int* plan)
+{
+    if (check_f8_weights(G, K, N) != SGAP_OK || !any_type(dtype) || R < 0 || R > kMaxSteps || x_rows < 0 || compute_units < 1 || !plan)
+        return invalid("bad arguments");
+    // only whether there are lists is looked at
+    const int32_t* const list = reinterpret_cast<const int32_t*>(0x1000);
+    const sgap::GroupedF8Args a{G, R, K, N, given_offsets ? list : nullptr, {given_src ? list : nullptr, 1, x_rows}, nullptr, nullptr,
+                                nullptr, nullptr, nullptr, N, compute_units};
+    const sgap::GroupedF8Plan p = sgap::plan_grouped_f8(a, dtype);
+    plan[0] = p.tiles ? 1 : 0;
+    plan[1] = p.rows;
+    plan[2] = p.columns;
+    plan[3] = p.far ? 1 : 0;
+    return SGAP_OK;
 }
 
 }  // extern "C"

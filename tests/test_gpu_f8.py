@@ -7,6 +7,7 @@ import torch
 from experts_util import E as EPS
 from experts_util import assert_within, grouped_mm, offsets_of, random
 from paper_2209_02882_amd import binding
+from test_f8_plan import plan
 from tokens_util import BLOCK, blocks, e4m3, f8_rows, f8_weights, filled, power_scale, random_codes, values
 
 pytestmark = pytest.mark.gpu
@@ -187,6 +188,56 @@ SHAPES = [  # sizes of groups, rows behind them, N, K
 def test_products(sizes, more, N, K, dtype):
     R = sum(sizes) + more
     check(*operands(R + N, R, len(sizes), N, K), K, offsets_of(sizes), R, dtype)
+
+
+# every kernel that a product may take, asked of the plan
+@pytest.mark.parametrize("G,R,N,K,dtype,want", [
+    (1, 11, 100, 500, torch.bfloat16, (0, 16, 16, 0)), (1, 40, 1000, 4000, torch.float16, (0, 32, 32, 0)),
+    (3, 100, 4000, 300, torch.bfloat16, (1, 64, 128, 0)), (5, 4100, 4000, 1100, torch.float16, (1, 128, 128, 0)),
+    (1, 4000, 8100, 530, torch.bfloat16, (1, 256, 256, 0)), (3, 6000, 4000, 1100, torch.float16, (1, 256, 256, 0)),
+    (2, 200, 3000, 400, torch.float32, (0, 32, 32, 0)), (3, 2000, 3900, 500, torch.float32, (1, 64, 128, 0)),
+    (2, 3000, 3900, 1500, torch.float32, (1, 128, 128, 0)),
+])
+@pytest.mark.parametrize("gathered", [False, True])
+def test_products_by_every_kernel(G, R, N, K, dtype, want, gathered):
+    assert plan(G, R, K, N, dtype, given=G > 1, src=gathered, compute_units=torch.cuda.get_device_properties(0).multi_processor_count) == want
+    gen = torch.Generator().manual_seed(R)
+    sizes = torch.distributions.Multinomial(R - 3, torch.rand(G, generator=gen) + 0.2).sample().int() if G > 1 else torch.tensor([R])
+    src = torch.randperm(R, generator=gen).int() if gathered else None
+    x, xs, w, ws = (t.cuda() for t in operands(R, (R + 1) // 2 if gathered else R, G, N, K))
+    off = offsets_of(sizes.tolist()) if G > 1 else None
+    y = product(x, xs, w, ws, K, off, R, dtype, src, 2 if gathered else 1).double()
+    # in 64 bits on the device: too many for the host
+    rows = values(x, xs, K, True)
+    rows = rows[torch.div(src.long().cuda(), 2, rounding_mode="floor")] if gathered else rows
+    u = {torch.float32: 2.0**-24, torch.float16: 2.0**-11, torch.bfloat16: 2.0**-8}[dtype]
+    for g, (a, b) in enumerate(zip([0] if off is None else off[:-1].tolist(), [R] if off is None else off[1:].tolist())):
+        wv, v = values(w[g:g + 1], ws[g:g + 1], K, False)[0].t().contiguous(), rows[a:b].contiguous()
+        want, size = v @ wv, v.abs() @ wv.abs()
+        slack = (K + 8) * EPS * size
+        if dtype != torch.float32:
+            eights = lambda z: torch.nn.functional.pad(z.abs(), (0, -K % 8)).unflatten(-1, (-1, 8)).amax(-1)  # noqa: E731
+            slack = slack + 7 * 2.0**-13 * (eights(v) @ eights(wv.t()).t().contiguous())
+        assert ((y[a:b] - want).abs() <= slack + u * (want.abs() + slack) + 2.0**-24).all()
+    last = R if off is None else int(off[-1])
+    assert not y[last:].any()
+
+
+def test_rows_gathered_from_more_than_4_gib():
+    K, N, R, x_rows = 4224, 512, 40_000, (1 << 20) + 5
+    assert plan(1, R, K, N, torch.bfloat16, given=False, src=True, x_rows=x_rows) == (1, 128, 128, 1)
+    _, _, w, ws = operands(1, 1, 1, N, K)
+    some, scales, _, _ = operands(2, 64, 1, 1, K)
+    x = torch.zeros(x_rows, K, dtype=torch.uint8, device="cuda")
+    xs = torch.ones(x_rows, K // BLOCK, device="cuda")
+    at = torch.cat([torch.arange(20), torch.arange(x_rows - 44, x_rows)])
+    x[at.cuda()], xs[at.cuda()] = some.view(torch.uint8).cuda(), scales.cuda()
+    which = torch.randint(0, 64, (R,), generator=torch.Generator().manual_seed(3))
+    y = filled(torch.bfloat16, R, N)
+    binding.sgap_grouped_mm_f8(1, R, K, N, None, x.view(F8), xs, w.cuda(), ws.cuda(), y, src=at[which].int().cuda())
+    want, size = grouped_mm(torch.tensor([0, 64]), values(some, scales, K, True), values(w, ws, K, False), "nk", 64)
+    lost = cut_off(torch.bfloat16, torch.tensor([0, 64]), some, scales, w, ws, K, 64)
+    assert_within(y, want[which], ((K + 8) * EPS * size + lost)[which])
 
 
 @pytest.mark.parametrize("R", [1, 2, 15, 16, 17, 31, 48, 63, 64, 65, 127, 128, 129, 256, 300, 1000])
