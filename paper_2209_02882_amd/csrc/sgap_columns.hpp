@@ -24,6 +24,28 @@ struct Columns {
             for (int i = 0; i < VEC; ++i) v[i] = (float)x[i];
         }
     }
+    // what nobody reads again soon
+    __device__ __forceinline__ void stream_load(const T* p)
+    {
+        if constexpr (VEC == 1) {
+            v[0] = (float)__builtin_nontemporal_load(p);
+        } else {
+            const piece_t<T> x = __builtin_nontemporal_load(reinterpret_cast<const typename Piece<T>::loose*>(p));
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = (float)x[i];
+        }
+    }
+    __device__ __forceinline__ void stream_store(T* p) const
+    {
+        if constexpr (VEC == 1) {
+            __builtin_nontemporal_store((T)v[0], p);
+        } else {
+            piece_t<T> x;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = (T)v[i];
+            __builtin_nontemporal_store((typename Piece<T>::loose)x, reinterpret_cast<typename Piece<T>::loose*>(p));
+        }
+    }
     __device__ __forceinline__ void store(T* p) const
     {
         if constexpr (VEC == 1) {

@@ -4,11 +4,12 @@
 // A lookup is the product with a sparse matrix that has one entry a row; the gradient is the product with its transpose, a
 // sum by segments of very different length: most rows of a table no token has, and one token may be a tenth of a batch.
 //
-// The gradient in three steps.  1. The tokens by their id, in their order within one: a workgroup has a range of ids and
+// The gradient in three steps.  1. The tokens by their id, those of one always in the same order: a workgroup has a range of ids and
 // looks at all tokens, so that it knows by itself how many come before its range, and no workgroup waits for another.
 // 2. Tiles of that order, each an equal number of tokens whatever ids they have; a run of one id that lies in a tile is
-// summed up and stored, what crosses a tile's ends goes to the workspace; rows without a token are cleared beside it.
-// 3. The parts of the runs that cross tiles are added, in their order.  Sums in 32 bits, rounded once; no atomics on floats.
+// summed up and stored, what crosses a tile's ends goes to the workspace.
+// 3. The parts of the runs that cross tiles are added, always in the same order, and rows without a token are cleared.  Sums in 32
+// bits, rounded once; no atomics on floats.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,8 +22,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kMostIds = 512;  // of a workgroup's range
-constexpr int kClearRows = 16;  // rows that a group of lanes looks at, whether they have a token
+constexpr int kMostIds = 256;  // of a workgroup's range
+constexpr int kList = 416;     // tokens of it that a wavefront collects, 256 at a time
+constexpr int kClearRows = 128;  // rows that a workgroup looks at, whether they have a token
 
 // Groups of `lanes` (a power of two, 64 at most) have an item each: a row, or a tile, and lanes * VEC of its columns.
 struct Spread {
@@ -49,23 +51,36 @@ __device__ __forceinline__ Place place_of(int lanes, int64_t column_items, int64
     return {item, ((group - item * column_items) * lanes + (threadIdx.x & (lanes - 1))) * VEC};
 }
 
-template <typename T, int VEC>
+// A group of lanes has TOKENS neighbouring tokens, all of their rows on the way together.
+template <typename T, int VEC, int TOKENS>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes, int64_t column_items, int64_t block0)
 {
     const Place at = place_of<VEC>(lanes, column_items, block0 + blockIdx.x);
-    if (at.item >= a.T || at.c >= a.D) return;
+    const int64_t t0 = at.item * TOKENS;
+    if (t0 >= a.T || at.c >= a.D) return;
     const int64_t first = piece_first<VEC>(at.c, a.D);
-    const int32_t id = a.ids[at.item];
-    Columns<T, VEC> x;
-    if (id >= 0 && id < a.V) {
-        x.load(static_cast<const T*>(a.weights) + id * a.ldw + first);
+    const T* __restrict__ W = static_cast<const T*>(a.weights) + first;
+    Columns<T, VEC> x[TOKENS];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) x.v[i] *= a.scale;
-    } else {
+    for (int u = 0; u < TOKENS; ++u) {
+        const int32_t id = t0 + u < a.T ? a.ids[t0 + u] : -1;
+        if (id >= 0 && id < a.V) {
+            x[u].load(W + id * a.ldw);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) x.v[i] = 0.0f;
+            for (int i = 0; i < VEC; ++i) x[u].v[i] *= a.scale;
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[u].v[i] = 0.0f;
+        }
     }
-    x.store(static_cast<T*>(a.out) + at.item * a.ldo + first);
+#pragma unroll
+    for (int u = 0; u < TOKENS; ++u) {
+        if (t0 + u >= a.T) break;
+        T* const out = static_cast<T*>(a.out) + (t0 + u) * a.ldo + first;
+        // many rows are written past the caches, which keep the table's frequent rows (16,384 by 2,048, bf16: 17.1 us, 25.1 without)
+        if constexpr (TOKENS > 1) x[u].stream_store(out);
+        else x[u].store(out);
+    }
 }
 
 // What the gradient keeps in its workspace.  Place p of the order has token order[p], of id key[p]; id v has the places
@@ -73,15 +88,18 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes,
 struct Sorted {
     int32_t *start, *key, *order;
     float* parts;  // tiles x 2 x D: of the run that a tile begins in the middle of, and of the one that goes on behind it
-    int64_t tile, tiles, bytes;
+    int64_t part, tile, tiles, bytes;  // places of a group of lanes, and of a workgroup of them
 };
-Sorted sorted_view(char* workspace, int64_t T, int64_t V, int64_t D)
+// groups: of lanes to a workgroup, four at least
+Sorted sorted_view(char* workspace, int64_t T, int64_t V, int64_t D, int groups)
 {
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
     Sorted s;
-    // tokens of a tile: 32, or what makes 1,024 tiles at most
-    s.tile = 32;
-    while (s.tile * 1024 < T) s.tile *= 2;
+    // tokens of a part: 8, or what makes 1,024 parts at most, or more where rows are so short that 4,096 wavefronts have more
+    s.part = 8;
+    const int64_t most = std::max<int64_t>(1024, (1 << 21) / std::max<int64_t>(D, 1));
+    while (s.part * most < T) s.part *= 2;
+    s.tile = s.part * groups;
     s.tiles = (T + s.tile - 1) / s.tile;
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
@@ -97,13 +115,37 @@ Sorted sorted_view(char* workspace, int64_t T, int64_t V, int64_t D)
     return s;
 }
 
-// ids range .. range + ids_of of a workgroup.  Every wavefront has a run of the tokens: it counts its own by id, the counts
-// are summed up over the wavefronts and the ids, and every wavefront puts its tokens in their places, in order.
+// Rows of the gradient that no token has, as 16-bit halves of zeros, whatever type they have: half of them are cleared beside the
+// sorting and half beside the joins, which both wait more than they work (all of them beside the joins: 8 us more for 65,536
+// rows of 2,048, bf16).
+struct Clearing {
+    uint16_t* __restrict__ rows;  // null: nothing is cleared
+    int64_t halves, pitch;
+};
+__device__ __forceinline__ void clear_row(const Clearing& c, int64_t v)
+{
+    typedef uint16_t loose __attribute__((ext_vector_type(8), aligned(2)));
+    const int lane = threadIdx.x & 63;
+    uint16_t* const row = c.rows + v * c.pitch;
+    if (c.halves < 8) {
+        if (lane < c.halves) row[lane] = 0;
+        return;
+    }
+    for (int64_t i = lane * 8; i < c.halves; i += 512) *reinterpret_cast<loose*>(row + min(i, c.halves - 8)) = loose{0, 0, 0, 0, 0, 0, 0, 0};
+}
+__device__ __forceinline__ bool cleared_early(int64_t v) { return (v & 1) == 0; }
+
+// ids range .. range + ids_of of a workgroup.  Every wavefront has a run of the tokens and collects those of the range, so that it
+// deals with 64 of them at a time; it counts them by id, the counts are summed up over the wavefronts and the ids, and every wavefront
+// puts its tokens in their places, always in the same order.  Where they are more than its list holds, it looks at the tokens again.
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* __restrict__ ids, int64_t T, int64_t V, int ids_of,
                                                                   int32_t* __restrict__ start, int32_t* __restrict__ key,
-                                                                  int32_t* __restrict__ order, int64_t block0)
+                                                                  int32_t* __restrict__ order, Clearing clearing, int64_t block0)
 {
     extern __shared__ int32_t count[];  // wavefronts x ids_of: tokens of an id, then the next place
+    __shared__ int32_t found[kSortWaves][kList];  // tokens of the range ...
+    __shared__ uint16_t found_id[kSortWaves][kList];  // ... and their ids in it
+    __shared__ bool none[kMostIds];
     __shared__ int32_t before[kSortWaves], wave_total[kSortWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int64_t range = (block0 + blockIdx.x) * ids_of;
@@ -111,22 +153,68 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     const int64_t share = ((T + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const int64_t first = min((int64_t)wave * share, T), end = min(first + share, T);
     int32_t* const own = count + wave * ids_of;
+    int32_t* const list = found[wave];
+    uint16_t* const list_id = found_id[wave];
     for (int i = lane; i < ids_of; i += 64) own[i] = 0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    int below = 0;
-    for (int64_t t0 = first; t0 < end; t0 += 256) {
-        uint32_t id[4];
+    // Collects the tokens of the range; `deal` has the list when it is full.  A lane has four neighbouring tokens, the next ones are on
+    // their way.  (id 2^32 - 1, which no range has, behind the last)
+    int fill = 0, below = 0;
+    const auto scan = [&](auto&& deal) {
+        if (first >= end) return;  // (no tokens at all: nothing to read in place of one past the last)
+        typedef int32_t loose __attribute__((ext_vector_type(4), aligned(4)));
+        constexpr int kAhead = 4;
+        loose next[kAhead];
+        const auto ask = [&](int64_t t0) {
+            if (t0 + 256 <= end) return *reinterpret_cast<const loose*>(ids + t0 + lane * 4);
+            loose v;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t t = t0 + u * 64 + lane;
-            id[u] = t < end ? (uint32_t)ids[t] : 0xffffffffu;
-        }
+            for (int u = 0; u < 4; ++u) {
+                const int64_t t = t0 + lane * 4 + u;
+                v[u] = ids[min(t, T - 1)];
+                v[u] = t < end ? v[u] : -1;
+            }
+            return v;
+        };
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            below += __popcll(__ballot(id[u] < lo));
-            if (id[u] - lo < n) atomicAdd(&own[id[u] - lo], 1);  // (counts: whole numbers)
+        for (int h = 0; h < kAhead; ++h) next[h] = ask(first + h * 256);
+#pragma unroll 1
+        for (int64_t t0 = first; t0 < end; t0 += 256) {
+            const loose id = next[0];
+#pragma unroll
+            for (int h = 0; h + 1 < kAhead; ++h) next[h] = next[h + 1];
+            next[kAhead - 1] = ask(t0 + kAhead * 256);
+            if (fill > kList - 256) {
+                deal();
+                fill = 0;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t in = (uint32_t)id[u] - lo;
+                below += (uint32_t)id[u] < lo ? 1 : 0;
+                const uint64_t hit = __ballot(in < n);
+                if (in < n) {
+                    const int at = fill + __popcll(hit & ((1ull << lane) - 1));
+                    list[at] = (int32_t)(t0 + lane * 4 + u);
+                    list_id[at] = (uint16_t)in;
+                }
+                fill += __popcll(hit);
+            }
         }
-    }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    bool whole = true;  // the list has all of the wavefront's
+    const auto counted = [&] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int i = lane; i < fill; i += 64) atomicAdd(&own[list_id[i]], 1);  // (counts: whole numbers)
+    };
+    scan([&] {
+        counted();
+        whole = false;
+    });
+    counted();
+#pragma unroll
+    for (int d = 32; d; d >>= 1) below += __shfl_xor(below, d);
     if (lane == 0) before[wave] = below;
     __syncthreads();
     int base = 0;
@@ -156,179 +244,324 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     if (i < ids_of) {
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) count[w * ids_of + i] += place;
+        none[i] = i < (int)n && total == 0;
         if (i < (int)n) {
             start[range + i] = place;
             if (range + i == V - 1) start[V] = place + total;
         }
     }
     __syncthreads();
-    for (int64_t t0 = first; t0 < end; t0 += 256) {
-        uint32_t id[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t t = t0 + u * 64 + lane;
-            id[u] = t < end ? (uint32_t)ids[t] : 0xffffffffu;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint32_t in = id[u] - lo;
-            uint64_t left = __ballot(in < n);
+    const auto placed = [&] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int l = 0; l < fill; l += 64) {
+            const int e = l + lane;
+            const int32_t token = e < fill ? list[e] : 0;
+            const uint32_t in = e < fill ? list_id[e] : 0xffffu;
+            uint64_t left = __ballot(e < fill);
             while (left) {
                 // the tokens of the id that the lowest lane left has
-                const uint32_t which = (uint32_t)__builtin_amdgcn_readlane((int)in, __builtin_ctzll(left));
+                const int leader = __builtin_ctzll(left);
+                const uint32_t which = (uint32_t)__builtin_amdgcn_readlane((int)in, leader);
                 const uint64_t same = __ballot(in == which);
-                const int at = own[which];
+                int at = 0;
+                if (lane == leader) at = atomicAdd(&own[which], __popcll(same));  // (this wavefront's alone)
+                at = __builtin_amdgcn_readlane(at, leader);
                 if (in == which) {
                     const int p = at + __popcll(same & ((1ull << lane) - 1));
-                    key[p] = (int32_t)id[u];
-                    order[p] = (int32_t)(t0 + u * 64 + lane);
+                    key[p] = (int32_t)(lo + in);
+                    order[p] = token;
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                if (lane == 0) own[which] = at + __popcll(same);
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 left &= ~same;
             }
         }
+    };
+    if (!whole) {
+        fill = 0;
+        scan(placed);
     }
+    placed();
+    if (!clearing.rows) return;
+    for (int r = wave; r < (int)n; r += kSortWaves)
+        if (none[r] && cleared_early(range + r)) clear_row(clearing, range + r);
 }
 
+// A piece of a row of the gradient, in accesses of 16 bytes at most.
 template <typename G, int VEC>
-__device__ __forceinline__ void store_row(const EmbedGradArgs& a, int64_t v, int64_t first, int shared, const float (&sum)[VEC])
+struct GradPiece {
+    static constexpr int kPart = VEC < Piece<G>::kCount ? 1 : Piece<G>::kCount, kParts = VEC / kPart;
+    Columns<G, kPart> part[kParts];
+    __device__ __forceinline__ void load(const G* p)
+    {
+#pragma unroll
+        for (int h = 0; h < kParts; ++h) part[h].load(p + h * kPart);
+    }
+    // = scale * sum (and +0 of nothing)
+    __device__ __forceinline__ void set(float scale, const float (&sum)[VEC])
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) part[i / kPart].v[i % kPart] = 0.0f + scale * sum[i];
+    }
+    __device__ __forceinline__ void add(float scale, const float (&sum)[VEC])
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) part[i / kPart].v[i % kPart] += scale * sum[i];
+    }
+    __device__ __forceinline__ void store(G* p) const
+    {
+#pragma unroll
+        for (int h = 0; h < kParts; ++h) part[h].store(p + h * kPart);
+    }
+};
+
+// A row's piece out of its sum; ADD: added to `was`, by each lane to its own columns alone (the first `shared` of a row's last
+// piece are the lane's in front).
+template <bool ADD, typename G, int VEC>
+__device__ __forceinline__ void store_row(const EmbedGradArgs& a, int64_t v, int64_t first, int shared, const float (&sum)[VEC],
+                                          GradPiece<G, VEC>& was)
 {
     G* const to = static_cast<G*>(a.dweights) + v * a.ldw + first;
-    if (a.accumulate && shared > 0) {
-        // columns that the lane in front has as well are added by it alone
+    if constexpr (ADD) {
+        was.add(a.scale, sum);
+        if (shared > 0) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-            if (i >= shared) to[i] = (G)((float)to[i] + a.scale * sum[i]);
-        return;
+            for (int i = 0; i < VEC; ++i)
+                if (i >= shared) to[i] = (G)was.part[i / was.kPart].v[i % was.kPart];
+            return;
+        }
+    } else {
+        was.set(a.scale, sum);
     }
-#pragma unroll
-    for (int h = 0; h < (VEC + Piece<G>::kCount - 1) / Piece<G>::kCount; ++h) {
-        constexpr int kPart = VEC < Piece<G>::kCount ? 1 : Piece<G>::kCount;
-        Columns<G, kPart> x;
-        if (a.accumulate) x.load(to + h * kPart);
-#pragma unroll
-        for (int i = 0; i < kPart; ++i) x.v[i] = (a.accumulate ? x.v[i] : 0.0f) + a.scale * sum[h * kPart + i];
-        x.store(to + h * kPart);
-    }
+    was.store(to);
 }
 
-// Behind the tiles' workgroups come those that clear the rows that no token has.
-template <typename T, typename G, int VEC>
-__global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedGradArgs a, Sorted s, int lanes, int64_t column_items, int64_t tile_blocks,
-                                                             int64_t block0)
+// A group of lanes has a part of the workgroup's tile, s.part places, and lanes * VEC columns.  A run within a part is stored; what
+// crosses parts is put together in LDS, and what crosses the tile's ends goes to the workspace.
+template <typename T, typename G, int VEC, bool ADD>
+__global__ __launch_bounds__(kThreads) void embed_sum_kernel(EmbedGradArgs a, Sorted s, int lanes, int64_t column_items, int64_t block0)
 {
     constexpr int kAhead = 8;
-    const int64_t block = block0 + blockIdx.x;
-    if (block >= tile_blocks) {
-        const Place at = place_of<VEC>(lanes, column_items, block - tile_blocks);
-        if (at.c >= a.D) return;
-        const int64_t first = piece_first<VEC>(at.c, a.D), v0 = at.item * kClearRows;
-        const float none[VEC] = {};
-#pragma unroll 4
-        for (int i = 0; i < kClearRows; ++i) {
-            const int64_t v = v0 + i;
-            if (v < a.V && s.start[v] == s.start[v + 1]) store_row<G, VEC>(a, v, first, 0, none);
-        }
-        return;
-    }
-    const Place at = place_of<VEC>(lanes, column_items, block);
-    const int64_t p0 = at.item * s.tile, used = s.start[a.V];
-    if (p0 >= used || at.c >= a.D) return;
-    const int64_t p1 = min(p0 + s.tile, used), first = piece_first<VEC>(at.c, a.D);
-    const int shared = (int)(at.c - first);
+    enum { kHead = 1, kThrough = 2, kTail = 4 };  // of a part: a run that began before it, which goes on behind it; one that begins in it and goes on
+    __shared__ float heads[VEC * kThreads], tails[VEC * kThreads];
+    __shared__ int marks[kThreads];
+    const int sub = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kThreads / lanes;
+    const int64_t block = block0 + blockIdx.x, tile = block / column_items;
+    const int64_t c = ((block - tile * column_items) * lanes + sub) * VEC;
+    const int64_t p0 = tile * s.tile + group * s.part, used = s.start[a.V];
+    const bool there = c < a.D;
+    const int64_t first = there ? piece_first<VEC>(c, a.D) : 0, p1 = min(p0 + s.part, used);
+    const int shared = (int)(c - first);
     const T* __restrict__ dout = static_cast<const T*>(a.dout) + first;
-    float* __restrict__ part = s.parts + at.item * 2 * a.D + first;
-    float sum[VEC];
+    int mark = 0;
+    int32_t last_run = 0;
+    if (p0 < used) {
+        float sum[VEC];
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
-    int32_t run = s.key[p0];
-    bool open = s.start[run] < p0;  // the run began in front of the tile
-    const auto keep = [&](int which) {
+        for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
+        bool open = p0 > 0 && s.key[p0 - 1] == s.key[p0];
+        for (int64_t p = p0; p < p1; p += kAhead) {
+            // the tokens of the places, and whether their runs go on behind them
+            int32_t id[kAhead + 1];
+            Columns<T, VEC> x[kAhead];
+            GradPiece<G, VEC> was[kAhead];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) part[which * a.D + i] = sum[i];
-    };
-    for (int64_t p = p0; p < p1; p += kAhead) {
-        int32_t id[kAhead];
-        Columns<T, VEC> x[kAhead];
+            for (int u = 0; u <= kAhead; ++u) id[u] = s.key[min(p + u, used - 1)];
+            if (p + kAhead >= used) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int64_t q = min(p + u, p1 - 1);
-            id[u] = s.key[q];
-            x[u].load(dout + s.order[q] * a.ldd);
-        }
+                for (int u = 0; u <= kAhead; ++u) id[u] = p + u < used ? id[u] : -1;
+            }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (p + u >= p1) break;
-            if (id[u] != run) {
-                if (open) keep(0);
-                else store_row<G, VEC>(a, run, first, shared, sum);
+            for (int u = 0; u < kAhead; ++u) {
+                x[u].stream_load(dout + s.order[min(p + u, p1 - 1)] * a.ldd);
+                // (not only where a run ends: a branch would wait for each)
+                if (ADD) was[u].load(static_cast<const G*>(a.dweights) + (id[u] >= 0 ? id[u] : id[0]) * a.ldw + first);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (p + u >= p1) break;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum[i] += x[u].v[i];
+                const bool ends = id[u] != id[u + 1];
+                if (!ends && p + u + 1 < p1) continue;
+                last_run = id[u];
+                if (open || !ends) {
+                    float* const to = open ? heads : tails;
+                    mark |= open ? (ends ? kHead : kHead | kThrough) : kTail;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) to[i * kThreads + threadIdx.x] = sum[i];
+                } else if (there) {
+                    store_row<ADD>(a, id[u], first, shared, sum, was[u]);
+                }
                 open = false;
-                run = id[u];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
             }
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) sum[i] += x[u].v[i];
         }
     }
-    if (open) keep(0);
-    else if (s.start[run + 1] > p1) keep(1);
-    else store_row<G, VEC>(a, run, first, shared, sum);
+    if (sub == 0) marks[group] = mark;
+    __syncthreads();
+    // the run that goes on behind this part, or, in the first, that began before the tile
+    const bool before = group == 0 && (mark & kHead);
+    for (int which = before ? 0 : 1; which < 2; ++which) {
+        if (which == 1 && !(mark & kTail)) break;
+        float sum[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum[i] = (which ? tails : heads)[i * kThreads + threadIdx.x];
+        bool goes_on = which == 1 || (mark & kThrough);
+        for (int g = group + 1; goes_on && g < groups; ++g) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] += heads[i * kThreads + g * lanes + sub];
+            goes_on = marks[g] & kThrough;
+        }
+        if (!there) continue;
+        GradPiece<G, VEC> piece;
+        if (which == 0 || goes_on) {
+            GradPiece<float, VEC> part;
+            part.set(1.0f, sum);
+            part.store(s.parts + (tile * 2 + which) * a.D + first);
+        } else {
+            if (ADD) piece.load(static_cast<const G*>(a.dweights) + last_run * a.ldw + first);
+            store_row<ADD>(a, last_run, first, shared, sum, piece);
+        }
+    }
 }
 
-// The runs that begin in a tile and go on behind it.
-template <typename G, int VEC>
-__global__ __launch_bounds__(kThreads) void embed_join_kernel(EmbedGradArgs a, Sorted s, int lanes, int64_t column_items, int64_t block0)
+constexpr int kJoinThreads = 1024, kFewTiles = 8;
+
+// The runs that begin in a tile and go on behind it: a group of lanes has one, and lanes * VEC of its columns, and a whole workgroup,
+// whose groups share the tiles, each of its longer ones (a token that is half of a batch).  Behind these workgroups, which wait more
+// than they work, come those that clear the rows that no token has.
+template <typename G, int VEC, bool ADD>
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedGradArgs a, Sorted s, Clearing clearing, int lanes, int64_t column_items,
+                                                                  int64_t join_blocks, int64_t block0)
 {
-    const Place at = place_of<VEC>(lanes, column_items, block0 + blockIdx.x);
-    const int64_t p0 = at.item * s.tile, p1 = p0 + s.tile, used = s.start[a.V];
-    if (p1 >= used || at.c >= a.D) return;
-    const int32_t run = s.key[p1 - 1];
-    if (s.start[run] < p0 || s.start[run + 1] <= p1) return;
-    const int64_t first = piece_first<VEC>(at.c, a.D), last = (s.start[run + 1] - 1) / s.tile;
-    const float* __restrict__ part = s.parts + at.item * 2 * a.D + first;
-    float sum[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) sum[i] = part[a.D + i];
-#pragma unroll 4
-    for (int64_t t = at.item + 1; t <= last; ++t) {
-        const float* __restrict__ more = s.parts + t * 2 * a.D + first;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) sum[i] += more[i];
+    __shared__ float shares[kJoinThreads * VEC];
+    __shared__ int32_t longer[kJoinThreads];
+    __shared__ int many;
+    const int64_t block = block0 + blockIdx.x;
+    if (block >= join_blocks) {
+        constexpr int kRows = kClearRows / (kJoinThreads / 64);
+        const int64_t v0 = (block - join_blocks) * kClearRows + (threadIdx.x >> 6) * kRows;
+        const int64_t v = v0 + (threadIdx.x & 63);
+        uint64_t rows = __ballot((threadIdx.x & 63) < kRows && v < a.V && !cleared_early(v) && s.start[v] == s.start[v + 1]);
+        for (; rows; rows &= rows - 1) clear_row(clearing, v0 + __builtin_ctzll(rows));
+        return;
     }
-    store_row<G, VEC>(a, run, first, (int)(at.c - first), sum);
+    const int sub = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
+    const int64_t used = s.start[a.V];
+    if (threadIdx.x == 0) many = 0;
+    __syncthreads();
+    // what group g of the workgroup has: a tile and columns; the run and the last tile it is in, -1 for none
+    struct Item {
+        int64_t tile, c, last;
+        int32_t run;
+    };
+    const auto item_of = [&](int g) {
+        // (a long run's columns are different workgroups')
+        const int64_t item = block * groups + g, columns = item / (s.tiles - 1);
+        Item it;
+        it.tile = item - columns * (s.tiles - 1);
+        it.c = (columns * lanes + sub) * VEC;
+        it.last = -1;
+        it.run = 0;
+        const int64_t p0 = it.tile * s.tile, p1 = p0 + s.tile;
+        if (p1 >= used) return it;
+        const int32_t next = s.key[p1], before = s.key[p0 > 0 ? p0 - 1 : 0];
+        it.run = s.key[p1 - 1];
+        if (next != it.run || (p0 > 0 && before == it.run)) return it;
+        it.last = ((int64_t)s.start[it.run + 1] - 1) / s.tile;
+        return it;
+    };
+    // the part that the run's first tile ends with, then those that the others begin with: every `step`th from the `from`th
+    const auto add_parts = [&](const Item& it, int64_t first, int from, int step, float (&sum)[VEC]) {
+#pragma unroll 8
+        for (int64_t t = it.tile + from; t <= it.last; t += step) {
+            GradPiece<float, VEC> more;
+            more.load(s.parts + (t * 2 + (t == it.tile ? 1 : 0)) * a.D + first);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] += more.part[i / more.kPart].v[i % more.kPart];
+        }
+    };
+    const auto finish = [&](const Item& it, int64_t first, const float (&sum)[VEC]) {
+        GradPiece<G, VEC> was;
+        if (ADD) was.load(static_cast<const G*>(a.dweights) + it.run * a.ldw + first);
+        store_row<ADD>(a, it.run, first, (int)(it.c - first), sum, was);
+    };
+    const Item own = item_of(group);
+    if (own.last >= own.tile + kFewTiles) {
+        if (sub == 0) longer[atomicAdd(&many, 1)] = group;  // (in any order: each is summed up by itself)
+    } else if (own.last >= 0 && own.c < a.D) {
+        const int64_t first = piece_first<VEC>(own.c, a.D);
+        float sum[VEC] = {};
+        add_parts(own, first, 0, 1, sum);
+        finish(own, first, sum);
+    }
+    __syncthreads();
+    for (int l = 0; l < many; ++l) {
+        const Item it = item_of(longer[l]);
+        const bool there = it.c < a.D;
+        const int64_t first = there ? piece_first<VEC>(it.c, a.D) : 0;
+        float sum[VEC] = {};
+        if (there) add_parts(it, first, group, groups, sum);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) shares[i * kJoinThreads + threadIdx.x] = sum[i];
+        __syncthreads();
+        // halves of the groups are added until one is left
+        for (int half = groups / 2; half > 0; half /= 2) {
+            if (group < half) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) shares[i * kJoinThreads + threadIdx.x] += shares[i * kJoinThreads + threadIdx.x + half * lanes];
+            }
+            __syncthreads();
+        }
+        if (group == 0 && there) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] = shares[i * kJoinThreads + threadIdx.x];
+            finish(it, first, sum);
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T, int VEC, int TOKENS>
+hipError_t embed_tokens(const EmbedArgs& a, const Spread& sp, hipStream_t s)
+{
+    return launch_parts(blocks_of(sp, (a.T + TOKENS - 1) / TOKENS), kThreads, [&](unsigned grid, int64_t block0) {
+        embed_kernel<T, VEC, TOKENS><<<grid, kThreads, 0, s>>>(a, sp.lanes, sp.column_items, block0);
+    });
 }
 
 template <typename T, int VEC>
 hipError_t embed(const EmbedArgs& a, hipStream_t s)
 {
     const Spread sp = spread<VEC>(a.D);
-    return launch_parts(blocks_of(sp, a.T), kThreads, [&](unsigned grid, int64_t block0) {
-        embed_kernel<T, VEC><<<grid, kThreads, 0, s>>>(a, sp.lanes, sp.column_items, block0);
-    });
+    // two tokens to a group where that leaves wavefronts enough for the chip (16,384 by 2,048, bf16: 27.8 us with one, 25.8, 26.7 with
+    // four)
+    return blocks_of(sp, a.T) >= 2048 ? embed_tokens<T, VEC, 2>(a, sp, s) : embed_tokens<T, VEC, 1>(a, sp, s);
 }
 
-template <typename T, typename G, int VEC>
+template <typename T, typename G, int VEC, bool ADD>
 hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
 {
-    const Sorted st = sorted_view(a.workspace, a.T, a.V, a.D);
+    const Spread sp = spread<VEC>(a.D);
+    const Sorted st = sorted_view(a.workspace, a.T, a.V, a.D, kThreads / sp.lanes);
+    // 512 ranges, or, with so many tokens that looking at them all counts, 256 (us of the gradient, 512 and 256: 16,384 tokens, 65,536
+    // rows of 2,048 78.5, 81.7; 65,536 tokens, 32,000 rows of 512 83.5, 72.7)
+    const int64_t ranges = a.T < 32768 ? 512 : 256;
     int ids_of = 1;
-    while (ids_of < kMostIds && (int64_t)ids_of * 512 < a.V) ids_of *= 2;
+    while (ids_of < kMostIds && ids_of * ranges < a.V) ids_of *= 2;
+    const int64_t halves = sizeof(G) / 2;
+    const Clearing clearing = {ADD ? nullptr : static_cast<uint16_t*>(a.dweights), a.D * halves, a.ldw * halves};
     hipError_t err = launch_parts((a.V + ids_of - 1) / ids_of, kSortThreads, [&](unsigned grid, int64_t block0) {
-        embed_sort_kernel<<<grid, kSortThreads, kSortWaves * ids_of * 4, s>>>(a.ids, a.T, a.V, ids_of, st.start, st.key, st.order, block0);
+        embed_sort_kernel<<<grid, kSortThreads, kSortWaves * ids_of * 4, s>>>(a.ids, a.T, a.V, ids_of, st.start, st.key, st.order, clearing, block0);
     });
     if (err != hipSuccess) return err;
-    const Spread sp = spread<VEC>(a.D);
-    const int64_t tile_blocks = blocks_of(sp, st.tiles);
-    const int64_t clearing = a.accumulate ? 0 : blocks_of(sp, (a.V + kClearRows - 1) / kClearRows);
-    err = launch_parts(tile_blocks + clearing, kThreads, [&](unsigned grid, int64_t block0) {
-        embed_sum_kernel<T, G, VEC><<<grid, kThreads, 0, s>>>(a, st, sp.lanes, sp.column_items, tile_blocks, block0);
+    err = launch_parts(st.tiles * sp.column_items, kThreads, [&](unsigned grid, int64_t block0) {
+        embed_sum_kernel<T, G, VEC, ADD><<<grid, kThreads, 0, s>>>(a, st, sp.lanes, sp.column_items, block0);
     });
-    if (err != hipSuccess || st.tiles < 2) return err;
-    return launch_parts(blocks_of(sp, st.tiles - 1), kThreads, [&](unsigned grid, int64_t block0) {
-        embed_join_kernel<G, VEC><<<grid, kThreads, 0, s>>>(a, st, sp.lanes, sp.column_items, block0);
+    if (err != hipSuccess) return err;
+    const int64_t groups = kJoinThreads / sp.lanes, joins = st.tiles > 1 ? ((st.tiles - 1) * sp.column_items + groups - 1) / groups : 0;
+    return launch_parts(joins + (ADD ? 0 : (a.V + kClearRows - 1) / kClearRows), kJoinThreads, [&](unsigned grid, int64_t block0) {
+        embed_join_kernel<G, VEC, ADD><<<grid, kJoinThreads, 0, s>>>(a, st, clearing, sp.lanes, sp.column_items, joins, block0);
     });
 }
 
@@ -338,17 +571,23 @@ hipError_t embed_by_width(const EmbedArgs& a, hipStream_t s)
     return a.D >= Piece<T>::kCount ? embed<T, Piece<T>::kCount>(a, s) : embed<T, 1>(a, s);
 }
 
+template <typename T, typename G>
+hipError_t grad_by_width(const EmbedGradArgs& a, hipStream_t s)
+{
+    constexpr int kVec = Piece<T>::kCount;
+    if (a.accumulate) return a.D >= kVec ? embed_grad<T, G, kVec, true>(a, s) : embed_grad<T, G, 1, true>(a, s);
+    return a.D >= kVec ? embed_grad<T, G, kVec, false>(a, s) : embed_grad<T, G, 1, false>(a, s);
+}
+
 template <typename T>
 hipError_t grad_by_type(const EmbedGradArgs& a, hipStream_t s)
 {
-    constexpr int kVec = Piece<T>::kCount;
-    if (a.grad_dtype == a.dtype) return a.D >= kVec ? embed_grad<T, T, kVec>(a, s) : embed_grad<T, T, 1>(a, s);
-    return a.D >= kVec ? embed_grad<T, float, kVec>(a, s) : embed_grad<T, float, 1>(a, s);
+    return a.grad_dtype == a.dtype ? grad_by_width<T, T>(a, s) : grad_by_width<T, float>(a, s);
 }
 
 }  // namespace
 
-int64_t embed_grad_workspace_bytes(int64_t T, int64_t V, int64_t D) { return sorted_view(nullptr, T, V, D).bytes; }
+int64_t embed_grad_workspace_bytes(int64_t T, int64_t V, int64_t D) { return sorted_view(nullptr, T, V, D, 4).bytes; }
 
 hipError_t launch_embed(const EmbedArgs& a, hipStream_t s)
 {

@@ -78,8 +78,10 @@ def test_gradient(T, V, D, kind, dtype, grad_dtype):
     assert not torch.signbit(grad[(tokens[:, 0] == 0).cuda()]).any()
 
 
-# more tokens than 1,024 tiles of 32 hold, so that tiles are longer; more ids than 512 ranges of 512
-@pytest.mark.parametrize("T,V,D,kind", [(40_000, 300, 24, "skewed"), (70_001, 3, 8, "uniform"), (200, 300_001, 16, "skewed")])
+# more tokens than 1,024 tiles (of rows of 2,048, and fewer of longer ones) of 8 hold, so that tiles are longer; more ids than 512 ranges
+# of 512; tokens of which one id's fill most tiles
+@pytest.mark.parametrize("T,V,D,kind", [(9_000, 40, 2_056, "skewed"), (20_000, 9, 2_050, "one"), (40_000, 300, 24, "skewed"), (70_001, 3, 8, "uniform"),
+                                        (200, 300_001, 16, "skewed"), (33_000, 70_000, 40, "skewed")])
 def test_gradient_of_many(T, V, D, kind):
     ids, d = draw_ids(kind, T, V), random(5, T, D)
     grad, ws = filled(torch.float32, V, D), workspace(T, V, D)

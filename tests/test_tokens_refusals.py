@@ -102,10 +102,11 @@ def test_products(changes, text):
 def test_sizes_of_workspaces():
     assert binding.sgap_route_balance_workspace_size(0, 8, 2, 1) > 0
     assert binding.sgap_embed_grad_workspace_size(0, 1, 0) >= 8
-    # start, key and order, and two rows of floats for each of 64 tiles of 32 tokens
+    # start, key and order, and two rows of floats for each of 64 tiles of four times 8 tokens
     assert binding.sgap_embed_grad_workspace_size(2048, 1000, 64) == 4096 + 8192 + 8192 + 64 * 2 * 64 * 4
-    # 1,024 tiles at most, however many the tokens
-    assert binding.sgap_embed_grad_workspace_size(1 << 20, 1, 256) == 256 + 2 * (4 << 20) + 1024 * 2 * 256 * 4
+    # 256 tiles at most, or 2^19 numbers, however many the tokens
+    assert binding.sgap_embed_grad_workspace_size(1 << 20, 1, 256) == 256 + 2 * (4 << 20) + 2048 * 2 * 256 * 4
+    assert binding.sgap_embed_grad_workspace_size(1 << 20, 1, 4096) == 256 + 2 * (4 << 20) + 256 * 2 * 4096 * 4
     with pytest.raises(binding.SgapError):
         binding.sgap_embed_grad_workspace_size(4, 0, 8)
     with pytest.raises(binding.SgapError):
