@@ -37,22 +37,44 @@ __device__ __forceinline__ float over_lanes_sum(float v)
     return v;
 }
 
-// V neighbouring experts of a row from e0 on, -infinity behind the last
-template <typename T, int V>
-__device__ __forceinline__ void load_experts(const T* __restrict__ row, int e0, int E, float (&x)[V])
-{
-    if constexpr (V > 1) {
-        typedef T loose __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-        if (e0 + V <= E) {
-            const loose v = *reinterpret_cast<const loose*>(row + e0);
+// V neighbouring experts' numbers of a row from e0 on, as they lie in memory.  FULL: E is a multiple of V, so that a lane has all of
+// them or none.  Either way without a branch, so that all that a row needs is on its way together; what is behind the last expert is
+// the row's first or last.
+template <typename T, int V, bool FULL>
+struct Experts {
+    typedef T loose __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+    T v[V];
+    __device__ __forceinline__ void load(const T* __restrict__ row, int e0, int E)
+    {
+        if constexpr (FULL && V > 1) {
+            const loose x = *reinterpret_cast<const loose*>(row + (e0 < E ? e0 : 0));
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = (float)v[i];
-            return;
+            for (int i = 0; i < V; ++i) v[i] = x[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = row[min(e0 + i, E - 1)];
         }
     }
+    // logits: -infinity behind the last
+    __device__ __forceinline__ void numbers(float (&x)[V], int e0, int E) const
+    {
 #pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = e0 + v < E ? (float)row[e0 + v] : -__builtin_inff();
-}
+        for (int i = 0; i < V; ++i) x[i] = e0 + i < E ? (float)v[i] : -__builtin_inff();
+    }
+    static __device__ __forceinline__ void store(T* __restrict__ row, int e0, int E, const float (&x)[V])
+    {
+        if constexpr (FULL && V > 1) {
+            loose o;
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = (T)x[i];
+            if (e0 < E) *reinterpret_cast<loose*>(row + e0) = o;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (e0 + i < E) row[e0 + i] = (T)x[i];
+        }
+    }
+};
 
 // x becomes the softmax of the row that LANES lanes hold; a row of which nothing is left becomes zeros, one with NaN or
 // +infinity NaN (of a maximum that passes NaN by, the exponentials still are).
@@ -82,18 +104,18 @@ __device__ __forceinline__ bool any_choice(int32_t mine)
     return LANES == 64 ? who != 0 : (who >> (lane & 48) & 0xffff) != 0;
 }
 template <int LANES>
-__device__ __forceinline__ int32_t choice_of(const int32_t* __restrict__ experts, int64_t t, int k, int E, bool row)
+__device__ __forceinline__ int32_t choice_of(const int32_t* __restrict__ experts, int64_t t, int k, int E)
 {
     const int sub = threadIdx.x & (LANES - 1);
-    const int32_t e = row && sub < k ? experts[t * k + sub] : -1;
-    return e < E ? e : -1;
+    const int32_t e = experts[t * k + min(sub, k - 1)];
+    return (int)(sub < k) & (int)(e < E) ? e : -1;  // (&&: a branch, and a wait for each row's)
 }
 
 // f - 1 of an expert of a sequence with n > 0 tokens
-__device__ __forceinline__ float over_even(int32_t count, int32_t n, int E, int k)
+// (whole numbers below 2^42, which 64-bit floats hold; even: k n, by: one over it)
+__device__ __forceinline__ float over_even(int32_t count, double even, float by, int E)
 {
-    const int64_t even = (int64_t)k * n;
-    return (float)((int64_t)count * E - even) / (float)even;
+    return (float)__builtin_fma((double)count, (double)E, -even) * by;
 }
 
 // What the tiles leave for the second launch: p's sums, pairs by expert, rows that chose.
@@ -123,7 +145,7 @@ Partial partial_view(char* workspace, int64_t T, int64_t E, int64_t S)
     return p;
 }
 
-template <typename T, int LANES, int V>
+template <typename T, int LANES, int V, bool FULL>
 __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, Partial p, int64_t block0)
 {
     constexpr int kGroups = kThreads / LANES;
@@ -139,20 +161,32 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
     float sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.0f;
-#pragma unroll 2
-    for (int i = 0; i < kRows / kGroups; ++i) {
-        const int r = i * kGroups + group;
-        const int64_t t = tile.first + r;
-        const bool row = r < tile.rows;
-        const int32_t e = choice_of<LANES>(a.experts, t, a.k, a.E, row);
-        if (e >= 0) atomicAdd(&counts[e], 1);
-        if (!any_choice<LANES>(e)) continue;
-        if (sub == 0) atomicAdd(&rows, 1);
-        float x[V];
-        load_experts<T, V>(static_cast<const T*>(a.logits) + t * a.ld, sub * V, a.E, x);
-        softmax<LANES, V>(x);
+    constexpr int kTurns = kRows / kGroups, kAtOnce = V * kTurns > 64 ? 64 / V : kTurns;  // a group's rows; on their way together
+    static_assert(kTurns % kAtOnce == 0, "");
+#pragma unroll 1
+    for (int i0 = 0; i0 < kTurns; i0 += kAtOnce) {
+        int32_t e[kAtOnce];
+        Experts<T, V, FULL> x[kAtOnce];
 #pragma unroll
-        for (int v = 0; v < V; ++v) sum[v] += x[v];
+        for (int i = 0; i < kAtOnce; ++i) {
+            // (in place of a row past the last, that one; it is not counted)
+            const int r = (i0 + i) * kGroups + group;
+            const int64_t t = tile.first + min(r, tile.rows - 1);
+            e[i] = choice_of<LANES>(a.experts, t, a.k, a.E);
+            if (r >= tile.rows) e[i] = -1;
+            x[i].load(static_cast<const T*>(a.logits) + t * a.ld, sub * V, a.E);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (e[i] >= 0) atomicAdd(&counts[e[i]], 1);
+            if (!any_choice<LANES>(e[i])) continue;
+            if (sub == 0) atomicAdd(&rows, 1);
+            float p[V];
+            x[i].numbers(p, sub * V, a.E);
+            softmax<LANES, V>(p);
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[v] += p[v];
+        }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) sums[group][sub * V + v] = sum[v];
@@ -198,8 +232,23 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
     float s = 0.0f;
     int32_t c = 0;
     if (line < lines) {
-#pragma unroll 8
-        for (int64_t t = first + line; t < end; t += lines) {
+        int64_t t = first + line;
+        constexpr int kAtOnce = 16;
+        for (; t + (kAtOnce - 1) * lines < end; t += kAtOnce * lines) {
+            float more[kAtOnce];
+            int32_t pairs[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                more[i] = p.sums[(t + i * lines) * a.E + e];
+                pairs[i] = p.counts[(t + i * lines) * a.E + e];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                s += more[i];
+                c += pairs[i];
+            }
+        }
+        for (; t < end; t += lines) {
             s += p.sums[t * a.E + e];
             c += p.counts[t * a.E + e];
         }
@@ -217,7 +266,8 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
             c += counts[i * a.E + e];
         }
         a.counts[seq * a.E + e] = c;
-        if (n > 0) loss = (1.0f + over_even(c, n, a.E, a.k)) * (s / (float)n);
+        const double even = (double)a.k * n;
+        if (n > 0) loss = (1.0f + over_even(c, even, 1.0f / (float)even, a.E)) * (s / (float)n);
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) loss += __shfl_xor(loss, d);
@@ -265,22 +315,33 @@ __global__ __launch_bounds__(kThreads) void balance_mean_kernel(BalanceArgs a, P
     }
 }
 
-template <typename T, int LANES, int V>
+// SEQUENCES: there are segments.
+template <typename T, int LANES, int V, bool FULL, bool SEQUENCES>
 __global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs a, int64_t row_blocks)
 {
     constexpr int kGroups = kThreads / LANES;
-    const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES;
-    const int used = sequences_used<kThreads>(a.rows, a.S);
+    const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES, e0 = sub * V;
+    Experts<int32_t, V, FULL> count;
+    int32_t n = 0;
+    if (!SEQUENCES) {
+        count.load(a.counts, e0, a.E);
+        n = a.rows[0];
+    }
     const float dloss = a.dloss[0];
+    const int used = SEQUENCES ? sequences_used<kThreads>(a.rows, a.S) : 1;
     int64_t of = -1;  // the sequence whose f are held
     float f[V], scale = 0.0f;
     for (int64_t b = blockIdx.x; b < row_blocks; b += gridDim.x) {
         const int64_t t = b * kGroups + group;
         if (t >= a.T) continue;
-        const int32_t e = choice_of<LANES>(a.experts, t, a.k, a.E, true);
+        Experts<T, V, FULL> held, was;
+        held.load(static_cast<const T*>(a.logits) + t * a.ld, e0, a.E);
+        const int32_t e = choice_of<LANES>(a.experts, t, a.k, a.E);
+        T* const out = static_cast<T*>(a.dlogits) + t * a.ldd;
+        if (a.accumulate) was.load(out, e0, a.E);
         int64_t seq = 0;
-        bool there = any_choice<LANES>(e);
-        if (a.segments) {
+        bool there = true;
+        if (SEQUENCES) {
             // the last sequence that begins at t or before it
             int64_t lo = 0, hi = a.S;
             while (lo < hi) {
@@ -288,49 +349,38 @@ __global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs 
                 if (a.segments[mid] <= t) lo = mid + 1;
                 else hi = mid;
             }
-            seq = lo - 1;
-            there = there && seq >= 0 && t < a.segments[seq + 1];
+            there = lo > 0 && t < a.segments[lo];
+            seq = lo > 0 ? lo - 1 : 0;
         }
-        const int32_t n = there ? a.rows[seq] : 0;
-        there = there && n > 0 && used > 0;
-        T* const out = static_cast<T*>(a.dlogits) + t * a.ldd;
+        if (seq != of) {
+            of = seq;
+            if (SEQUENCES) {
+                count.load(a.counts + seq * a.E, e0, a.E);
+                n = a.rows[seq];
+            }
+            const double even = (double)a.k * n;
+            const float by = n > 0 ? 1.0f / (float)even : 0.0f;
+            scale = n > 0 && used > 0 ? dloss / ((float)used * (float)n) : 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) f[v] = e0 + v < a.E ? over_even(count.v[v], even, by, a.E) : 0.0f;
+        }
+        there = any_choice<LANES>(e) && there && n > 0 && used > 0;
         if (!there && a.accumulate) continue;
         float x[V];
         if (there) {
-            if (seq != of) {
-                of = seq;
-                scale = dloss / ((float)used * (float)n);
-#pragma unroll
-                for (int v = 0; v < V; ++v) f[v] = sub * V + v < a.E ? over_even(a.counts[seq * a.E + sub * V + v], n, a.E, a.k) : 0.0f;
-            }
-            load_experts<T, V>(static_cast<const T*>(a.logits) + t * a.ld, sub * V, a.E, x);
+            held.numbers(x, e0, a.E);
             softmax<LANES, V>(x);
             float inner = 0.0f;
 #pragma unroll
             for (int v = 0; v < V; ++v) inner = __builtin_fmaf(f[v], x[v], inner);
             inner = over_lanes_sum<LANES>(inner);
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = scale * x[v] * (f[v] - inner);
+            for (int v = 0; v < V; ++v) x[v] = scale * x[v] * (f[v] - inner) + (a.accumulate ? (float)was.v[v] : 0.0f);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) x[v] = 0.0f;
         }
-        if (V > 1 && sub * V + V <= a.E) {
-            typedef T loose __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-            loose o;
-            if (a.accumulate) {
-                const loose was = *reinterpret_cast<const loose*>(out + sub * V);
-#pragma unroll
-                for (int v = 0; v < V; ++v) x[v] += (float)was[v];
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) o[v] = (T)x[v];
-            *reinterpret_cast<loose*>(out + sub * V) = o;
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (sub * V + v < a.E) out[sub * V + v] = (T)(a.accumulate ? (float)out[sub * V + v] + x[v] : x[v]);
-        }
+        held.store(out, e0, a.E, x);
     }
 }
 
@@ -353,8 +403,10 @@ hipError_t balance(const BalanceArgs& a, hipStream_t s)
 {
     const Partial p = partial_view(a.workspace, a.T, a.E, a.S);
     hipError_t err = by_experts(a.E, [&](auto lanes, auto v) {
+        constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
         return launch_parts(most_row_tiles(a.S, a.T, kRows, a.segments != nullptr), kThreads, [&](unsigned grid, int64_t block0) {
-            balance_tiles_kernel<T, decltype(lanes)::value, decltype(v)::value><<<grid, kThreads, 0, s>>>(a, p, block0);
+            if (a.E % V == 0) balance_tiles_kernel<T, L, V, true><<<grid, kThreads, 0, s>>>(a, p, block0);
+            else balance_tiles_kernel<T, L, V, false><<<grid, kThreads, 0, s>>>(a, p, block0);
         });
     });
     if (err != hipSuccess) return err;
@@ -373,7 +425,14 @@ hipError_t balance_grad(const BalanceGradArgs& a, hipStream_t s)
         constexpr int kGroups = kThreads / decltype(lanes)::value;
         const int64_t row_blocks = (a.T + kGroups - 1) / kGroups;
         const unsigned grid = (unsigned)(row_blocks < 2048 ? row_blocks : 2048);
-        balance_grad_kernel<T, decltype(lanes)::value, decltype(v)::value><<<grid, kThreads, 0, s>>>(a, row_blocks);
+        constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
+        if (a.E % V == 0) {
+            if (a.segments) balance_grad_kernel<T, L, V, true, true><<<grid, kThreads, 0, s>>>(a, row_blocks);
+            else balance_grad_kernel<T, L, V, true, false><<<grid, kThreads, 0, s>>>(a, row_blocks);
+        } else {
+            if (a.segments) balance_grad_kernel<T, L, V, false, true><<<grid, kThreads, 0, s>>>(a, row_blocks);
+            else balance_grad_kernel<T, L, V, false, false><<<grid, kThreads, 0, s>>>(a, row_blocks);
+        }
         return hipGetLastError();
     });
 }
