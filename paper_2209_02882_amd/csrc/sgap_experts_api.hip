@@ -48,7 +48,7 @@ int check_grouped(int64_t G, int64_t R, int64_t K, int64_t N, const int32_t* off
         return invalid("dimension exceeds int32 index range: R, K and N are at most 2^31 - 65536");
     if (!offsets && G != 1) return invalid("offsets may be null for one group only");
     if (src_div < 1 || src_div > kMaxIndex) return invalid("src_div must be positive");
-    if (!src && src_div != 1) return invalid("src_div needs src");
+    if (!src && src_div != 1 && R > 0) return invalid("src_div needs src");
     if (!src && x_rows < R) return invalid("X has fewer rows than the product");
     if (ldx < K) return invalid("ldx is less than a row");
     if (ldy < N) return invalid("ldy is less than a row");

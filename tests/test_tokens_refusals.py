@@ -122,6 +122,9 @@ def test_empty_calls_launch_nothing():
     assert lib.sgap_f8_rows(*{**ROWS, "R": 0, "X": None}.values()) == 0
     assert lib.sgap_f8_weights(*{**WEIGHTS, "N": 0, "W": None}.values()) == 0
     assert lib.sgap_grouped_mm_f8(*{**MM, "R": 0, "X": None, "Y": None}.values()) == 0
+    # a list of no rows has no address
+    assert lib.sgap_grouped_mm_f8(*{**MM, "R": 0, "x_rows": 0, "src_div": 2, "X": None, "Y": None}.values()) == 0
+    assert lib.sgap_grouped_mm(4, 0, 16, 24, 2, P, None, 16, 0, None, 2, P, 0, None, 24, None) == 0
     assert lib.sgap_grouped_mm_f8(*{**MM, "N": 0, "W": None, "Y": None}.values()) == 0
 
 
