@@ -7,8 +7,10 @@
 //
 // A row is held by 16 lanes (up to 256 experts) or by a wavefront, some neighbouring experts to a lane, which keeps the sums of
 // its own experts over the rows that it sees.  Tiles of rows never cross a sequence; a second launch sums up a sequence's tiles,
-// a third the sequences where there is more than one.  The logits are read once each way (4 MB for 16,384 tokens and 128 experts
-// in bf16, which no launch waits for): what is left is the launches.  Sums of floats in a fixed order; the only atomics count
+// a third the sequences, or a sequence's parts, where there is more than one.  The logits are read once each way (4 MB for 16,384 tokens and 128 experts
+// in bf16, which no launch waits for): what is left is the launches, 15.2 us both ways in a row of passes, where three empty ones
+// take 10.  From about 300 experts on it is the exponentials and sums of the vector unit and the bytes: 65,536 rows of 512 in bf16,
+// 67 MB, 23 us forth and 28 us for the gradient, 201 MB in all at 3.9 TB/s.  Sums of floats in a fixed order; the only atomics count
 // whole numbers in LDS.
 #include "sgap_grouped.hpp"
 #include "sgap_tokens.hpp"
@@ -22,73 +24,112 @@ constexpr int kRows = 64;           // of a tile
 constexpr int kJoinThreads = 1024;  // of a sequence's sum
 constexpr int kMostExperts = 1024;
 
+// op over 16 lanes or all 64, the same bits in each: 16 lanes by turning them, then the two halves of each 32 and of the 64 changing
+// places.  (By way of LDS, as a shuffle goes, each step takes as long as a row's exponentials.)
+template <int LANES, typename F>
+__device__ __forceinline__ float over_lanes(float v, F&& op)
+{
+    const auto bits = [](float x) { return __builtin_bit_cast(int, x); };
+    const auto number = [](int x) { return __builtin_bit_cast(float, x); };
+    v = op(v, number(__builtin_amdgcn_update_dpp(0, bits(v), 0x128, 0xf, 0xf, true)));
+    v = op(v, number(__builtin_amdgcn_update_dpp(0, bits(v), 0x124, 0xf, 0xf, true)));
+    v = op(v, number(__builtin_amdgcn_update_dpp(0, bits(v), 0x122, 0xf, 0xf, true)));
+    v = op(v, number(__builtin_amdgcn_update_dpp(0, bits(v), 0x121, 0xf, 0xf, true)));
+    if constexpr (LANES == 64) {
+        const auto a = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
+        v = op(number(a[0]), number(a[1]));
+        const auto b = __builtin_amdgcn_permlane32_swap(bits(v), bits(v), false, false);
+        v = op(number(b[0]), number(b[1]));
+    }
+    return v;
+}
 template <int LANES>
 __device__ __forceinline__ float over_lanes_max(float v)
 {
-#pragma unroll
-    for (int d = LANES / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 template <int LANES>
 __device__ __forceinline__ float over_lanes_sum(float v)
 {
-#pragma unroll
-    for (int d = LANES / 2; d; d >>= 1) v += __shfl_xor(v, d);
-    return v;
+    return over_lanes<LANES>(v, [](float a, float b) { return a + b; });
 }
 
-// V neighbouring experts' numbers of a row from e0 on, as they lie in memory.  FULL: E is a multiple of V, so that a lane has all of
-// them or none.  Either way without a branch, so that all that a row needs is on its way together; what is behind the last expert is
-// the row's first or last.
-template <typename T, int V, bool FULL>
-struct Experts {
-    typedef T loose __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-    T v[V];
-    __device__ __forceinline__ void load(const T* __restrict__ row, int e0, int E)
+// A lane's experts of a row: pieces of P neighbouring ones, as they lie in memory, a piece of every lane and then the next of
+// every lane.  The last piece of a row whose length P does not divide reaches back into the one before, so that every load is
+// whole and in the row, without a branch: all that a row needs is on its way together.  What it has in common with the one before,
+// and what pieces behind the last expert hold (the row's first), is not this lane's own: it is neither summed nor counted.
+// (E is at least P.)  By elements, 17,403 rows of 184 took 46 us both ways in place of 18.
+constexpr int kMostPiece = 8;
+template <int LANES, int V>
+struct Held {
+    static constexpr int P = V < kMostPiece ? V : kMostPiece, kPieces = V / P;
+    int first[kPieces];  // expert that the piece begins with
+    int own[kPieces];    // its first element that is this lane's, P: none
+    __device__ __forceinline__ Held(int E)
     {
-        if constexpr (FULL && V > 1) {
-            const loose x = *reinterpret_cast<const loose*>(row + (e0 < E ? e0 : 0));
+        const int sub = threadIdx.x & (LANES - 1);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = x[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = row[min(e0 + i, E - 1)];
+        for (int h = 0; h < kPieces; ++h) {
+            const int e = (h * LANES + sub) * P, f = min(e, E - P);
+            own[h] = e < E ? e - f : P;
+            first[h] = e < E ? f : 0;
         }
     }
-    // logits: -infinity behind the last
-    __device__ __forceinline__ void numbers(float (&x)[V], int e0, int E) const
+    __device__ __forceinline__ bool has(int v) const { return v % P >= own[v / P]; }
+    __device__ __forceinline__ int expert(int v) const { return first[v / P] + v % P; }
+};
+template <typename T, int LANES, int V>
+struct Experts {
+    using H = Held<LANES, V>;
+    typedef T loose __attribute__((ext_vector_type(H::P), aligned(sizeof(T))));
+    loose piece[H::kPieces];
+    __device__ __forceinline__ void load(const T* __restrict__ row, const H& held)
     {
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = e0 + i < E ? (float)v[i] : -__builtin_inff();
+        for (int h = 0; h < H::kPieces; ++h) piece[h] = *reinterpret_cast<const loose*>(row + held.first[h]);
     }
-    static __device__ __forceinline__ void store(T* __restrict__ row, int e0, int E, const float (&x)[V])
+    __device__ __forceinline__ T operator[](int v) const
     {
-        if constexpr (FULL && V > 1) {
+        if constexpr (H::P == 1) return reinterpret_cast<const T&>(piece[v]);
+        else return piece[v / H::P][v % H::P];
+    }
+    // (two lanes that have an element both store the same)
+    static __device__ __forceinline__ void store(T* __restrict__ row, const H& held, const float (&x)[V])
+    {
+#pragma unroll
+        for (int h = 0; h < H::kPieces; ++h) {
             loose o;
+            if constexpr (H::P == 1) reinterpret_cast<T&>(o) = (T)x[h];
+            else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = (T)x[i];
-            if (e0 < E) *reinterpret_cast<loose*>(row + e0) = o;
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (e0 + i < E) row[e0 + i] = (T)x[i];
+                for (int i = 0; i < H::P; ++i) o[i] = (T)x[h * H::P + i];
+            }
+            if (held.own[h] < H::P) *reinterpret_cast<loose*>(row + held.first[h]) = o;
         }
     }
 };
 
-// x becomes the softmax of the row that LANES lanes hold; a row of which nothing is left becomes zeros, one with NaN or
+// x: the softmax of the row that LANES lanes hold; a row of which nothing is left becomes zeros, one with NaN or
 // +infinity NaN (of a maximum that passes NaN by, the exponentials still are).
-template <int LANES, int V>
-__device__ __forceinline__ void softmax(float (&x)[V])
+template <typename T, int LANES, int V>
+__device__ __forceinline__ void softmax(const Experts<T, LANES, V>& logits, const Held<LANES, V>& held, float (&x)[V])
 {
-    float m = x[0];
+    float m = -__builtin_inff();
 #pragma unroll
-    for (int v = 1; v < V; ++v) m = fmaxf(m, x[v]);
+    for (int v = 0; v < V; ++v) {
+        x[v] = (float)logits[v];
+        m = fmaxf(m, x[v]);
+    }
     m = over_lanes_max<LANES>(m);
     m = m == -__builtin_inff() ? 0.0f : m;
     float total = 0.0f;
 #pragma unroll
-    for (int v = 0; v < V; ++v) total += x[v] = expf(x[v] - m);
+    for (int v = 0; v < V; ++v) {
+        // (2^ by the instruction for it: the factor's rounding is another |x - m| 2^-24 of the result, as the difference's is, and what
+        // is below 2^-126 becomes 0.  With a function that does more, 65,536 rows of 512 in bf16 take 30 us in place of 23.)
+        x[v] = __builtin_amdgcn_exp2f((x[v] - m) * 1.44269504f);
+        total += held.has(v) ? x[v] : 0.0f;
+    }
     total = over_lanes_sum<LANES>(total);
     const float scale = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
@@ -123,8 +164,9 @@ struct Partial {
     float* sums;       // tiles x E
     int32_t* counts;   // tiles x E
     int32_t* rows;     // tiles
-    float* losses;     // sequences
+    float* losses;     // sequences x parts
     int64_t tiles, bytes;
+    int parts, part;   // workgroups that share a sequence's experts, and experts of each
 };
 Partial partial_view(char* workspace, int64_t T, int64_t E, int64_t S)
 {
@@ -140,12 +182,16 @@ Partial partial_view(char* workspace, int64_t T, int64_t E, int64_t S)
     p.sums = reinterpret_cast<float*>(take(p.tiles * E * 4));
     p.counts = reinterpret_cast<int32_t*>(take(p.tiles * E * 4));
     p.rows = reinterpret_cast<int32_t*>(take(p.tiles * 4));
-    p.losses = reinterpret_cast<float*>(take(S * 4));
+    // one workgroup for a sequence, or one for 64 of its experts where it has much to read (us of the join, one and several:
+    // 35,906 rows of 353 26, 10; 65,536 rows of 512 46, 12; the mean's launch comes to 2)
+    p.part = p.tiles / S * E >= 65536 ? 64 : (int)E;
+    p.parts = (int)((E + p.part - 1) / p.part);
+    p.losses = reinterpret_cast<float*>(take(S * p.parts * 4));
     p.bytes = at;
     return p;
 }
 
-template <typename T, int LANES, int V, bool FULL>
+template <typename T, int LANES, int V>
 __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, Partial p, int64_t block0)
 {
     constexpr int kGroups = kThreads / LANES;
@@ -158,6 +204,7 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
     for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
     if (threadIdx.x == 0) rows = 0;
     __syncthreads();
+    const Held<LANES, V> held(a.E);
     float sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) sum[v] = 0.0f;
@@ -166,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
 #pragma unroll 1
     for (int i0 = 0; i0 < kTurns; i0 += kAtOnce) {
         int32_t e[kAtOnce];
-        Experts<T, V, FULL> x[kAtOnce];
+        Experts<T, LANES, V> x[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
             // (in place of a row past the last, that one; it is not counted)
@@ -174,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
             const int64_t t = tile.first + min(r, tile.rows - 1);
             e[i] = choice_of<LANES>(a.experts, t, a.k, a.E);
             if (r >= tile.rows) e[i] = -1;
-            x[i].load(static_cast<const T*>(a.logits) + t * a.ld, sub * V, a.E);
+            x[i].load(static_cast<const T*>(a.logits) + t * a.ld, held);
         }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
@@ -182,14 +229,14 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
             if (!any_choice<LANES>(e[i])) continue;
             if (sub == 0) atomicAdd(&rows, 1);
             float p[V];
-            x[i].numbers(p, sub * V, a.E);
-            softmax<LANES, V>(p);
+            softmax(x[i], held, p);
 #pragma unroll
             for (int v = 0; v < V; ++v) sum[v] += p[v];
         }
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) sums[group][sub * V + v] = sum[v];
+    for (int v = 0; v < V; ++v)
+        if (held.has(v)) sums[group][held.expert(v)] = sum[v];
     __syncthreads();
     for (int e = threadIdx.x; e < a.E; e += kThreads) {
         float s = 0.0f;
@@ -201,13 +248,14 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
     if (threadIdx.x == 0) p.rows[index] = rows;
 }
 
-// A sequence's tiles, by one workgroup: LINES of E threads each take every LINES-th tile.
+// A sequence's tiles, or of a part of its experts: lines of E threads each take every `lines`th tile.
 __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs a, Partial p, int64_t block0)
 {
     __shared__ float sums[kJoinThreads], wave_loss[kJoinThreads / 64];
     __shared__ int32_t counts[kJoinThreads], wave_rows[kJoinThreads / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t seq = block0 + blockIdx.x;
+    const int64_t item = block0 + blockIdx.x, seq = item / p.parts;
+    const int part = (int)(item - seq * p.parts), e0 = part * p.part, experts = min(p.part, a.E - e0);
     // the sequence's first tile: those of the sequences before it
     int64_t first = 0;
     if (a.segments) {
@@ -228,29 +276,26 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
 #pragma unroll
     for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
     if (lane == 0) wave_rows[wave] = n;
-    const int lines = kJoinThreads / a.E, line = threadIdx.x / a.E, e = threadIdx.x - line * a.E;
+    // (no more lines than a line has loads on their way: they are added up one after the other)
+    constexpr int kAtOnce = 16;
+    const int lines = min(kJoinThreads / experts, 2 * kAtOnce), line = threadIdx.x / experts, e = threadIdx.x - line * experts;
     float s = 0.0f;
     int32_t c = 0;
     if (line < lines) {
-        int64_t t = first + line;
-        constexpr int kAtOnce = 16;
-        for (; t + (kAtOnce - 1) * lines < end; t += kAtOnce * lines) {
+        for (int64_t t = first + line; t < end; t += kAtOnce * lines) {
             float more[kAtOnce];
             int32_t pairs[kAtOnce];
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) {
-                more[i] = p.sums[(t + i * lines) * a.E + e];
-                pairs[i] = p.counts[(t + i * lines) * a.E + e];
+                const int64_t at = min(t + i * lines, end - 1) * a.E + e0 + e;
+                more[i] = p.sums[at];
+                pairs[i] = p.counts[at];
             }
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) {
-                s += more[i];
-                c += pairs[i];
+                s += t + i * lines < end ? more[i] : 0.0f;
+                c += t + i * lines < end ? pairs[i] : 0;
             }
-        }
-        for (; t < end; t += lines) {
-            s += p.sums[t * a.E + e];
-            c += p.counts[t * a.E + e];
         }
     }
     sums[threadIdx.x] = s;
@@ -260,12 +305,12 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
 #pragma unroll
     for (int w = 0; w < kJoinThreads / 64; ++w) n += wave_rows[w];
     float loss = 0.0f;
-    if (threadIdx.x < a.E) {
+    if ((int)threadIdx.x < experts) {
         for (int i = 1; i < lines; ++i) {
-            s += sums[i * a.E + e];
-            c += counts[i * a.E + e];
+            s += sums[i * experts + e];
+            c += counts[i * experts + e];
         }
-        a.counts[seq * a.E + e] = c;
+        a.counts[seq * a.E + e0 + e] = c;
         const double even = (double)a.k * n;
         if (n > 0) loss = (1.0f + over_even(c, even, 1.0f / (float)even, a.E)) * (s / (float)n);
     }
@@ -276,8 +321,8 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
     if (threadIdx.x == 0) {
         loss = 0.0f;
         for (int w = 0; w < kJoinThreads / 64; ++w) loss += wave_loss[w];
-        a.rows[seq] = n;
-        (a.S == 1 ? a.loss : p.losses + seq)[0] = loss;
+        if (part == 0) a.rows[seq] = n;
+        (a.S * p.parts == 1 ? a.loss : p.losses + item)[0] = loss;
     }
 }
 
@@ -303,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void balance_mean_kernel(BalanceArgs a, P
     __shared__ float part[kThreads / 64];
     const int used = sequences_used<kThreads>(a.rows, a.S);
     float s = 0.0f;
-    for (int64_t i = threadIdx.x; i < a.S; i += kThreads) s += p.losses[i];
+    for (int64_t i = threadIdx.x; i < a.S * p.parts; i += kThreads) s += p.losses[i];
 #pragma unroll
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
@@ -316,15 +361,16 @@ __global__ __launch_bounds__(kThreads) void balance_mean_kernel(BalanceArgs a, P
 }
 
 // SEQUENCES: there are segments.
-template <typename T, int LANES, int V, bool FULL, bool SEQUENCES>
+template <typename T, int LANES, int V, bool SEQUENCES>
 __global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs a, int64_t row_blocks)
 {
     constexpr int kGroups = kThreads / LANES;
-    const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES, e0 = sub * V;
-    Experts<int32_t, V, FULL> count;
+    const int group = threadIdx.x / LANES;
+    const Held<LANES, V> held(a.E);
+    Experts<int32_t, LANES, V> count;
     int32_t n = 0;
     if (!SEQUENCES) {
-        count.load(a.counts, e0, a.E);
+        count.load(a.counts, held);
         n = a.rows[0];
     }
     const float dloss = a.dloss[0];
@@ -334,11 +380,11 @@ __global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs 
     for (int64_t b = blockIdx.x; b < row_blocks; b += gridDim.x) {
         const int64_t t = b * kGroups + group;
         if (t >= a.T) continue;
-        Experts<T, V, FULL> held, was;
-        held.load(static_cast<const T*>(a.logits) + t * a.ld, e0, a.E);
+        Experts<T, LANES, V> logits, was;
+        logits.load(static_cast<const T*>(a.logits) + t * a.ld, held);
         const int32_t e = choice_of<LANES>(a.experts, t, a.k, a.E);
         T* const out = static_cast<T*>(a.dlogits) + t * a.ldd;
-        if (a.accumulate) was.load(out, e0, a.E);
+        if (a.accumulate) was.load(out, held);
         int64_t seq = 0;
         bool there = true;
         if (SEQUENCES) {
@@ -355,32 +401,31 @@ __global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs 
         if (seq != of) {
             of = seq;
             if (SEQUENCES) {
-                count.load(a.counts + seq * a.E, e0, a.E);
+                count.load(a.counts + seq * a.E, held);
                 n = a.rows[seq];
             }
             const double even = (double)a.k * n;
             const float by = n > 0 ? 1.0f / (float)even : 0.0f;
             scale = n > 0 && used > 0 ? dloss / ((float)used * (float)n) : 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) f[v] = e0 + v < a.E ? over_even(count.v[v], even, by, a.E) : 0.0f;
+            for (int v = 0; v < V; ++v) f[v] = over_even(count[v], even, by, a.E);
         }
         there = any_choice<LANES>(e) && there && n > 0 && used > 0;
         if (!there && a.accumulate) continue;
         float x[V];
         if (there) {
-            held.numbers(x, e0, a.E);
-            softmax<LANES, V>(x);
+            softmax(logits, held, x);
             float inner = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) inner = __builtin_fmaf(f[v], x[v], inner);
+            for (int v = 0; v < V; ++v) inner = held.has(v) ? __builtin_fmaf(f[v], x[v], inner) : inner;
             inner = over_lanes_sum<LANES>(inner);
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = scale * x[v] * (f[v] - inner) + (a.accumulate ? (float)was.v[v] : 0.0f);
+            for (int v = 0; v < V; ++v) x[v] = scale * x[v] * (f[v] - inner) + (a.accumulate ? (float)was[v] : 0.0f);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) x[v] = 0.0f;
         }
-        held.store(out, e0, a.E, x);
+        logits.store(out, held, x);
     }
 }
 
@@ -405,15 +450,14 @@ hipError_t balance(const BalanceArgs& a, hipStream_t s)
     hipError_t err = by_experts(a.E, [&](auto lanes, auto v) {
         constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
         return launch_parts(most_row_tiles(a.S, a.T, kRows, a.segments != nullptr), kThreads, [&](unsigned grid, int64_t block0) {
-            if (a.E % V == 0) balance_tiles_kernel<T, L, V, true><<<grid, kThreads, 0, s>>>(a, p, block0);
-            else balance_tiles_kernel<T, L, V, false><<<grid, kThreads, 0, s>>>(a, p, block0);
+            balance_tiles_kernel<T, L, V><<<grid, kThreads, 0, s>>>(a, p, block0);
         });
     });
     if (err != hipSuccess) return err;
-    err = launch_parts(a.S, kJoinThreads, [&](unsigned grid, int64_t block0) {
+    err = launch_parts(a.S * p.parts, kJoinThreads, [&](unsigned grid, int64_t block0) {
         balance_join_kernel<<<grid, kJoinThreads, 0, s>>>(a, p, block0);
     });
-    if (err != hipSuccess || a.S == 1) return err;
+    if (err != hipSuccess || a.S * p.parts == 1) return err;
     balance_mean_kernel<<<1, kThreads, 0, s>>>(a, p);
     return hipGetLastError();
 }
@@ -426,13 +470,8 @@ hipError_t balance_grad(const BalanceGradArgs& a, hipStream_t s)
         const int64_t row_blocks = (a.T + kGroups - 1) / kGroups;
         const unsigned grid = (unsigned)(row_blocks < 2048 ? row_blocks : 2048);
         constexpr int L = decltype(lanes)::value, V = decltype(v)::value;
-        if (a.E % V == 0) {
-            if (a.segments) balance_grad_kernel<T, L, V, true, true><<<grid, kThreads, 0, s>>>(a, row_blocks);
-            else balance_grad_kernel<T, L, V, true, false><<<grid, kThreads, 0, s>>>(a, row_blocks);
-        } else {
-            if (a.segments) balance_grad_kernel<T, L, V, false, true><<<grid, kThreads, 0, s>>>(a, row_blocks);
-            else balance_grad_kernel<T, L, V, false, false><<<grid, kThreads, 0, s>>>(a, row_blocks);
-        }
+        if (a.segments) balance_grad_kernel<T, L, V, true><<<grid, kThreads, 0, s>>>(a, row_blocks);
+        else balance_grad_kernel<T, L, V, false><<<grid, kThreads, 0, s>>>(a, row_blocks);
         return hipGetLastError();
     });
 }
