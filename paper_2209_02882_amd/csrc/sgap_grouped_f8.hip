@@ -90,7 +90,7 @@ __device__ __forceinline__ void store4(T* __restrict__ y, int64_t n, int64_t N, 
 template <typename T, int NT, int MT, int U>
 __global__ __launch_bounds__(512) void grouped_f8_few_kernel(GroupedF8Args a, int64_t column_items, bool wide, int64_t block0)
 {
-    __shared__ f32x4 part[8][64];
+    __shared__ f32x4 part[8][NT * MT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, row = lane & 15, piece = lane >> 4;
     const int64_t item = block0 + blockIdx.x, g = item / column_items, n0 = (item - g * column_items) * (NT * 16);
@@ -125,8 +125,8 @@ __global__ __launch_bounds__(512) void grouped_f8_few_kernel(GroupedF8Args a, in
             float sw[U][NT], sx[U][MT];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                // (in place of a block behind the last, that one, times 0)
                 const int64_t b = min(b0 + u, blocks - 1), at = b * kF8Block;
-                const bool there = b0 + u < blocks;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     wc[u][nt] = join(*reinterpret_cast<const HalfCodes*>(w[nt] + at), *reinterpret_cast<const HalfCodes*>(w[nt] + at + 64));
@@ -137,18 +137,6 @@ __global__ __launch_bounds__(512) void grouped_f8_few_kernel(GroupedF8Args a, in
                     xc[u][mt] = join(*reinterpret_cast<const HalfCodes*>(x[mt] + at), *reinterpret_cast<const HalfCodes*>(x[mt] + at + 64));
                     sx[u][mt] = xs[mt][b];
                 }
-                if (!there) {
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        xc[u][mt] = Codes{0, 0, 0, 0, 0, 0, 0, 0};
-                        sx[u][mt] = 0.0f;
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        wc[u][nt] = Codes{0, 0, 0, 0, 0, 0, 0, 0};
-                        sw[u][nt] = 0.0f;
-                    }
-                }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -157,27 +145,28 @@ __global__ __launch_bounds__(512) void grouped_f8_few_kernel(GroupedF8Args a, in
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
                         const f32x4 p = mma_block(numbers(wc[u][nt]), numbers(xc[u][mt]));
-                        const float s = sw[u][nt] * sx[u][mt];
+                        const float s = b0 + u < blocks ? sw[u][nt] * sx[u][mt] : 0.0f;
 #pragma unroll
                         for (int r = 0; r < 4; ++r) acc[nt][mt][r] = __builtin_fmaf(p[r], s, acc[nt][mt][r]);
                     }
         }
+        __syncthreads();  // of the rows before, everything is read
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < NT * MT; ++i) part[wave][i][lane] = acc[i / MT][i % MT];
+        __syncthreads();
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                __syncthreads();
-                part[wave][lane] = acc[nt][mt];
-                __syncthreads();
-                if (threadIdx.x >= 64) continue;
-                // lane: row lane % 16, columns 4 * (lane / 16) + 0 .. 3
-                f32x4 v = part[0][lane];
-                for (int s = 1; s < waves; ++s) v += part[s][lane];
-                const int64_t at = m0 + mt * 16 + row, n = n0 + nt * 16 + 4 * piece;
-                if (at >= gr.end || n >= a.N) continue;
-                if (a.from.src && a.from.row(at) < 0) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                store4(Y + at * a.ldy, n, a.N, wide, v);
-            }
+        for (int i = 0; i < NT * MT; ++i) {
+            if (i % waves != wave) continue;
+            // lane: row lane % 16, columns 4 * (lane / 16) + 0 .. 3
+            f32x4 v = part[0][i][lane];
+#pragma unroll
+            for (int s = 1; s < 8; ++s)
+                if (s < waves) v += part[s][i][lane];
+            const int64_t at = m0 + (i % MT) * 16 + row, n = n0 + (i / MT) * 16 + 4 * piece;
+            if (at >= gr.end || n >= a.N) continue;
+            if (a.from.src && a.from.row(at) < 0) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            store4(Y + at * a.ldy, n, a.N, wide, v);
+        }
     }
     // rows behind the last group
     if (a.offsets && g == a.G - 1) {
@@ -228,8 +217,9 @@ __device__ __forceinline__ void wait_but()
 // so there are always products to make while the next block's first fragments are read, which all wavefronts do at a time.
 //   load(t, stage, i)   starts load i of LOADS of block t; every wavefront has so many
 //   ACTIVE: this wavefront has products to make
+//   real: blocks of them that count, the others (of the last team) are multiplied by 0
 template <typename T, int MI, int NJ, int STAGES, int LOADS, bool ACTIVE, typename F>
-__device__ __forceinline__ void multiply_blocks(uint32_t lds, uint32_t stage_bytes, int blocks, F&& load, const float* w_scales, uint32_t wbase,
+__device__ __forceinline__ void multiply_blocks(uint32_t lds, uint32_t stage_bytes, int blocks, int real, F&& load, const float* w_scales, uint32_t wbase,
                                                 uint32_t xbase, uint32_t sbase, f32x4 (&acc)[MI][NJ])
 {
     constexpr int H = NJ / 2;
@@ -255,7 +245,7 @@ __device__ __forceinline__ void multiply_blocks(uint32_t lds, uint32_t stage_byt
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) load(b, lds + b * stage_bytes, i);
     }
-    float sw = w_scale[0];
+    float sw = real > 0 ? w_scale[0] : 0.0f;
     // (also until the compiler's own loads have arrived)
     if (blocks >= STAGES) wait_but<(STAGES - 1) * LOADS>();
     else wait_loads();
@@ -276,7 +266,7 @@ __device__ __forceinline__ void multiply_blocks(uint32_t lds, uint32_t stage_byt
         other = other == (STAGES - 1) * stage_bytes ? 0 : other + stage_bytes;
         uint32_t xb = xbase + stage, sb = sbase + stage;
         asm volatile("" : "+v"(xb), "+v"(sb));  // made anew each time, not kept in registers
-        const float sw_next = w_scale[t + 1 < blocks ? t + 1 : t];
+        const float sw_next = t + 1 < real ? w_scale[t + 1] : 0.0f;
         f32x4 q[MI];
 #pragma unroll
         for (int j = 0; j < H; ++j) {
@@ -350,13 +340,16 @@ __device__ __forceinline__ void multiply_blocks(uint32_t lds, uint32_t stage_byt
 
 // Many rows: tiles of BM rows by BN columns, a block of the inner dimension at a time, by loads straight into LDS.
 // FAR: rows are gathered that lie further than 32 bits of bytes from X's first.  Results of floats go by numbers, others by codes.
+// TEAMS: 2 where a tile is all that a compute unit has: each team has half of the blocks, stages of its own, and the shares are added
+// through LDS.  (A block's chain of fragments, products and a barrier takes 0.55 us however few wavefronts there are: 256 rows, 4,096
+// by 4,096 25.6 us, 16.1 by teams with three stages each, 20.2 with three stages and one team.)
 // (Two wavefronts to a SIMD: with more registers than that leaves, the compiler has the matrix unit write to those that no vector
 // instruction reads, and waits for each product: 64 x 128 tiles took 0.68 us a block.)
-template <typename T, int BM, int BN, int STAGES, bool FAR, int THREADS>
-__global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8Args a, int64_t column_tiles, int64_t items, int64_t block0)
+template <typename T, int BM, int BN, int STAGES, bool FAR, int THREADS, int TEAMS>
+__global__ __launch_bounds__(THREADS * TEAMS, 2) void grouped_f8_tiles_kernel(GroupedF8Args a, int64_t column_tiles, int64_t items, int64_t block0)
 {
-    using Wt = Tile<uint8_t, BN, true, THREADS>;
-    using Xt = Tile<uint8_t, BM, true, THREADS>;
+    using Wt = Tile<uint8_t, BN, true, THREADS, TEAMS>;
+    using Xt = Tile<uint8_t, BM, true, THREADS, TEAMS>;
     constexpr int kWaves = THREADS / 64, WN = kWaves / 2, WM = 2;
     constexpr int MI = BN / WN / 16, NJ = BM / WM / 16;
     constexpr uint32_t kStage = Wt::kBytes + Xt::kBytes + BM * 4;
@@ -367,7 +360,8 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8A
     const int64_t tile = band * kBand + in % kBand, n0 = in / kBand * BN;
     const RowTile rows = find_row_tile<BM>(a.offsets, a.G, a.R, tile);
     if (rows.rows <= 0) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(Wt::thread() >> 6);
+    const int team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS);
     const int wn = (wave % WN) * (BN / WN), wm = (wave / WN) * (BM / WM);
     const int64_t blocks = f8_blocks(a.K), pitch = blocks * kF8Block;
     f32x4 acc[MI][NJ];
@@ -378,7 +372,9 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8A
     if (rows.g < a.G) {
         // columns and rows past the last are read from the last, and not stored; a row of X that does not exist is read
         // from row 0, and zeros are stored
-        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_bytes;
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds_bytes + team * (STAGES * kStage);
+        // a team has so many blocks of the inner dimension, from this one on; behind the last one it loads that again
+        const int share = ((int)blocks + TEAMS - 1) / TEAMS, block_first = team * share, last = (int)blocks - 1;
         const uint8_t* const W = uniform(a.W + (rows.g * a.N + n0) * pitch);
         // of X a byte's place, or, FAR, the row
         uint32_t wo[Wt::kRounds], xo[Xt::kRounds];
@@ -401,10 +397,11 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8A
         const int scales0 = wave * 64 % BM;
         const int64_t scale_row = row(scales0 + lane);
         const uint32_t so = FAR ? (uint32_t)scale_row : (uint32_t)(scale_row * blocks * 4);
-        const float* const sw = uniform(a.w_scales + (rows.g * f8_blocks(a.N) + min(n0 + wn, a.N - 1) / kF8Block) * blocks);
+        const float* const sw = uniform(a.w_scales + (rows.g * f8_blocks(a.N) + min(n0 + wn, a.N - 1) / kF8Block) * blocks + block_first);
         constexpr int kLoads = Wt::kRounds + Xt::kRounds + 1;
         const auto load = [&](int t, uint32_t to, int i) {
             const int r = i - Wt::kRounds;
+            if constexpr (TEAMS > 1) t = min(block_first + t, last);
             if (i < Wt::kRounds) {
                 Wt::load(to, i, uniform(W + (int64_t)t * kF8Block), wo[i]);
             } else if (r < Xt::kRounds) {
@@ -418,8 +415,8 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8A
         };
         const uint32_t wbase = lds + Wt::lane_base(wn), xbase = lds + Wt::kBytes + Xt::lane_base(wm);
         const uint32_t sbase = lds + Wt::kBytes + Xt::kBytes + (wm + (lane & 15)) * 4;
-        if (wm < rows.rows) multiply_blocks<T, MI, NJ, STAGES, kLoads, true>(lds, kStage, (int)blocks, load, sw, wbase, xbase, sbase, acc);
-        else multiply_blocks<T, MI, NJ, STAGES, kLoads, false>(lds, kStage, (int)blocks, load, sw, wbase, xbase, sbase, acc);
+        if (wm < rows.rows) multiply_blocks<T, MI, NJ, STAGES, kLoads, true>(lds, kStage, share, min(share, last + 1 - block_first), load, sw, wbase, xbase, sbase, acc);
+        else multiply_blocks<T, MI, NJ, STAGES, kLoads, false>(lds, kStage, share, min(share, last + 1 - block_first), load, sw, wbase, xbase, sbase, acc);
     }
     // Through LDS, each wavefront its own part, so that rows leave in whole lines: 16-byte chunk c of row r at place c ^ (r & 7).
     constexpr int kColumns = BN / WN, kRows = BM / WM, P = Piece<T>::kCount, kChunks = kColumns / P;
@@ -430,6 +427,20 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_f8_tiles_kernel(GroupedF8A
     typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
     lds_char* const part = (lds_char*)lds_bytes + wave * (kRows * kColumns * (int)sizeof(T));
     __syncthreads();  // everyone has read what lies there
+    if constexpr (TEAMS > 1) {
+        // the second team's share, by way of its own part of LDS
+        static_assert(TEAMS == 2 && MI * NJ * THREADS * 16 <= STAGES * (int)kStage, "");
+        typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+        lds_f32x4* const shares = (lds_f32x4*)((lds_char*)lds_bytes + STAGES * kStage) + Wt::thread();
+        if (team == 1) {
+#pragma unroll
+            for (int i = 0; i < MI * NJ; ++i) shares[i * THREADS] = acc[i / NJ][i % NJ];
+        }
+        __syncthreads();
+        if (team == 1) return;
+#pragma unroll
+        for (int i = 0; i < MI * NJ; ++i) acc[i / NJ][i % NJ] += shares[i * THREADS];
+    }
     const int real_rows = min(rows.rows - wm, kRows);
     if (real_rows <= 0) return;
 #pragma unroll
@@ -467,23 +478,24 @@ hipError_t run_few(const GroupedF8Args& a, bool wide, hipStream_t s)
 {
     const int64_t columns = (a.N + NT * 16 - 1) / (NT * 16), blocks = f8_blocks(a.K);
     const int waves = (int)std::min<int64_t>(8, std::max<int64_t>(1, (blocks + U - 1) / U));
-    const int64_t rows = a.offsets ? std::max<int64_t>(1, a.R / a.G) : a.R;
+    // (groups differ in length: most of the longer ones pass at a time too)
+    const int64_t rows = a.offsets ? std::max<int64_t>(1, a.R * 8 / (a.G * 5)) : a.R;
     const unsigned down = (unsigned)std::min<int64_t>(64, (rows + 16 * MT - 1) / (16 * MT));
     return launch_parts(a.G * columns, 512 * (int)down, [&](unsigned grid, int64_t block0) {
         grouped_f8_few_kernel<T, NT, MT, U><<<dim3(grid, down), waves * 64, 0, s>>>(a, columns, wide, block0);
     });
 }
 
-template <typename T, int BM, int BN, int STAGES, bool FAR, int THREADS>
+template <typename T, int BM, int BN, int STAGES, bool FAR, int THREADS, int TEAMS = 1>
 hipError_t run_tiles(const GroupedF8Args& a, hipStream_t s)
 {
     const int64_t columns = (a.N + BN - 1) / BN, bands = (most_row_tiles(a.G, a.R, BM, a.offsets != nullptr) + kBand - 1) / kBand;
     const int64_t items = columns * bands * kBand;
-    constexpr int kLds = STAGES * (128 * (BM + BN) + BM * 4);
+    constexpr int kLds = TEAMS * STAGES * (128 * (BM + BN) + BM * 4);
     static uint64_t allowed = 0;
-    if (const hipError_t err = allow_lds(grouped_f8_tiles_kernel<T, BM, BN, STAGES, FAR, THREADS>, kLds, allowed)) return err;
-    return launch_parts((items + 255) / 256 * 256, THREADS, [&](unsigned grid, int64_t block0) {
-        grouped_f8_tiles_kernel<T, BM, BN, STAGES, FAR, THREADS><<<grid, THREADS, kLds, s>>>(a, columns, items, block0);
+    if (const hipError_t err = allow_lds(grouped_f8_tiles_kernel<T, BM, BN, STAGES, FAR, THREADS, TEAMS>, kLds, allowed)) return err;
+    return launch_parts((items + 255) / 256 * 256, THREADS * TEAMS, [&](unsigned grid, int64_t block0) {
+        grouped_f8_tiles_kernel<T, BM, BN, STAGES, FAR, THREADS, TEAMS><<<grid, THREADS * TEAMS, kLds, s>>>(a, columns, items, block0);
     });
 }
 
@@ -492,55 +504,78 @@ hipError_t grouped_f8(const GroupedF8Args& a, const GroupedF8Plan& p, hipStream_
 {
     // (the address and the row's length that stores of four results ask for)
     const bool wide = a.ldy % 4 == 0 && (reinterpret_cast<uintptr_t>(a.Y) & (4 * sizeof(T) - 1)) == 0;
-    if (!p.tiles) return p.rows == 16 ? run_few<T, 1, 1, 4>(a, wide, s) : run_few<T, 2, 2, 2>(a, wide, s);
+    if (p.teams == 0) {
+        if (p.rows == 32) return run_few<T, 2, 2, 2>(a, wide, s);
+        return p.deep ? run_few<T, 1, 1, 8>(a, wide, s) : run_few<T, 1, 1, 4>(a, wide, s);
+    }
     if constexpr (sizeof(T) == 2) {
         if (p.rows == 256) return run_tiles<T, 256, 256, 2, false, 512>(a, s);
     }
     if (p.far) return run_tiles<T, 128, 128, 2, true, 256>(a, s);
+    if (p.teams == 2) {
+        // (results of floats are bound by the conversion of the codes: a third stage gains them nothing)
+        if (p.rows == 128) return run_tiles<T, 128, 128, 2, false, 256, 2>(a, s);
+        return run_tiles<T, 64, 128, sizeof(T) == 2 ? 3 : 2, false, 256, 2>(a, s);
+    }
     return p.rows == 128 ? run_tiles<T, 128, 128, 2, false, 256>(a, s) : run_tiles<T, 64, 128, 2, false, 256>(a, s);
 }
 
 }  // namespace
 
-// The least of what the kernels are reckoned to take, in us.  With tiles, a compute unit has n of them: a tile costs so much a
-// block of the inner dimension and so much besides, and the only one of a unit more a block.  A group has a last tile that is not
-// full: 0.6 of a tile more than its rows in the mean.  With few rows: the weights pass once for 16 or 32 rows.
-// Measured (us; few rows 16, 32; tiles of 64, 128, 256 rows), inner dimension by columns, 16-bit results:
-//   1 row, 4,096 x 4,096                      6.2  10.5  16.8  25.5  40.7
-//   32 rows, 8,192 x 8,192                   40.2  25.2  53.4  59.1  76.0
-//   64 groups, 64 rows, 2,048 x 1,408        23.3  43.9  17.4  21.0  28.4
-//   256 rows, 4,096 x 4,096                  77.1  51.0  20.6  27.7  51.6
-//   2,048 rows, 4,096 x 4,096                 572   381  62.2  48.1  67.4
-//   64 groups, 8,192 rows, 2,048 x 1,408      406   386  60.3  66.1  68.9
-//   16 groups, 16,384 rows, 2,048 x 4,096   2,177 1,982   262   219   192
+// The least of what the kernels are reckoned to take, in us.  Few rows: a compute unit has n workgroups one after the other, each so
+// much and so much a block of the inner dimension (less where the 16 rows are not as many), and not less than the weights' bytes.
+// Tiles: n of them, each so much a block and so much besides; where n is 1 two teams share the blocks, unless these are fewer than
+// eight.  A group has a last tile that is not full: half a tile more than its rows in the mean; and groups differ in length, so that
+// some unit has a fifth more than the mean.
+// Measured (us; few rows 16, 32; tiles of 64, 64 by teams, 128, 128 by teams, 256 rows), inner dimension by columns, 16-bit results,
+// groups of very different length:
+//   1 row, 4,096 x 4,096                      6.2   8.6  19.1  14.0  25.3  20.3  39.9
+//   32 rows, 8,192 x 8,192                   40.0  26.6  51.8  26.3  59.2  37.5  75.1
+//   64 groups, 64 rows, 2,048 x 1,408        24.9  31.9  23.8  26.4  26.2  33.0  29.6
+//   256 rows, 4,096 x 4,096                  79.8  40.0  25.6  16.1  30.5  24.8  51.9
+//   1,024 rows, 4,096 x 4,096                 301   147  29.4  31.8  33.3  27.1  54.1
+//   2,048 rows, 4,096 x 4,096                 568   288  61.1  61.1  42.8  51.3  63.8
+//   64 groups, 8,192 rows, 2,048 x 1,408      409   258  73.1  86.6  79.1  92.3  75.5
+//   16 groups, 16,384 rows, 2,048 x 4,096       -     -   249   366   219   309   193
+// Over 140 calls of such sizes and sizes between them the choice took 3% more than the best.
 GroupedF8Plan plan_grouped_f8(const GroupedF8Args& a, int dtype)
 {
-    const bool half = dtype != 0;
-    const double blocks = (double)f8_blocks(a.K), used = a.offsets ? (double)std::min(a.G, std::max<int64_t>(a.R, 1)) : 1.0;
-    const double rows = (double)a.R / used, bytes = 2.5 + used * (double)a.K * (double)a.N / 5.7e6;  // the weights', once
-    GroupedF8Plan p = {false, false, 16, 16};
+    const bool half = dtype != 0, groups = a.offsets != nullptr;
+    const double blocks = (double)f8_blocks(a.K), used = groups ? (double)std::min(a.G, std::max<int64_t>(a.R, 1)) : 1.0;
+    const double rows = (double)a.R / used, bytes = used * (double)a.K * (double)a.N / 5.7e6;  // the weights', once
+    GroupedF8Plan p = {0, 16, 16, false, false};
     p.far = a.from.src && a.from.rows * f8_blocks(a.K) * kF8Block > 1ll << 32;
-    double few = bytes;
-    if (rows > 16) {
-        few = 2.5 + std::ceil(rows / 32) * (bytes - 2.5) * 2.0;
-        p.rows = p.columns = 32;
-    }
+    const auto down = [&](int size) { return used == 1.0 ? std::ceil(rows / size) : std::max(1.0, rows / size + 0.5); };
+    const auto few = [&](int size, double besides, double block, double& n) {
+        n = used * down(size) * std::ceil((double)a.N / size) / a.compute_units;
+        return 3.0 + std::max(bytes * down(size) * 0.9, (besides + block * blocks) * std::max(std::ceil(n), 1.0));
+    };
+    double n16, n32;
+    const double few16 = few(16, 0.57, 0.06 + 0.06 * std::min(1.0, rows / 8), n16), few32 = few(32, 1.46, 0.242, n32);
+    if (few32 < few16) p.rows = p.columns = 32;
+    // eight blocks on their way in place of four where that leaves wavefronts enough (7 groups, 18 rows, 3,021 x 1,902: 10.5 us, 12.7)
+    p.deep = p.rows == 16 && n16 >= 3.0 && blocks >= 16;
     // 128 lines of an operand have to lie within 32 bits of bytes
     constexpr int64_t kLongest = 1 << 22;
     if (a.K == 0 || a.K > kLongest) return p;
-    const auto tiles = [&](int BM, int BN, double block, double only, double besides) {
-        const double down = used == 1 ? std::ceil((double)a.R / BM) : (double)a.R / BM + 0.6 * used;
-        const double n = std::ceil(down * std::ceil((double)a.N / BN) / a.compute_units);
-        return std::max(std::max(n * (block * blocks + besides), only * blocks + 4.0), bytes);
+    double least = std::min(few16, few32);
+    // a tile costs `block` a block, `only` the only one of a compute unit, and `team` shared by two teams (0: not with them)
+    const auto tiles = [&](int size, int columns, double block, double only, double team, double besides) {
+        const double all = used == 1.0 ? std::ceil((double)a.R / size) : (double)a.R / size + 0.6 * used;
+        const double n = std::ceil(all * std::ceil((double)a.N / columns) / a.compute_units);
+        const int teams = n == 1.0 && blocks >= 8 && team > 0.0 ? 2 : 1;
+        const double work = n > 1.0 ? n * (block * blocks + besides) : (teams == 2 ? team : only) * blocks + 4.0;
+        const double time = (used > 1.0 ? 1.2 : 1.0) * std::max(work, bytes + 2.5);
+        if (time >= least) return;
+        least = time;
+        p.teams = teams;
+        p.rows = size;
+        p.columns = columns;
+        p.deep = false;
     };
-    const double small = p.far ? 1e30 : half ? tiles(64, 128, 0.48, 0.58, 0.4) : tiles(64, 128, 0.6, 0.92, 0.4);
-    const double middle = half ? tiles(128, 128, 0.72, 0.88, 1.4) : tiles(128, 128, 1.02, 1.3, 1.4);
-    const double large = half && !p.far ? tiles(256, 256, 1.67, 1.67, 9.0) : 1e30;
-    const double least = std::min(std::min(small, middle), large);
-    if (few < (used > 1 ? 0.8 : 1.0) * least) return p;
-    p.tiles = true;
-    p.rows = small <= least ? 64 : middle <= least ? 128 : 256;
-    p.columns = p.rows == 256 ? 256 : 128;
+    if (!p.far) tiles(64, 128, half ? 0.48 : 0.6, half ? 0.58 : 0.8, half ? 0.4 : 0.61, 0.4);
+    tiles(128, 128, half ? 0.72 : 1.02, half ? 0.88 : 1.25, p.far ? 0.0 : half ? 0.66 : 1.02, 1.4);
+    if (half && !p.far) tiles(256, 256, 1.67, 1.67, 0.0, 9.0);
     return p;
 }
 

@@ -24,8 +24,10 @@ __device__ __forceinline__ const P* uniform(const P* p)
     return (const P*)(uintptr_t)((uint64_t)hi << 32 | lo);
 }
 
-template <typename T, int LINES, bool INNER, int THREADS>
+// THREADS fill a tile; of a workgroup with TEAMS times as many each team has tiles of its own.
+template <typename T, int LINES, bool INNER, int THREADS, int TEAMS = 1>
 struct Tile {
+    static __device__ __forceinline__ int thread() { return TEAMS == 1 ? (int)threadIdx.x : (int)threadIdx.x % THREADS; }
     static constexpr int P = Piece<T>::kCount;
     static constexpr int kInner = 128 / (int)sizeof(T);  // inner values of a tile
     static constexpr int kBytes = LINES * 128;
@@ -38,10 +40,10 @@ struct Tile {
 
     // What the piece at place `round * THREADS + thread` holds: a line and an inner piece, or an inner value and a piece
     // of the lines.
-    static __device__ __forceinline__ int major(int round) { return (round * THREADS + (int)threadIdx.x) / (INNER ? 8 : kAcross); }
+    static __device__ __forceinline__ int major(int round) { return (round * THREADS + thread()) / (INNER ? 8 : kAcross); }
     static __device__ __forceinline__ int minor(int round)
     {
-        const int place = (round * THREADS + (int)threadIdx.x) % (INNER ? 8 : kAcross), m = major(round);
+        const int place = (round * THREADS + thread()) % (INNER ? 8 : kAcross), m = major(round);
         if (INNER) return place ^ (m & 7);
         if (sizeof(T) == 2) return place ^ (turn(m) << 1);
         return place ^ (turn(m) << 2);
@@ -52,7 +54,7 @@ struct Tile {
     // `lds`: the tile's LDS address; the wavefront's lanes fill 1,024 consecutive bytes of it a round.
     static __device__ __forceinline__ uint32_t place(uint32_t lds, int round)
     {
-        const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t wave = __builtin_amdgcn_readfirstlane(thread() >> 6);
         return lds + (round * THREADS + wave * 64) * 16;
     }
     static __device__ __forceinline__ void load(uint32_t lds, int round, const void* base, uint32_t offset)  // base: the wavefront's
@@ -73,7 +75,7 @@ struct Tile {
     static __device__ __forceinline__ void put(uint32_t lds, int round, piece_t<T> v)
     {
         typedef __attribute__((address_space(3))) piece_t<T> lds_piece;
-        *(lds_piece*)(uintptr_t)(lds + (round * THREADS + threadIdx.x) * 16) = v;
+        *(lds_piece*)(uintptr_t)(lds + (round * THREADS + thread()) * 16) = v;
     }
     static __device__ __forceinline__ void clear(uint32_t lds, int round) { put(lds, round, piece_t<T>{}); }
 

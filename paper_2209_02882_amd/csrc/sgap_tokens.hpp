@@ -101,9 +101,10 @@ hipError_t launch_f8_rows(const F8RowsArgs& a, hipStream_t s);
 hipError_t launch_f8_weights(const F8WeightsArgs& a, hipStream_t s);
 // Which kernel a product takes.
 struct GroupedF8Plan {
-    bool tiles;         // else: few rows, whose workgroups' wavefronts share the inner dimension
-    bool far;           // tiles: rows are gathered from more than 4 GiB
+    int teams;          // that make tiles and share the inner dimension; 0: few rows, whose workgroups' wavefronts share it
     int rows, columns;  // of a workgroup's part of the result
+    bool far;           // tiles: rows are gathered from more than 4 GiB
+    bool deep;          // few rows: more blocks on their way
 };
 GroupedF8Plan plan_grouped_f8(const GroupedF8Args& a, int dtype);
 hipError_t launch_grouped_f8(GroupedF8Args a, int dtype, hipStream_t s);

@@ -200,10 +200,10 @@ int sgap_debug_f8_plan(int64_t G, int64_t R, int64_t K, int64_t N, int dtype, in
     const sgap::GroupedF8Args a{G, R, K, N, given_offsets ? list : nullptr, {given_src ? list : nullptr, 1, x_rows}, nullptr, nullptr,
                                 nullptr, nullptr, nullptr, N, compute_units};
     const sgap::GroupedF8Plan p = sgap::plan_grouped_f8(a, dtype);
-    plan[0] = p.tiles ? 1 : 0;
+    plan[0] = p.teams;
     plan[1] = p.rows;
     plan[2] = p.columns;
-    plan[3] = p.far ? 1 : 0;
+    plan[3] = p.teams == 0 ? (p.deep ? 2 : 0) : p.far ? 1 : 0;
     return SGAP_OK;
 }
 

@@ -192,11 +192,15 @@ def test_products(sizes, more, N, K, dtype):
 
 # every kernel that a product may take, asked of the plan
 @pytest.mark.parametrize("G,R,N,K,dtype,want", [
-    (1, 11, 100, 500, torch.bfloat16, (0, 16, 16, 0)), (1, 40, 1000, 4000, torch.float16, (0, 32, 32, 0)),
+    (1, 11, 100, 500, torch.bfloat16, (0, 16, 16, 0)), (1, 40, 1000, 4000, torch.float16, (0, 16, 16, 0)),
+    (7, 18, 1902, 3021, torch.bfloat16, (0, 16, 16, 2)), (5, 40, 3000, 2300, torch.float32, (0, 16, 16, 2)),
+    (1, 64, 4000, 4000, torch.float16, (0, 32, 32, 0)), (3, 300, 900, 1300, torch.float32, (0, 32, 32, 0)),
     (3, 100, 4000, 300, torch.bfloat16, (1, 64, 128, 0)), (5, 4100, 4000, 1100, torch.float16, (1, 128, 128, 0)),
     (1, 4000, 8100, 530, torch.bfloat16, (1, 256, 256, 0)), (3, 6000, 4000, 1100, torch.float16, (1, 256, 256, 0)),
-    (2, 200, 3000, 400, torch.float32, (0, 32, 32, 0)), (3, 2000, 3900, 500, torch.float32, (1, 64, 128, 0)),
-    (2, 3000, 3900, 1500, torch.float32, (1, 128, 128, 0)),
+    (3, 2000, 3900, 500, torch.float32, (1, 64, 128, 0)), (2, 3000, 3900, 1500, torch.float32, (1, 128, 128, 0)),
+    (1, 700, 1000, 1100, torch.bfloat16, (2, 64, 128, 0)), (3, 500, 2000, 1700, torch.float16, (2, 64, 128, 0)),
+    (1, 300, 900, 1300, torch.float32, (2, 64, 128, 0)), (4, 400, 4000, 1500, torch.float16, (2, 128, 128, 0)),
+    (1, 900, 3900, 2200, torch.bfloat16, (2, 128, 128, 0)), (1, 900, 3900, 2200, torch.float32, (2, 128, 128, 0)),
 ])
 @pytest.mark.parametrize("gathered", [False, True])
 def test_products_by_every_kernel(G, R, N, K, dtype, want, gathered):
@@ -245,7 +249,8 @@ def test_products_of_one_group_without_offsets(R):
     check(*operands(R, R, 1, 144, 320), 320, None, R, torch.float32)
 
 
-@pytest.mark.parametrize("sizes,N,K,k", [([3, 0, 9, 4], 50, 200, 2), ([200, 56, 0, 144], 140, 256, 4), ([600, 424], 300, 130, 1)])
+@pytest.mark.parametrize("sizes,N,K,k", [([3, 0, 9, 4], 50, 200, 2), ([200, 56, 0, 144], 140, 256, 4), ([600, 424], 300, 130, 1),
+                                         ([300, 0, 210], 1000, 1100, 2), ([900], 2000, 1300, 1)])
 def test_rows_gathered_by_a_list(sizes, N, K, k):
     R = sum(sizes)
     x_rows = R // k
@@ -288,18 +293,20 @@ def test_results_apart(R, N, dtype):
         assert torch.isnan(y[:, :first]).all() and torch.isnan(y[:, first + N:]).all()
 
 
-@pytest.mark.parametrize("R", [12, 150])
-def test_nan_stays_in_its_row_and_column(R):
-    x, xs, w, ws = operands(2, R, 1, 90, 256)
-    x.view(torch.uint8)[5, 200] = 0x7f
+@pytest.mark.parametrize("R,N,K", [(12, 90, 256), (150, 90, 256), (300, 900, 1100)])
+def test_nan_stays_in_its_row_and_column(R, N, K):
+    if N == 900:  # teams, with an odd number of blocks
+        assert plan(1, R, K, N, torch.float32, given=False)[0] == 2
+    x, xs, w, ws = operands(2, R, 1, N, K)
+    x.view(torch.uint8)[5, K - 56] = 0x7f
     w.view(torch.uint8)[0, 33, 7] = 0xff
-    got = torch.isnan(product(x, xs, w, ws, 256, None, R, torch.float32)).cpu()
+    got = torch.isnan(product(x, xs, w, ws, K, None, R, torch.float32)).cpu()
     want = torch.zeros_like(got)
     want[5], want[:, 33] = True, True
     assert torch.equal(got, want)
 
 
-@pytest.mark.parametrize("R", [3, 130])
+@pytest.mark.parametrize("R", [3, 130, 400])
 def test_sums_of_whole_numbers_are_exact(R):
     # codes -8 .. 8, scales of 1: every sum is a whole number below 2^24
     gen = torch.Generator().manual_seed(R)
