@@ -4,12 +4,13 @@
 // A lookup is the product with a sparse matrix that has one entry a row; the gradient is the product with its transpose, a
 // sum by segments of very different length: most rows of a table no token has, and one token may be a tenth of a batch.
 //
-// The gradient in three steps.  1. The tokens by their id, those of one always in the same order: a workgroup has a range of ids and
-// looks at all tokens, so that it knows by itself how many come before its range, and no workgroup waits for another.
+// The gradient of many tokens in three steps.  1. The tokens by their id, those of one always in the same order: a workgroup has a range
+// of ids and looks at all tokens, so that it knows by itself how many come before its range, and no workgroup waits for another.
 // 2. Tiles of that order, each an equal number of tokens whatever ids they have; a run of one id that lies in a tile is
 // summed up and stored, what crosses a tile's ends goes to the workspace.
 // 3. The parts of the runs that cross tiles are added, always in the same order, and rows without a token are cleared.  Sums in 32
-// bits, rounded once; no atomics on floats.
+// bits, rounded once; no atomics on floats.  Of a few tokens it is one launch, in which every workgroup looks at all tokens for those of
+// its rows.
 #include <algorithm>
 #include <type_traits>
 
@@ -24,7 +25,7 @@ constexpr int kThreads = 256;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMostIds = 256;  // of a workgroup's range
 constexpr int kList = 416;     // tokens of it that a wavefront collects, 256 at a time
-constexpr int kClearRows = 128;  // rows that a workgroup looks at, whether they have a token
+constexpr int kClearRows = 128;  // rows that a workgroup looks at and clears where they have no token
 
 // Groups of `lanes` (a power of two, 64 at most) have an item each: a row, or a tile, and lanes * VEC of its columns.
 struct Spread {
@@ -115,25 +116,39 @@ Sorted sorted_view(char* workspace, int64_t T, int64_t V, int64_t D, int groups)
     return s;
 }
 
-// Rows of the gradient that no token has, as 16-bit halves of zeros, whatever type they have: half of them are cleared beside the
-// sorting and half beside the joins, which both wait more than they work (all of them beside the joins: 8 us more for 65,536
-// rows of 2,048, bf16).
+// Rows of the gradient that no token has, as 16-bit halves of zeros, whatever type they have.  Neighbouring ones are cleared as one
+// piece of memory where nothing lies between them: by rows, their ends write parts of lines, and short ones use few lanes (100 tokens,
+// by rows and so: 262,144 rows of 64 in 16 bits 25 us, 12; 66,727 of 2,280 floats 188, 124).
 struct Clearing {
     uint16_t* __restrict__ rows;  // null: nothing is cleared
     int64_t halves, pitch;
 };
-__device__ __forceinline__ void clear_row(const Clearing& c, int64_t v)
+__device__ __forceinline__ void clear_halves(uint16_t* to, int64_t n)
 {
     typedef uint16_t loose __attribute__((ext_vector_type(8), aligned(2)));
     const int lane = threadIdx.x & 63;
-    uint16_t* const row = c.rows + v * c.pitch;
-    if (c.halves < 8) {
-        if (lane < c.halves) row[lane] = 0;
+    if (n < 8) {
+        if (lane < n) to[lane] = 0;
         return;
     }
-    for (int64_t i = lane * 8; i < c.halves; i += 512) *reinterpret_cast<loose*>(row + min(i, c.halves - 8)) = loose{0, 0, 0, 0, 0, 0, 0, 0};
+    for (int64_t i = lane * 8; i < n; i += 512) *reinterpret_cast<loose*>(to + min(i, n - 8)) = loose{0, 0, 0, 0, 0, 0, 0, 0};
 }
-__device__ __forceinline__ bool cleared_early(int64_t v) { return (v & 1) == 0; }
+// rows v0 + i for the bits i of `which`, by a wavefront
+__device__ __forceinline__ void clear_rows(const Clearing& c, int64_t v0, uint64_t which)
+{
+    while (which) {
+        const int i = __builtin_ctzll(which);
+        const uint64_t others = ~(which >> i);
+        const int run = c.pitch != c.halves ? 1 : others ? __builtin_ctzll(others) : 64;
+        clear_halves(c.rows + (v0 + i) * c.pitch, run * c.halves);
+        which &= run == 64 ? 0 : ~(((1ull << run) - 1) << i);
+    }
+}
+// With many tokens half of the rows are cleared beside the sorting and half beside the joins, which both wait more than they work (all
+// of them beside the joins: 8 us more for 65,536 rows of 2,048, bf16): blocks of kClearBlock in turn (of 1, 4 and 8 rows: these 100.0,
+// 100.4, 102.7 us with their lookup, 50,001 of 1,001 floats 95.7, 92.3, 89.0).
+constexpr int kClearBlock = 4;
+__device__ __forceinline__ bool cleared_early(int64_t v) { return (v / kClearBlock & 1) == 0; }
 
 // ids range .. range + ids_of of a workgroup.  Every wavefront has a run of the tokens and collects those of the range, so that it
 // deals with 64 of them at a time; it counts them by id, the counts are summed up over the wavefronts and the ids, and every wavefront
@@ -281,8 +296,9 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     }
     placed();
     if (!clearing.rows) return;
-    for (int r = wave; r < (int)n; r += kSortWaves)
-        if (none[r] && cleared_early(range + r)) clear_row(clearing, range + r);
+    const int mine = (ids_of + kSortWaves - 1) / kSortWaves, r = wave * mine + lane;  // a wavefront's rows, neighbouring ones
+    static_assert(kMostIds <= 64 * kSortWaves, "");
+    clear_rows(clearing, range + wave * mine, __ballot(lane < mine && r < (int)n && none[min(r, kMostIds - 1)] && cleared_early(range + r)));
 }
 
 // A piece of a row of the gradient, in accesses of 16 bytes at most.
@@ -439,11 +455,10 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedGradArgs 
     __shared__ int many;
     const int64_t block = block0 + blockIdx.x;
     if (block >= join_blocks) {
-        constexpr int kRows = kClearRows / (kJoinThreads / 64);
-        const int64_t v0 = (block - join_blocks) * kClearRows + (threadIdx.x >> 6) * kRows;
-        const int64_t v = v0 + (threadIdx.x & 63);
-        uint64_t rows = __ballot((threadIdx.x & 63) < kRows && v < a.V && !cleared_early(v) && s.start[v] == s.start[v + 1]);
-        for (; rows; rows &= rows - 1) clear_row(clearing, v0 + __builtin_ctzll(rows));
+        constexpr int kMine = kClearRows / (kJoinThreads / 64);  // a wavefront's rows, of which half are cleared late
+        const int lane = threadIdx.x & 63;
+        const int64_t v0 = (block - join_blocks) * kClearRows + (threadIdx.x >> 6) * kMine, v = v0 + lane;
+        clear_rows(clearing, v0, __ballot(lane < kMine && v < a.V && !cleared_early(v) && s.start[min(v, a.V - 1)] == s.start[min(v, a.V - 1) + 1]));
         return;
     }
     const int sub = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
@@ -522,6 +537,161 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedGradArgs 
     }
 }
 
+constexpr int kFewTokens = 8192, kFewThreads = 1024, kFewWaves = kFewThreads / 64, kFewRows = 1024;
+
+// The gradient of a few tokens in one launch: workgroup b has the rows b, b + 2^shift, .. (so that frequent ids, which vocabularies have
+// first, are different workgroups'), looks at all tokens and lists those of its rows.  A wavefront has a row and lanes * VEC columns and
+// adds up the tokens that the list has for the row; a row of many tokens is the whole workgroup's, whose wavefronts share the list.
+// The rows that a workgroup clears are others, neighbouring ones.
+template <typename T, typename G, int VEC, bool ADD>
+__global__ __launch_bounds__(kFewThreads) void embed_few_kernel(EmbedGradArgs a, Clearing clearing, int shift)
+{
+    constexpr int kAhead = 8, kMany = 32;  // tokens on their way; more of them are a row of many
+    __shared__ uint16_t tokens[kFewTokens];
+    __shared__ uint16_t rows_of[kFewTokens];
+    __shared__ int count[kFewRows], found[kFewWaves];
+    __shared__ bool busy[ADD ? 1 : kFewRows];  // of the rows to be cleared
+    __shared__ float shares[kFewWaves][VEC][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int64_t b = blockIdx.x, step = 1ll << shift;
+    const int rows = (int)((a.V - b + step - 1) >> shift);  // kFewRows at most
+    static_assert(kFewRows == kFewThreads && kFewRows == 64 * kFewWaves && kFewTokens <= 65536, "");
+    count[threadIdx.x] = 0;
+    const int clear_each = (int)((a.V + (int64_t)gridDim.x * gridDim.y - 1) / ((int64_t)gridDim.x * gridDim.y));  // kFewRows at most
+    const int64_t clear0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (clear_each);
+    if (!ADD) busy[threadIdx.x] = false;
+    // a wavefront has a run of the tokens
+    constexpr int kEach = kFewTokens / kFewThreads;
+    int32_t id[kEach];
+    uint64_t hits[kEach];
+    int fill = 0;
+    const int share = ((int)a.T + kFewThreads - 1) / kFewThreads * 64;  // kEach * 64 at most
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int at = wave * share + i * 64 + lane;
+        id[i] = a.ids[min(at, (int)a.T - 1)];
+        id[i] = (int)(i * 64 < share) & (int)(at < a.T) ? id[i] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        hits[i] = __ballot(id[i] >= 0 && id[i] < a.V && (id[i] & (step - 1)) == b);
+        fill += __popcll(hits[i]);
+    }
+    if (lane == 0) found[wave] = fill;
+    __syncthreads();
+    if (!ADD) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+            if (id[i] >= clear0 && id[i] < clear0 + clear_each && id[i] < a.V) busy[id[i] - clear0] = true;
+    }
+    int at = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+        at += w < wave ? found[w] : 0;
+        all += found[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (hits[i] >> lane & 1) {
+            const int to = at + __popcll(hits[i] & ((1ull << lane) - 1)), row = id[i] >> shift;
+            tokens[to] = (uint16_t)(wave * share + i * 64 + lane);
+            rows_of[to] = (uint16_t)row;
+            atomicAdd(&count[row], 1);  // (whole numbers)
+        }
+        at += __popcll(hits[i]);
+    }
+    __syncthreads();
+    // sum += the rows of dout of the list's entries from .. to that are row r's, in their order
+    const auto add_tokens = [&](int r, int from, int to, int64_t first, float (&sum)[VEC]) {
+        const T* __restrict__ dout = static_cast<const T*>(a.dout) + first;
+        for (int e0 = from; e0 < to; e0 += 64) {
+            const int e = e0 + lane;
+            const bool mine = e < to && rows_of[e] == r;
+            const int token = e < to ? tokens[e] : 0;
+            uint64_t left = __ballot(mine);
+            while (__popcll(left) >= kAhead) {
+                Columns<T, VEC> x[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    x[u].load(dout + (int64_t)__builtin_amdgcn_readlane(token, __builtin_ctzll(left)) * a.ldd);
+                    left &= left - 1;
+                }
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) sum[i] += x[u].v[i];
+            }
+            if (left) {
+                // (in place of one that is not there, the last, and not added)
+                const int n = __popcll(left);
+                Columns<T, VEC> x[kAhead];
+#pragma unroll
+                for (int u = 0; u + 1 < kAhead; ++u) {
+                    x[u].load(dout + (int64_t)__builtin_amdgcn_readlane(token, __builtin_ctzll(left)) * a.ldd);
+                    left = left & (left - 1) ? left & (left - 1) : left;
+                }
+#pragma unroll
+                for (int u = 0; u + 1 < kAhead; ++u)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) sum[i] += u < n ? x[u].v[i] : 0.0f;
+            }
+        }
+    };
+    const int pieces = (int)((a.D + 64 * VEC - 1) / (64 * VEC));
+    const auto row_of = [&](int r) { return b + ((int64_t)r << shift); };
+    // a wavefront's rows, as many as lanes at most
+    const int own = lane * kFewWaves + wave, n = own < rows ? count[own] : -1;
+    if constexpr (!ADD) {
+        const int mine = (clear_each + kFewWaves - 1) / kFewWaves, r = wave * mine + lane;  // a wavefront's rows, neighbouring ones
+        clear_rows(clearing, clear0 + wave * mine,
+                   __ballot(lane < mine && r < clear_each && clear0 + r < a.V && !busy[min(r, kFewRows - 1)]));
+    }
+    for (uint64_t left = __ballot(n > 0 && n <= kMany); left; left &= left - 1) {
+        const int r = __builtin_ctzll(left) * kFewWaves + wave;
+        const int64_t v = row_of(r);
+        for (int piece = blockIdx.y; piece < pieces; piece += gridDim.y) {
+            const int64_t c = ((int64_t)piece * 64 + lane) * VEC;
+            const bool there = c < a.D;
+            const int64_t first = there ? piece_first<VEC>(c, a.D) : 0;
+            float sum[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
+            GradPiece<G, VEC> was;
+            if (ADD) was.load(static_cast<const G*>(a.dweights) + v * a.ldw + first);
+            add_tokens(r, 0, all, first, sum);
+            if (there) store_row<ADD>(a, v, first, (int)(c - first), sum, was);
+        }
+    }
+    for (int g = 0; g < rows; g += 64)
+    for (uint64_t left = __ballot(g + lane < rows && count[min(g + lane, rows - 1)] > kMany); left; left &= left - 1) {
+        const int r = g + __builtin_ctzll(left), each = (all + kFewWaves - 1) / kFewWaves, from = min(wave * each, all);
+        const int64_t v = row_of(r);
+        for (int piece = blockIdx.y; piece < pieces; piece += gridDim.y) {
+            const int64_t c = ((int64_t)piece * 64 + lane) * VEC;
+            const bool there = c < a.D;
+            const int64_t first = there ? piece_first<VEC>(c, a.D) : 0;
+            float sum[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) sum[i] = 0.0f;
+            add_tokens(r, from, min(from + each, all), first, sum);
+            __syncthreads();  // the shares before are read
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) shares[wave][i][lane] = sum[i];
+            __syncthreads();
+            if (wave != piece % kFewWaves || !there) continue;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                sum[i] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kFewWaves; ++w) sum[i] += shares[w][i][lane];
+            }
+            GradPiece<G, VEC> was;
+            if (ADD) was.load(static_cast<const G*>(a.dweights) + v * a.ldw + first);
+            store_row<ADD>(a, v, first, (int)(c - first), sum, was);
+        }
+    }
+}
+
 template <typename T, int VEC, int TOKENS>
 hipError_t embed_tokens(const EmbedArgs& a, const Spread& sp, hipStream_t s)
 {
@@ -542,6 +712,21 @@ hipError_t embed(const EmbedArgs& a, hipStream_t s)
 template <typename T, typename G, int VEC, bool ADD>
 hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
 {
+    const int64_t halves = sizeof(G) / 2;
+    const Clearing clearing = {ADD ? nullptr : static_cast<uint16_t*>(a.dweights), a.D * halves, a.ldw * halves};
+    // One launch for a few tokens.  It reads a frequent token's rows by one compute unit, and where a large table is cleared that comes on
+    // top.  (us, three launches and one, ids' frequency one over their rank, 16 bits: 92 tokens, 496 rows of 557 15.4, 5.0; 1,498, 551 of
+    // 256 19.0, 7.6; 4,096, 32,000 of 1,024 41.2, 20.5; 8,192, 8,000 of 512 35.0, 19.0; 8,192, 65,536 of 2,048 82.9, 88.2, and added up
+    // 64.6, 36.1.  At its worst, all tokens of one id, 4,096 of 1,024 take 34.5, 53.7.)
+    if (a.T > 0 && a.T <= kFewTokens && a.V <= 1 << 22 && (ADD || a.T <= 1024 || a.V * a.D * (int64_t)sizeof(G) <= 128 << 20)) {
+        // 256 workgroups, by rows first; columns are shared by four of them where there are so many, so that a frequent token's are
+        const int64_t pieces = (a.D + 64 * VEC - 1) / (64 * VEC), four = std::min<int64_t>(pieces, 4);
+        int shift = 0;
+        while ((int64_t)kFewRows << shift < a.V || (four << shift < 256 && 2ll << shift <= a.V)) ++shift;
+        const int64_t across = std::min(pieces, std::max<int64_t>(four, 256 >> shift));
+        embed_few_kernel<T, G, VEC, ADD><<<dim3(1u << shift, (unsigned)across), kFewThreads, 0, s>>>(a, clearing, shift);
+        return hipGetLastError();
+    }
     const Spread sp = spread<VEC>(a.D);
     const Sorted st = sorted_view(a.workspace, a.T, a.V, a.D, kThreads / sp.lanes);
     // 512 ranges, or, with so many tokens that looking at them all counts, 256 (us of the gradient, 512 and 256: 16,384 tokens, 65,536
@@ -549,8 +734,6 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
     const int64_t ranges = a.T < 32768 ? 512 : 256;
     int ids_of = 1;
     while (ids_of < kMostIds && ids_of * ranges < a.V) ids_of *= 2;
-    const int64_t halves = sizeof(G) / 2;
-    const Clearing clearing = {ADD ? nullptr : static_cast<uint16_t*>(a.dweights), a.D * halves, a.ldw * halves};
     hipError_t err = launch_parts((a.V + ids_of - 1) / ids_of, kSortThreads, [&](unsigned grid, int64_t block0) {
         embed_sort_kernel<<<grid, kSortThreads, kSortWaves * ids_of * 4, s>>>(a.ids, a.T, a.V, ids_of, st.start, st.key, st.order, clearing, block0);
     });

@@ -21,7 +21,7 @@ def plan(G, R, K, N, dtype, given=True, src=False, x_rows=None, compute_units=25
     (1, 1, 4_096, 4_096, BF16, (0, 16, 16, 0)),
     (1, 32, 8_192, 8_192, BF16, (0, 32, 32, 0)),
     (8, 8, 8_192, 1_024, F16, (0, 16, 16, 0)),
-    (64, 64, 2_048, 1_408, F16, (0, 16, 16, 0)),
+    (64, 64, 2_048, 1_408, F16, (0, 16, 16, 2)),
     (1, 128, 4_096, 256, BF16, (0, 16, 16, 0)),
     (1, 256, 4_096, 4_096, BF16, (2, 64, 128, 0)),
     (1, 1_024, 4_096, 4_096, BF16, (2, 128, 128, 0)),

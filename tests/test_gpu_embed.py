@@ -28,6 +28,17 @@ def draw_ids(kind, T, V, seed=0):
     return torch.from_numpy(ids.astype(np.int32))
 
 
+# The gradient of a few tokens goes in one launch, of more in three.  With so many tokens beside the real ones that no row has, and whose
+# gradients are NaN, small sizes take the three.
+OTHERS = [0, 8_300]
+
+
+def among(others, ids, d):
+    before, behind = torch.full((others // 3,), -1, dtype=torch.int32), torch.full((others - others // 3,), -1, dtype=torch.int32)
+    nan = lambda n: torch.full((len(n), d.shape[1]), float("nan"), dtype=d.dtype)  # noqa: E731
+    return (torch.cat([before, ids, behind]), torch.cat([nan(before), d, nan(behind)])) if others else (ids, d)
+
+
 def workspace(T, V, D):
     return torch.full((binding.sgap_embed_grad_workspace_size(T, V, D),), 0x5a, dtype=torch.uint8, device="cuda")
 
@@ -63,19 +74,37 @@ def test_infinities_and_nan_of_a_row_stay_its_own():
     assert_within(out, torch.stack([w[2], w[0], torch.zeros(3), w[1]]).double() * 0.5, 0.0)
 
 
+@pytest.mark.parametrize("others", OTHERS)
 @pytest.mark.parametrize("dtype,grad_dtype", [(t, t) for t in TYPES] + [(torch.float16, torch.float32), (torch.bfloat16, torch.float32)])
 @pytest.mark.parametrize("T,V,D,kind", [
     (1, 1, 1, "one"), (1, 700, 64, "uniform"), (31, 3, 5, "mixed"), (32, 4, 64, "one"), (33, 4, 64, "one"), (64, 2, 8, "sorted"), (65, 9, 129, "sorted"),
     (300, 40, 1001, "mixed"), (1000, 513, 96, "skewed"), (1025, 1500, 520, "skewed"), (2048, 1, 16, "one"), (700, 90, 8, "none"),
     (4096, 20000, 40, "skewed"), (3000, 5, 264, "uniform"), (129, 65, 4104, "skewed"),
 ])
-def test_gradient(T, V, D, kind, dtype, grad_dtype):
-    ids, d = draw_ids(kind, T, V, seed=T), random(T + V, T, D, dtype=dtype)
-    grad, ws = filled(grad_dtype, V, D), workspace(T, V, D)
-    binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda(), grad, scale=0.75, workspace=ws)
+def test_gradient(T, V, D, kind, dtype, grad_dtype, others):
+    ids, d = among(others, draw_ids(kind, T, V, seed=T), random(T + V, T, D, dtype=dtype))
+    grad, ws = filled(grad_dtype, V, D), workspace(len(ids), V, D)
+    binding.sgap_embed_grad(len(ids), V, D, ids.cuda(), d.cuda(), grad, scale=0.75, workspace=ws)
     want, size, tokens = embed_grad(ids, d, V, 0.75)
     assert_within(grad, want, (tokens + 4) * E * size)
     assert not torch.signbit(grad[(tokens[:, 0] == 0).cuda()]).any()
+
+
+# as few ids as there are rows for a wavefront, more, and as many as one launch deals with; tokens up to its limit and behind it; one
+# id's that a whole workgroup adds up, all of them or beside others
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("T,V,D,kind", [(4_097, 1_025, 24, "skewed"), (1_024, 262_150, 136, "skewed"), (1_025, 262_150, 136, "skewed"), (8_192, 300, 40, "skewed"), (8_193, 300, 40, "skewed"),
+                                        (33, 3, 1_032, "one"), (3_000, 2, 2_056, "sorted"), (1_000, 300_007, 8, "skewed"), (50, 1 << 22, 8, "skewed"),
+                                        (50, (1 << 22) + 1, 8, "skewed"), (700, 5_000, 520, "mixed"), (8_192, 70_001, 8, "uniform"), (64, 256, 5, "mixed")])
+def test_gradient_of_few(T, V, D, kind, accumulate):
+    ids, d = draw_ids(kind, T, V, seed=V), random(5, T, D, dtype=torch.bfloat16)
+    was = random(2, V, D) if accumulate else torch.zeros(V, D)
+    grad = was.cuda() if accumulate else filled(torch.float32, V, D)
+    binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda(), grad, scale=-0.5, accumulate=accumulate, workspace=workspace(T, V, D))
+    want, size, tokens = embed_grad(ids, d, V, -0.5)
+    assert_within(grad, want + was.double(), (tokens + 5) * E * (size + was.double().abs()))
+    none = tokens[:, 0] == 0
+    assert torch.equal(grad.cpu()[none], was[none]) and (accumulate or not torch.signbit(grad[none.cuda()]).any())
 
 
 # more tokens than 1,024 tiles (of rows of 2,048, and fewer of longer ones) of 8 hold, so that tiles are longer; more ids than 512 ranges
@@ -90,12 +119,14 @@ def test_gradient_of_many(T, V, D, kind):
     assert_within(grad, want, (tokens + 4) * E * size)
 
 
+@pytest.mark.parametrize("others", OTHERS)
 @pytest.mark.parametrize("dtype,grad_dtype", [(torch.float32, torch.float32), (torch.float16, torch.float16), (torch.bfloat16, torch.float32)])
 @pytest.mark.parametrize("T,V,D,kind", [(1, 5, 3, "uniform"), (100, 30, 77, "mixed"), (500, 12, 1001, "skewed"), (333, 1000, 136, "skewed"), (90, 7, 64, "none")])
-def test_gradient_is_added(T, V, D, kind, dtype, grad_dtype):
-    ids, d, was = draw_ids(kind, T, V), random(1, T, D, dtype=dtype), random(2, V, D, dtype=grad_dtype)
+def test_gradient_is_added(T, V, D, kind, dtype, grad_dtype, others):
+    ids, d = among(others, draw_ids(kind, T, V), random(1, T, D, dtype=dtype))
+    was = random(2, V, D, dtype=grad_dtype)
     grad = was.cuda()
-    binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda(), grad, scale=-1.5, accumulate=True, workspace=workspace(T, V, D))
+    binding.sgap_embed_grad(len(ids), V, D, ids.cuda(), d.cuda(), grad, scale=-1.5, accumulate=True, workspace=workspace(len(ids), V, D))
     want, size, tokens = embed_grad(ids, d, V, -1.5)
     none = (tokens[:, 0] == 0)
     assert torch.equal(grad.cpu()[none], was[none])
@@ -109,10 +140,12 @@ def test_gradient_of_no_tokens_clears_the_table():
     assert torch.equal(grad, torch.zeros_like(grad))
 
 
+@pytest.mark.parametrize("others", OTHERS)
 @pytest.mark.parametrize("grad_dtype", [torch.float32, torch.float16])
-def test_gradient_with_rows_apart(grad_dtype):
-    T, V, D = 400, 37, 51
-    ids, d = draw_ids("mixed", T, V), random(1, T, D + 9, dtype=torch.float16)
+def test_gradient_with_rows_apart(grad_dtype, others):
+    V, D = 37, 51
+    ids, d = among(others, draw_ids("mixed", 400, V), random(1, 400, D + 9, dtype=torch.float16))
+    T = len(ids)
     grad = filled(grad_dtype, V, D + 6)
     binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda()[:, 3:3 + D], grad[:, 1:1 + D], workspace=workspace(T, V, D))
     want, size, tokens = embed_grad(ids, d[:, 3:3 + D], V, 1.0)
@@ -132,8 +165,9 @@ def test_gradient_against_differences():
     assert abs((grad.cpu().double() * z.double()).sum() - slope) <= ((tokens + 6) * E * size * z.double().abs()).sum()
 
 
-def test_the_same_bits_on_every_call():
-    T, V, D = 3000, 200, 264
+@pytest.mark.parametrize("T", [3_000, 9_000])
+def test_the_same_bits_on_every_call(T):
+    V, D = 200, 264
     ids, d = draw_ids("skewed", T, V).cuda(), random(1, T, D, dtype=torch.bfloat16).cuda()
     first = None
     for _ in range(3):
@@ -143,8 +177,9 @@ def test_the_same_bits_on_every_call():
         assert torch.equal(grad.view(torch.int16), first.view(torch.int16))
 
 
-def test_captured_and_replayed_on_other_tokens():
-    T, V, D = 500, 60, 136
+@pytest.mark.parametrize("T", [500, 8_500])
+def test_captured_and_replayed_on_other_tokens(T):
+    V, D = 60, 136
     ids, d = draw_ids("skewed", T, V).cuda(), random(1, T, D).cuda()
     w, out, grad, ws = random(2, V, D).cuda(), filled(torch.float32, T, D), filled(torch.float32, V, D), workspace(T, V, D)
 
@@ -168,8 +203,9 @@ def test_captured_and_replayed_on_other_tokens():
         assert_within(out, embed(ids.cpu(), w.cpu(), 1.0), 0.0)
 
 
-def test_two_streams_with_a_workspace_each():
-    T, V, D = 2000, 100, 264
+@pytest.mark.parametrize("T", [2_000, 8_500])
+def test_two_streams_with_a_workspace_each(T):
+    V, D = 100, 264
     streams = [torch.cuda.Stream() for _ in range(2)]
     made = []
     for i, s in enumerate(streams):
