@@ -11,6 +11,10 @@
 // 3. The parts of the runs that cross tiles are added, always in the same order, and rows without a token are cleared.  Sums in 32
 // bits, rounded once; no atomics on floats.  Of a few tokens it is one launch, in which every workgroup looks at all tokens for those of
 // its rows.
+//
+// Bound by memory where there are many: 16,384 tokens (a tenth of them one), 65,536 rows of 2,048, bf16: the lookup 16.4 us, 106 MB at
+// 6.5 TB/s; the gradient 76 us: sorting 27, which clears 122 MB, sums 21, which read 67 MB, joins 18, which clear the other half: 339 MB
+// at 4.5 TB/s.  Of few the launches are: 8 rows of 4,096 3.4 us, and 1,498 tokens' gradient in 551 rows of 256 7.6.
 #include <algorithm>
 #include <type_traits>
 
@@ -78,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a, int lanes,
     for (int u = 0; u < TOKENS; ++u) {
         if (t0 + u >= a.T) break;
         T* const out = static_cast<T*>(a.out) + (t0 + u) * a.ldo + first;
-        // many rows are written past the caches, which keep the table's frequent rows (16,384 by 2,048, bf16: 17.1 us, 25.1 without)
+        // many rows are written past the caches, which keep the table's frequent rows (16,384 by 2,048, bf16: 16.4 us, 22.5 without)
         if constexpr (TOKENS > 1) x[u].stream_store(out);
         else x[u].store(out);
     }
@@ -145,7 +149,7 @@ __device__ __forceinline__ void clear_rows(const Clearing& c, int64_t v0, uint64
     }
 }
 // With many tokens half of the rows are cleared beside the sorting and half beside the joins, which both wait more than they work (all
-// of them beside the joins: 8 us more for 65,536 rows of 2,048, bf16): blocks of kClearBlock in turn (of 1, 4 and 8 rows: these 100.0,
+// of them beside the joins: 83 us in place of 76 for 65,536 rows of 2,048, bf16): blocks of kClearBlock in turn (of 1, 4 and 8 rows: these 100.0,
 // 100.4, 102.7 us with their lookup, 50,001 of 1,001 floats 95.7, 92.3, 89.0).
 constexpr int kClearBlock = 4;
 __device__ __forceinline__ bool cleared_early(int64_t v) { return (v / kClearBlock & 1) == 0; }
@@ -704,8 +708,8 @@ template <typename T, int VEC>
 hipError_t embed(const EmbedArgs& a, hipStream_t s)
 {
     const Spread sp = spread<VEC>(a.D);
-    // two tokens to a group where that leaves wavefronts enough for the chip (16,384 by 2,048, bf16: 27.8 us with one, 25.8, 26.7 with
-    // four)
+    // two tokens to a group where that leaves wavefronts enough for the chip, and many rows are written (16,384 by 2,048, bf16: 23.9 us
+    // with one, 16.4, 16.8 with four)
     return blocks_of(sp, a.T) >= 2048 ? embed_tokens<T, VEC, 2>(a, sp, s) : embed_tokens<T, VEC, 1>(a, sp, s);
 }
 

@@ -10,6 +10,11 @@
 //            Every instruction for these codes on this chip does so.
 //   numbers  the codes as bfloat16, which holds them all, and its matrix instruction: exact products, added in 32 bits, at 3.5
 //            times the matrix unit's time.  For results of floats, and for few rows, where the weights' bytes are the bound.
+//
+// Few rows are bound by the weights' bytes (64 rows over 64 groups, 2,048 x 1,408: 119 MB in 24.1 us, 4.9 TB/s) or, where these are few too,
+// by a block's way through the wavefront; many rows by the tiles' loads beside the products: 256 x 256 tiles take 1.46 to 1.83 us a block
+// from one run to the next, 1.3 without the products and 1.3 without the loads, and some 9 us to start and to store.  8,192 rows, 4,096 x
+// 8,192, 16 bits: 260 us, 2.1 PFLOP/s, where the library's product of such numbers with one scale reaches 2.5.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
