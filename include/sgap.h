@@ -781,9 +781,10 @@ int sgap_route_combine_grad(int64_t T, int64_t k, int64_t D, int dtype, const vo
  *            the device, but nothing outside 0 .. R is touched whatever they
  *            hold); null: one group of all rows, G = 1
  *   X        x_rows rows of K elements, ldx apart
- *   src      null: src(r) = r (and src_div is 1, unless R is 0); else R entries, and row r takes row
- *            src[r] / src_div of X: with sgap_route_topk's order and its k that
- *            is the token of each pair.  A row outside X counts as zeros.
+ *   src      null: src(r) = r (and src_div is 1, unless R is 0); else R entries,
+ *            and row r takes row src[r] / src_div of X: with sgap_route_topk's
+ *            order and its k that is the token of each pair.  A row outside X
+ *            counts as zeros.
  *   W        G matrices, contiguous: SGAP_WEIGHTS_NK N x K (Y = X W^T), or
  *            SGAP_WEIGHTS_KN K x N (Y = X W)
  *   Y        R x N, rows ldy apart

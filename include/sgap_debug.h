@@ -107,11 +107,11 @@ int sgap_debug_group_seg_reduce(const float* in, const int32_t* span, float* out
  *     workgroup's part of the result; plan[3]: 1 where X is addressed in 64
  *     bits; plan[4]: 1 where workgroups begin at different places of the inner
  *     dimension; plan[5]: 1 where rows are read element by element.
- *   sgap_debug_f8_plan: the same of sgap_grouped_mm_f8.  plan[0]: teams
- *     that make tiles and share the inner dimension, 0 where wavefronts do; plan[1], plan[2]: rows and
- *     columns of a workgroup's part of the result; plan[3]: 1 where gathered
- *     rows are addressed in 64 bits, 2 where wavefronts have eight blocks on
- *     their way.
+ *   sgap_debug_f8_plan: the same of sgap_grouped_mm_f8.  plan[0]: teams that
+ *     make tiles and share the inner dimension, 0 where wavefronts do;
+ *     plan[1], plan[2]: rows and columns of a workgroup's part of the result;
+ *     plan[3]: 1 where gathered rows are addressed in 64 bits, 2 where
+ *     wavefronts have eight blocks on their way.
  */
 int64_t sgap_debug_tile_deal(int64_t tiles, int grid, int block, int64_t* out_tiles, int64_t capacity);
 int sgap_debug_plan_nnz_serial(int group_size, int lanes_per_row, int cols_per_lane, int64_t nnz_hint,

@@ -222,7 +222,8 @@ def test_two_streams_with_a_workspace_each(T):
         assert_within(grad, want, (tokens + 4) * E * size)
 
 
-def test_places_beyond_32_bits():
+@pytest.mark.parametrize("others", OTHERS)
+def test_places_beyond_32_bits(others):
     # a table of 4.3 GB, whose last rows lie beyond 2^32 bytes (2^31 elements), and a gradient of the same size
     V, D, T = 1 << 19, 4104, 64
     ids = torch.arange(V - T, V, dtype=torch.int32).flip(0)
@@ -232,7 +233,8 @@ def test_places_beyond_32_bits():
     out = filled(torch.float16, T, D)
     binding.sgap_embed(T, V, D, ids.cuda(), w, out)
     assert torch.equal(out.cpu(), rows.flip(0))
-    binding.sgap_embed_grad(T, V, D, ids.cuda(), out, w, workspace=workspace(T, V, D))
+    ids, out = among(others, ids, out.cpu())
+    binding.sgap_embed_grad(len(ids), V, D, ids.cuda(), out.cuda(), w, workspace=workspace(len(ids), V, D))
     assert torch.equal(w[V - T:].cpu(), rows)
     assert not w[:V - T].any()
 
