@@ -13,8 +13,8 @@
 // its rows.
 //
 // Bound by memory where there are many: 16,384 tokens (a tenth of them one), 65,536 rows of 2,048, bf16: the lookup 16.4 us, 106 MB at
-// 6.5 TB/s; the gradient 76 us: sorting 27, which clears 122 MB, sums 21, which read 67 MB, joins 18, which clear the other half: 339 MB
-// at 4.5 TB/s.  Of few the launches are: 8 rows of 4,096 3.4 us, and 1,498 tokens' gradient in 551 rows of 256 7.6.
+// 6.5 TB/s; the gradient 74 us: sorting 27, which clears 122 MB, sums 21, which read 67 MB, joins 18, which clear the other half: 339 MB
+// at 4.6 TB/s.  Of few the launches are: 8 rows of 4,096 3.4 us, and 1,498 tokens' gradient in 551 rows of 256 7.6.
 #include <algorithm>
 #include <type_traits>
 
@@ -127,6 +127,9 @@ struct Clearing {
     uint16_t* __restrict__ rows;  // null: nothing is cleared
     int64_t halves, pitch;
 };
+// PAST: past the caches, which keep what other kernels read (65,536 rows of 2,048, bf16, lookup and gradient: 99.9 us, 90.7; one launch of few
+// tokens has nothing to keep: 66,727 rows of 2,280 floats 124 us, 145)
+template <bool PAST>
 __device__ __forceinline__ void clear_halves(uint16_t* to, int64_t n)
 {
     typedef uint16_t loose __attribute__((ext_vector_type(8), aligned(2)));
@@ -135,22 +138,27 @@ __device__ __forceinline__ void clear_halves(uint16_t* to, int64_t n)
         if (lane < n) to[lane] = 0;
         return;
     }
-    for (int64_t i = lane * 8; i < n; i += 512) *reinterpret_cast<loose*>(to + min(i, n - 8)) = loose{0, 0, 0, 0, 0, 0, 0, 0};
+    for (int64_t i = lane * 8; i < n; i += 512) {
+        loose* const at = reinterpret_cast<loose*>(to + min(i, n - 8));
+        if constexpr (PAST) __builtin_nontemporal_store(loose{0, 0, 0, 0, 0, 0, 0, 0}, at);
+        else *at = loose{0, 0, 0, 0, 0, 0, 0, 0};
+    }
 }
 // rows v0 + i for the bits i of `which`, by a wavefront
+template <bool PAST>
 __device__ __forceinline__ void clear_rows(const Clearing& c, int64_t v0, uint64_t which)
 {
     while (which) {
         const int i = __builtin_ctzll(which);
         const uint64_t others = ~(which >> i);
         const int run = c.pitch != c.halves ? 1 : others ? __builtin_ctzll(others) : 64;
-        clear_halves(c.rows + (v0 + i) * c.pitch, run * c.halves);
+        clear_halves<PAST>(c.rows + (v0 + i) * c.pitch, run * c.halves);
         which &= run == 64 ? 0 : ~(((1ull << run) - 1) << i);
     }
 }
 // With many tokens half of the rows are cleared beside the sorting and half beside the joins, which both wait more than they work (all
 // of them beside the joins: 83 us in place of 76 for 65,536 rows of 2,048, bf16): blocks of kClearBlock in turn (of 1, 4 and 8 rows: these 100.0,
-// 100.4, 102.7 us with their lookup, 50,001 of 1,001 floats 95.7, 92.3, 89.0).
+// 100.4, 102.7 us with their lookup, 50,001 of 1,001 floats 95.7, 92.3, 89.0, not past the caches).
 constexpr int kClearBlock = 4;
 __device__ __forceinline__ bool cleared_early(int64_t v) { return (v / kClearBlock & 1) == 0; }
 
@@ -302,7 +310,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     if (!clearing.rows) return;
     const int mine = (ids_of + kSortWaves - 1) / kSortWaves, r = wave * mine + lane;  // a wavefront's rows, neighbouring ones
     static_assert(kMostIds <= 64 * kSortWaves, "");
-    clear_rows(clearing, range + wave * mine, __ballot(lane < mine && r < (int)n && none[min(r, kMostIds - 1)] && cleared_early(range + r)));
+    clear_rows<true>(clearing, range + wave * mine, __ballot(lane < mine && r < (int)n && none[min(r, kMostIds - 1)] && cleared_early(range + r)));
 }
 
 // A piece of a row of the gradient, in accesses of 16 bytes at most.
@@ -462,7 +470,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedGradArgs 
         constexpr int kMine = kClearRows / (kJoinThreads / 64);  // a wavefront's rows, of which half are cleared late
         const int lane = threadIdx.x & 63;
         const int64_t v0 = (block - join_blocks) * kClearRows + (threadIdx.x >> 6) * kMine, v = v0 + lane;
-        clear_rows(clearing, v0, __ballot(lane < kMine && v < a.V && !cleared_early(v) && s.start[min(v, a.V - 1)] == s.start[min(v, a.V - 1) + 1]));
+        clear_rows<true>(clearing, v0, __ballot(lane < kMine && v < a.V && !cleared_early(v) && s.start[min(v, a.V - 1)] == s.start[min(v, a.V - 1) + 1]));
         return;
     }
     const int sub = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = kJoinThreads / lanes;
@@ -647,7 +655,7 @@ __global__ __launch_bounds__(kFewThreads) void embed_few_kernel(EmbedGradArgs a,
     const int own = lane * kFewWaves + wave, n = own < rows ? count[own] : -1;
     if constexpr (!ADD) {
         const int mine = (clear_each + kFewWaves - 1) / kFewWaves, r = wave * mine + lane;  // a wavefront's rows, neighbouring ones
-        clear_rows(clearing, clear0 + wave * mine,
+        clear_rows<false>(clearing, clear0 + wave * mine,
                    __ballot(lane < mine && r < clear_each && clear0 + r < a.V && !busy[min(r, kFewRows - 1)]));
     }
     for (uint64_t left = __ballot(n > 0 && n <= kMany); left; left &= left - 1) {
