@@ -8,8 +8,7 @@
 // What is no finite number becomes NaN and has no part in its block's scale.
 //
 // Bound by memory: a value is read once and its codes are written once, 128 bytes of a block side by side.  16,384 rows of 4,096,
-// bf16: 39.0 us, 5.2 TB/s; weights of 16 x 4,096 x 2,048, bf16: 77 us, 5.2 TB/s, transposed too 102 us, 5.3 TB/s (a copy reaches
-// 5.5).  A thread's loads are all on their way together: where a row's length makes each a branch of its own, the weights took 118 us.
+// bf16: 39.0 us, 5.2 TB/s; weights of 16 x 4,096 x 2,048, bf16: 69 us, 5.9 TB/s, transposed too 93 us, 5.8 TB/s (a copy reaches 5.5).  A thread's loads are all on their way together: where a row's length makes each a branch of its own, the weights took 118 us.
 #include <type_traits>
 
 #include "sgap_tokens.hpp"
@@ -54,12 +53,16 @@ template <typename T, bool EIGHTS>
 struct Eight {
     static constexpr int P = Piece<T>::kCount;
     piece_t<T> v[8 / P];
+    template <bool PAST = false>
     __device__ __forceinline__ void load(const T* __restrict__ row, int64_t c, int64_t K)
     {
         if (EIGHTS || c + 8 <= K) {
             const T* const from = row + (!EIGHTS || c < K ? c : 0);
 #pragma unroll
-            for (int h = 0; h < 8 / P; ++h) v[h] = load_piece(from + h * P);
+            for (int h = 0; h < 8 / P; ++h) {
+                if constexpr (PAST) v[h] = __builtin_nontemporal_load(reinterpret_cast<const typename Piece<T>::loose*>(from + h * P));
+                else v[h] = load_piece(from + h * P);
+            }
             return;
         }
 #pragma unroll
@@ -103,8 +106,16 @@ __global__ __launch_bounds__(kThreads) void f8_rows_kernel(F8RowsArgs a, int64_t
     }
 }
 
-// A workgroup has a block of 128 x 128 weights: sixteen lanes a row of them, sixteen rows at a time.
-template <typename T, bool BOTH, bool EIGHTS>
+template <bool PAST>
+__device__ __forceinline__ void store_codes(uint8_t* to, uint32_t lo, uint32_t hi)
+{
+    const uint64_t both = (uint64_t)hi << 32 | lo;
+    if constexpr (PAST) __builtin_nontemporal_store(both, reinterpret_cast<uint64_t*>(to));
+    else *reinterpret_cast<uint64_t*>(to) = both;
+}
+
+// A workgroup has a block of 128 x 128 weights: sixteen lanes a row of them, sixteen rows at a time.  PAST: past the caches.
+template <typename T, bool BOTH, bool EIGHTS, bool PAST>
 __global__ __launch_bounds__(kThreads) void f8_weights_kernel(F8WeightsArgs a, int64_t blocks_n, int64_t blocks_k, int64_t block0)
 {
     constexpr int kTurns = kF8Block / (kThreads / 16), kPitch = kF8Block + 4;
@@ -119,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void f8_weights_kernel(F8WeightsArgs a, i
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int64_t n = min(n0 + i * (kThreads / 16) + line, a.N - 1);
-        held[i].load(static_cast<const T*>(a.W) + (g * a.N + n) * a.K, k0 + part * 8, a.K);
+        held[i].template load<PAST>(static_cast<const T*>(a.W) + (g * a.N + n) * a.K, k0 + part * 8, a.K);
     }
     const auto numbers = [&](int i, float (&x)[8]) {
         held[i].numbers(x, n0 + i * (kThreads / 16) + line < a.N && (!EIGHTS || k0 + part * 8 < a.K));
@@ -148,7 +159,7 @@ __global__ __launch_bounds__(kThreads) void f8_weights_kernel(F8WeightsArgs a, i
         float x[8];
         numbers(i, x);
         const uint32_t lo = encode(x, s.back), hi = encode(x + 4, s.back);
-        if (n0 + n < a.N) *reinterpret_cast<uint2*>(a.codes + ((g * a.N + n0 + n) * blocks_k + kb) * kF8Block + part * 8) = make_uint2(lo, hi);
+        if (n0 + n < a.N) store_codes<PAST>(a.codes + ((g * a.N + n0 + n) * blocks_k + kb) * kF8Block + part * 8, lo, hi);
         if constexpr (BOTH) {
             *reinterpret_cast<uint32_t*>(tile + n * kPitch + part * 8) = lo;
             *reinterpret_cast<uint32_t*>(tile + n * kPitch + part * 8 + 4) = hi;
@@ -177,7 +188,7 @@ __global__ __launch_bounds__(kThreads) void f8_weights_kernel(F8WeightsArgs a, i
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int64_t k = k0 + columns4 * 4 + c;
-                if (k < a.K) *reinterpret_cast<uint2*>(a.codes_t + ((g * a.K + k) * blocks_n + nb) * kF8Block + rows8 * 8) = make_uint2(w[c], w[4 + c]);
+                if (k < a.K) store_codes<PAST>(a.codes_t + ((g * a.K + k) * blocks_n + nb) * kF8Block + rows8 * 8, w[c], w[4 + c]);
             }
         }
     }
@@ -200,14 +211,22 @@ hipError_t f8_rows(const F8RowsArgs& a, hipStream_t s)
     return a.R * blocks_k < 65536 ? f8_rows<T, 1, true>(a, blocks_k, s) : f8_rows<T, 2, true>(a, blocks_k, s);
 }
 
-template <typename T, bool BOTH>
+template <typename T, bool BOTH, bool PAST>
 hipError_t f8_weights(const F8WeightsArgs& a, hipStream_t s)
 {
     const int64_t blocks_n = f8_blocks(a.N), blocks_k = f8_blocks(a.K);
     return launch_parts(a.G * blocks_n * blocks_k, kThreads, [&](unsigned grid, int64_t block0) {
-        if (a.K % 8) f8_weights_kernel<T, BOTH, false><<<grid, kThreads, 0, s>>>(a, blocks_n, blocks_k, block0);
-        else f8_weights_kernel<T, BOTH, true><<<grid, kThreads, 0, s>>>(a, blocks_n, blocks_k, block0);
+        if (a.K % 8) f8_weights_kernel<T, BOTH, false, PAST><<<grid, kThreads, 0, s>>>(a, blocks_n, blocks_k, block0);
+        else f8_weights_kernel<T, BOTH, true, PAST><<<grid, kThreads, 0, s>>>(a, blocks_n, blocks_k, block0);
     });
+}
+template <typename T, bool BOTH>
+hipError_t f8_weights(const F8WeightsArgs& a, hipStream_t s)
+{
+    // past the caches where values and codes are more than these hold (us through and past them, bf16, both ways round, alone and with a
+    // product of 1,024 rows behind: 4 x 4,096 x 2,048 31.0, 27.0 and 49.2, 49.8; 8 x 53.7, 48.9 and 78.0, 73.8; 16 x 103, 93 and 134, 131;
+    // 1 x 4,096 x 4,096 13.9, 13.4 and 44.0, 48.2)
+    return a.G * a.N * a.K >= 1ll << 26 ? f8_weights<T, BOTH, true>(a, s) : f8_weights<T, BOTH, false>(a, s);
 }
 template <typename T>
 hipError_t f8_weights(const F8WeightsArgs& a, hipStream_t s)

@@ -131,6 +131,19 @@ def test_weights_of_extremes(dtype):
     same(got[0], codes)
 
 
+# more weights than go through the caches: the same as of each matrix by itself, which is few enough
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,K", [(4_700, 4_801), (4_699, 4_808)])
+def test_weights_past_the_caches(N, K, dtype):
+    assert 3 * N * K >= 1 << 26 > N * K
+    w = torch.randn(3, N, K, generator=torch.Generator("cuda").manual_seed(K), device="cuda").to(dtype)
+    for both in (True, False):
+        all_of = to_weights(w, both)
+        for g in range(3):
+            for whole, alone in zip(all_of, to_weights(w[g:g + 1], both)):
+                assert torch.equal(whole[g].view(torch.uint8), alone[0].view(torch.uint8))
+
+
 def test_scales_are_the_smallest_powers():
     for most in (448.0, 448.00003, 447.99997, 1.0, 1e-38, 1e-45, 3.4e38, 0.0):
         s = power_scale(np.array([float(np.float32(most))]))[0]
