@@ -282,23 +282,23 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         for (int l = 0; l < fill; l += 64) {
             const int e = l + lane;
-            const int32_t token = e < fill ? list[e] : 0;
-            const uint32_t in = e < fill ? list_id[e] : 0xffffu;
-            uint64_t left = __ballot(e < fill);
-            while (left) {
-                // the tokens of the id that the lowest lane left has
-                const int leader = __builtin_ctzll(left);
-                const uint32_t which = (uint32_t)__builtin_amdgcn_readlane((int)in, leader);
-                const uint64_t same = __ballot(in == which);
-                int at = 0;
-                if (lane == leader) at = atomicAdd(&own[which], __popcll(same));  // (this wavefront's alone)
-                at = __builtin_amdgcn_readlane(at, leader);
-                if (in == which) {
-                    const int p = at + __popcll(same & ((1ull << lane) - 1));
-                    key[p] = (int32_t)(lo + in);
-                    order[p] = token;
-                }
-                left &= ~same;
+            const bool mine = e < fill;
+            const int32_t token = mine ? list[e] : 0;
+            const uint32_t in = mine ? list_id[e] : 0;
+            // the lanes whose tokens have this one's id, a bit of it at a time (one id after the other, which is slow where a workgroup
+            // has many tokens of many ids: 65,536 tokens, ids' frequency one over their rank, 65,536 rows of 1,024 with their lookup 400 us, 129)
+            uint64_t same = __ballot(mine);
+            for (uint32_t bit = 1; bit < (uint32_t)ids_of; bit <<= 1) {
+                const uint64_t has = __ballot((in & bit) != 0);
+                same &= (in & bit) != 0 ? has : ~has;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            int at = 0;
+            if (mine && rank == 0) at = atomicAdd(&own[in], __popcll(same));  // (this wavefront's alone)
+            at = __shfl(at, mine ? __builtin_ctzll(same) : lane) + rank;
+            if (mine) {
+                key[at] = (int32_t)(lo + in);
+                order[at] = token;
             }
         }
     };
@@ -741,9 +741,9 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
     }
     const Spread sp = spread<VEC>(a.D);
     const Sorted st = sorted_view(a.workspace, a.T, a.V, a.D, kThreads / sp.lanes);
-    // 512 ranges, or, with so many tokens that looking at them all counts, 256 (us of the gradient, 512 and 256: 16,384 tokens, 65,536
-    // rows of 2,048 78.5, 81.7; 65,536 tokens, 32,000 rows of 512 83.5, 72.7)
-    const int64_t ranges = a.T < 32768 ? 512 : 256;
+    // 256 ranges, one for each compute unit (us of lookup and gradient, 512 and 256: 16,384 tokens, 65,536 rows of 2,048 95.7, 95.0; 16,384
+    // rows 62.3, 57.8; 12,000 tokens, 50,001 rows of 64 26.1, 22.1)
+    constexpr int64_t ranges = 256;
     int ids_of = 1;
     while (ids_of < kMostIds && ids_of * ranges < a.V) ids_of *= 2;
     hipError_t err = launch_parts((a.V + ids_of - 1) / ids_of, kSortThreads, [&](unsigned grid, int64_t block0) {

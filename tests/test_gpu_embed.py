@@ -107,12 +107,25 @@ def test_gradient_of_few(T, V, D, kind, accumulate):
     assert torch.equal(grad.cpu()[none], was[none]) and (accumulate or not torch.signbit(grad[none.cuda()]).any())
 
 
-# more tokens than 1,024 tiles (of rows of 2,048, and fewer of longer ones) of 8 hold, so that tiles are longer; more ids than 512 ranges
-# of 512; tokens of which one id's fill most tiles
+# more tokens than 1,024 tiles (of rows of 2,048, and fewer of longer ones) of 8 hold, so that tiles are longer; more ids than 256 ranges
+# of 256; tokens of which one id's fill most tiles
 @pytest.mark.parametrize("T,V,D,kind", [(9_000, 40, 2_056, "skewed"), (20_000, 9, 2_050, "one"), (40_000, 300, 24, "skewed"), (70_001, 3, 8, "uniform"),
                                         (200, 300_001, 16, "skewed"), (33_000, 70_000, 40, "skewed")])
 def test_gradient_of_many(T, V, D, kind):
     ids, d = draw_ids(kind, T, V), random(5, T, D)
+    grad, ws = filled(torch.float32, V, D), workspace(T, V, D)
+    binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda(), grad, workspace=ws)
+    want, size, tokens = embed_grad(ids, d, V, 1.0)
+    assert_within(grad, want, (tokens + 4) * E * size)
+
+
+# an id's frequency one over its rank, as words have it: half of the tokens are of one workgroup's ids, hundreds of them among any 256 tokens
+@pytest.mark.parametrize("T,V,D", [(60_001, 70_001, 16), (20_000, 65_536, 24), (9_000, 257, 40)])
+def test_gradient_of_words(T, V, D):
+    g = torch.Generator().manual_seed(T)
+    ids = ((V + 1.0) ** torch.rand(T, generator=g, dtype=torch.float64)).int() - 1
+    ids[torch.rand(T, generator=g) < 0.03] = -1
+    d = random(5, T, D, dtype=torch.bfloat16)
     grad, ws = filled(torch.float32, V, D), workspace(T, V, D)
     binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda(), grad, workspace=ws)
     want, size, tokens = embed_grad(ids, d, V, 1.0)
