@@ -165,9 +165,10 @@ __device__ __forceinline__ bool cleared_early(int64_t v) { return (v / kClearBlo
 // ids range .. range + ids_of of a workgroup.  Every wavefront has a run of the tokens and collects those of the range, so that it
 // deals with 64 of them at a time; it counts them by id, the counts are summed up over the wavefronts and the ids, and every wavefront
 // puts its tokens in their places, always in the same order.  Where they are more than its list holds, it looks at the tokens again.
+// unseen: every other workgroup clears in place of the next one, whatever tokens there are; the later steps write the rows in use.
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t* __restrict__ ids, int64_t T, int64_t V, int ids_of,
                                                                   int32_t* __restrict__ start, int32_t* __restrict__ key,
-                                                                  int32_t* __restrict__ order, Clearing clearing, int64_t block0)
+                                                                  int32_t* __restrict__ order, Clearing clearing, bool unseen, int64_t block0)
 {
     extern __shared__ int32_t count[];  // wavefronts x ids_of: tokens of an id, then the next place
     __shared__ int32_t found[kSortWaves][kList];  // tokens of the range ...
@@ -175,8 +176,14 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
     __shared__ bool none[kMostIds];
     __shared__ int32_t before[kSortWaves], wave_total[kSortWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int64_t range = (block0 + blockIdx.x) * ids_of;
+    const int64_t block = block0 + blockIdx.x, range = (unseen ? block / 2 : block) * ids_of;
     const uint32_t lo = (uint32_t)range, n = (uint32_t)min((int64_t)ids_of, V - range);
+    const int mine = (ids_of + kSortWaves - 1) / kSortWaves, r = wave * mine + lane;  // a wavefront's rows to be cleared, neighbouring ones
+    static_assert(kMostIds <= 64 * kSortWaves, "");
+    if (unseen && block % 2 == 0) {
+        clear_rows<true>(clearing, range + wave * mine, __ballot(lane < mine && r < (int)n && cleared_early(range + r)));
+        return;
+    }
     const int64_t share = ((T + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const int64_t first = min((int64_t)wave * share, T), end = min(first + share, T);
     int32_t* const own = count + wave * ids_of;
@@ -307,9 +314,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(const int32_t*
         scan(placed);
     }
     placed();
-    if (!clearing.rows) return;
-    const int mine = (ids_of + kSortWaves - 1) / kSortWaves, r = wave * mine + lane;  // a wavefront's rows, neighbouring ones
-    static_assert(kMostIds <= 64 * kSortWaves, "");
+    if (unseen || !clearing.rows) return;
     clear_rows<true>(clearing, range + wave * mine, __ballot(lane < mine && r < (int)n && none[min(r, kMostIds - 1)] && cleared_early(range + r)));
 }
 
@@ -744,10 +749,15 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
     // 256 ranges, one for each compute unit (us of lookup and gradient, 512 and 256: 16,384 tokens, 65,536 rows of 2,048 95.7, 95.0; 16,384
     // rows 62.3, 57.8; 12,000 tokens, 50,001 rows of 64 26.1, 22.1)
     constexpr int64_t ranges = 256;
+    // Few of many long rows are in use: cleared without waiting for the tokens, which writes the rows in use twice.  (us of lookup and
+    // gradient after the tokens are known and before, ids' frequencies even / one over their rank: 9,000 tokens, 262,144 rows of 512
+    // floats 123, 113 / 121, 111; 16,384, 65,536 of 1,024 in 16 bits 56.8, 51.4 / 57.6, 53.0; 16,384, 65,536 of 2,048 95.8, 96.4 / 88.1, 84.1;
+    // shorter rows: 9,000, 131,072 of 256 floats 45.5, 48.5 / 45.7, 49.4; more tokens: 10,000, 30,000 of 1,000 39.7, 41.4 / 46.3, 47.7)
+    const bool unseen = !ADD && a.T <= a.V / 4 && a.D * (int64_t)sizeof(G) >= 2048;
     int ids_of = 1;
     while (ids_of < kMostIds && ids_of * ranges < a.V) ids_of *= 2;
-    hipError_t err = launch_parts((a.V + ids_of - 1) / ids_of, kSortThreads, [&](unsigned grid, int64_t block0) {
-        embed_sort_kernel<<<grid, kSortThreads, kSortWaves * ids_of * 4, s>>>(a.ids, a.T, a.V, ids_of, st.start, st.key, st.order, clearing, block0);
+    hipError_t err = launch_parts((a.V + ids_of - 1) / ids_of * (unseen ? 2 : 1), kSortThreads, [&](unsigned grid, int64_t block0) {
+        embed_sort_kernel<<<grid, kSortThreads, kSortWaves * ids_of * 4, s>>>(a.ids, a.T, a.V, ids_of, st.start, st.key, st.order, clearing, unseen, block0);
     });
     if (err != hipSuccess) return err;
     err = launch_parts(st.tiles * sp.column_items, kThreads, [&](unsigned grid, int64_t block0) {

@@ -119,6 +119,22 @@ def test_gradient_of_many(T, V, D, kind):
     assert_within(grad, want, (tokens + 4) * E * size)
 
 
+# long rows of which few are in use; side by side, which are cleared as one piece of memory, and apart; rows that no range divides
+@pytest.mark.parametrize("apart", [0, 7])
+@pytest.mark.parametrize("T,V,D,kind", [(8_193, 33_003, 513, "skewed"), (9_001, 36_005, 516, "mixed"), (1_100, 65_601, 520, "uniform")])
+def test_gradient_of_few_rows_of_many(T, V, D, kind, apart):
+    ids, d = draw_ids(kind, T, V), random(5, T, D, dtype=torch.bfloat16)
+    ids[T // 2], ids[T // 3] = V - 1, -1
+    held = filled(torch.float32, V + 2, D + apart)
+    grad = held[1:V + 1, apart // 2:apart // 2 + D]
+    binding.sgap_embed_grad(T, V, D, ids.cuda(), d.cuda(), grad, scale=-2.0, workspace=workspace(T, V, D))
+    want, size, tokens = embed_grad(ids, d, V, -2.0)
+    assert_within(grad.contiguous(), want, (tokens + 4) * E * size)
+    assert not torch.signbit(grad[(tokens[:, 0] == 0).cuda()]).any()
+    assert torch.isnan(held[0]).all() and torch.isnan(held[V + 1]).all()
+    assert torch.isnan(held[:, :apart // 2]).all() and torch.isnan(held[:, apart // 2 + D:]).all()
+
+
 # an id's frequency one over its rank, as words have it: half of the tokens are of one workgroup's ids, hundreds of them among any 256 tokens
 @pytest.mark.parametrize("T,V,D", [(60_001, 70_001, 16), (20_000, 65_536, 24), (9_000, 257, 40)])
 def test_gradient_of_words(T, V, D):
