@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRows = 64;           // of a tile
-constexpr int kJoinThreads = 1024;  // of a sequence's sum
+constexpr int kJoinThreads = 1024, kManyThreads = 256;  // of a sequence's sum, and of one of many sequences'
 constexpr int kMostExperts = 1024;
 
 // op over 16 lanes or all 64, the same bits in each: 16 lanes by turning them, then the two halves of each 32 and of the 64 changing
@@ -167,6 +167,7 @@ struct Partial {
     float* losses;     // sequences x parts
     int64_t tiles, bytes;
     int parts, part;   // workgroups that share a sequence's experts, and experts of each
+    int threads;       // of those
 };
 Partial partial_view(char* workspace, int64_t T, int64_t E, int64_t S)
 {
@@ -184,11 +185,43 @@ Partial partial_view(char* workspace, int64_t T, int64_t E, int64_t S)
     p.rows = reinterpret_cast<int32_t*>(take(p.tiles * 4));
     // one workgroup for a sequence, or one for 64 of its experts where it has much to read (us of the join, one and several:
     // 35,906 rows of 353 26, 10; 65,536 rows of 512 46, 12; the mean's launch comes to 2)
-    p.part = p.tiles / S * E >= 65536 ? 64 : (int)E;
+    // (Many sequences share the compute units: 1,000 of 16,384 tokens, 128 experts, loss alone with workgroups of 1,024 threads 21.6 us,
+    // of 256 14.3; 20,000 sequences 246, 99; one long one and 999 of a token each 25.3, 20.0; of 65,536 tokens, 256 experts 29.9, 22.8 and 58, 71)
+    p.threads = S >= 512 ? kManyThreads : kJoinThreads;
+    p.part = p.tiles / S * E >= 65536 ? 64 : (int)(E < p.threads ? E : p.threads);
     p.parts = (int)((E + p.part - 1) / p.part);
     p.losses = reinterpret_cast<float*>(take(S * p.parts * 4));
     p.bytes = at;
     return p;
+}
+
+// The first tile of sequence `seq`, which begins at token `first`: the sequences before it have first tokens, so that no more than
+// min(seq, first) of them have any, and each has one tile at most that is not full.  Some tiles are of no sequence, but nobody has to count
+// those of all sequences before (which took 31 us of 41 with 1,000 sequences, and 5 ms with 20,000).
+__device__ __forceinline__ int64_t first_tile(int64_t first, int64_t seq) { return first / kRows + min(seq, first); }
+
+// Tile number `index`, of no rows if no sequence has it.  By one wavefront, whose lanes look for the last sequence that begins at this tile or
+// before it in 64 places at a time; every lane gets the answer.
+__device__ __forceinline__ RowTile find_tile(const int32_t* __restrict__ segments, int S, int64_t T, int64_t index)
+{
+    if (!segments) return {0, index * kRows, (int)min((int64_t)kRows, T - index * kRows)};
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = S;
+    for (;;) {
+        const int step = (n + 63) / 64, seq = lo + min(lane * step, n - 1);
+        const GroupRows rows = group_rows(segments, seq, T);
+        const int64_t tile = first_tile(rows.first, seq);
+        const uint64_t upto = __ballot(lane * step < n && tile <= index);
+        if (!upto) return {S, 0, 0};
+        const int who = 63 - __builtin_clzll(upto);
+        if (step == 1) {
+            const int64_t first = __builtin_amdgcn_readlane((int)rows.first, who), end = __builtin_amdgcn_readlane((int)rows.end, who);
+            const int64_t at = first + (index - first_tile(first, lo + who)) * kRows;
+            return {lo + who, at, at < end ? (int)min((int64_t)kRows, end - at) : 0};
+        }
+        lo += who * step;
+        n = min(step, n - who * step);
+    }
 }
 
 template <typename T, int LANES, int V>
@@ -199,8 +232,16 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
     __shared__ int32_t counts[kMostExperts], rows;
     const int sub = threadIdx.x & (LANES - 1), group = threadIdx.x / LANES;
     const int64_t index = block0 + blockIdx.x;
-    const RowTile tile = find_row_tile<kRows>(a.segments, a.S, a.T, index);
-    if (tile.rows <= 0 || tile.g >= a.S) return;
+    const RowTile tile = find_tile(a.segments, (int)a.S, a.T, index);
+    if (tile.rows <= 0) {
+        // (read only where offsets in no order give it to a sequence all the same)
+        for (int e = threadIdx.x; e < a.E; e += kThreads) {
+            p.sums[index * a.E + e] = 0.0f;
+            p.counts[index * a.E + e] = 0;
+        }
+        if (threadIdx.x == 0) p.rows[index] = 0;
+        return;
+    }
     for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
     if (threadIdx.x == 0) rows = 0;
     __syncthreads();
@@ -249,36 +290,26 @@ __global__ __launch_bounds__(kThreads) void balance_tiles_kernel(BalanceArgs a, 
 }
 
 // A sequence's tiles, or of a part of its experts: lines of E threads each take every `lines`th tile.
-__global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs a, Partial p, int64_t block0)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void balance_join_kernel(BalanceArgs a, Partial p, int64_t block0)
 {
-    __shared__ float sums[kJoinThreads], wave_loss[kJoinThreads / 64];
-    __shared__ int32_t counts[kJoinThreads], wave_rows[kJoinThreads / 64];
+    __shared__ float sums[THREADS], wave_loss[THREADS / 64];
+    __shared__ int32_t counts[THREADS], wave_rows[THREADS / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t item = block0 + blockIdx.x, seq = item / p.parts;
     const int part = (int)(item - seq * p.parts), e0 = part * p.part, experts = min(p.part, a.E - e0);
-    // the sequence's first tile: those of the sequences before it
-    int64_t first = 0;
-    if (a.segments) {
-        for (int64_t g0 = 0; g0 < seq; g0 += 64) {
-            GroupRows r = {0, 0};
-            if (g0 + lane < seq) r = group_rows(a.segments, g0 + lane, a.T);
-            int t = (int)((r.end - r.first + kRows - 1) / kRows);
-#pragma unroll
-            for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d);
-            first += t;
-        }
-    }
     const GroupRows own = group_rows(a.segments, seq, a.T);
+    const int64_t first = first_tile(own.first, seq);
     // (offsets that are not in order may name more tiles than there are)
     const int64_t end = min(first + (own.end - own.first + kRows - 1) / kRows, p.tiles);
     int n = 0;
-    for (int64_t t = first + threadIdx.x; t < end; t += kJoinThreads) n += p.rows[t];
+    for (int64_t t = first + threadIdx.x; t < end; t += THREADS) n += p.rows[t];
 #pragma unroll
     for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
     if (lane == 0) wave_rows[wave] = n;
     // (no more lines than a line has loads on their way: they are added up one after the other)
     constexpr int kAtOnce = 16;
-    const int lines = min(kJoinThreads / experts, 2 * kAtOnce), line = threadIdx.x / experts, e = threadIdx.x - line * experts;
+    const int lines = min(THREADS / experts, 2 * kAtOnce), line = threadIdx.x / experts, e = threadIdx.x - line * experts;
     float s = 0.0f;
     int32_t c = 0;
     if (line < lines) {
@@ -303,7 +334,7 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
     __syncthreads();
     n = 0;
 #pragma unroll
-    for (int w = 0; w < kJoinThreads / 64; ++w) n += wave_rows[w];
+    for (int w = 0; w < THREADS / 64; ++w) n += wave_rows[w];
     float loss = 0.0f;
     if ((int)threadIdx.x < experts) {
         for (int i = 1; i < lines; ++i) {
@@ -320,7 +351,7 @@ __global__ __launch_bounds__(kJoinThreads) void balance_join_kernel(BalanceArgs 
     __syncthreads();
     if (threadIdx.x == 0) {
         loss = 0.0f;
-        for (int w = 0; w < kJoinThreads / 64; ++w) loss += wave_loss[w];
+        for (int w = 0; w < THREADS / 64; ++w) loss += wave_loss[w];
         if (part == 0) a.rows[seq] = n;
         (a.S * p.parts == 1 ? a.loss : p.losses + item)[0] = loss;
     }
@@ -332,6 +363,7 @@ __device__ __forceinline__ int sequences_used(const int32_t* __restrict__ rows, 
 {
     __shared__ int32_t part[THREADS / 64];
     int n = 0;
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < S; i += THREADS) n += rows[i] > 0;
 #pragma unroll
     for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
@@ -348,6 +380,7 @@ __global__ __launch_bounds__(kThreads) void balance_mean_kernel(BalanceArgs a, P
     __shared__ float part[kThreads / 64];
     const int used = sequences_used<kThreads>(a.rows, a.S);
     float s = 0.0f;
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < a.S * p.parts; i += kThreads) s += p.losses[i];
 #pragma unroll
     for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
@@ -454,8 +487,9 @@ hipError_t balance(const BalanceArgs& a, hipStream_t s)
         });
     });
     if (err != hipSuccess) return err;
-    err = launch_parts(a.S * p.parts, kJoinThreads, [&](unsigned grid, int64_t block0) {
-        balance_join_kernel<<<grid, kJoinThreads, 0, s>>>(a, p, block0);
+    err = launch_parts(a.S * p.parts, p.threads, [&](unsigned grid, int64_t block0) {
+        if (p.threads == kManyThreads) balance_join_kernel<kManyThreads><<<grid, kManyThreads, 0, s>>>(a, p, block0);
+        else balance_join_kernel<kJoinThreads><<<grid, kJoinThreads, 0, s>>>(a, p, block0);
     });
     if (err != hipSuccess || a.S * p.parts == 1) return err;
     balance_mean_kernel<<<1, kThreads, 0, s>>>(a, p);

@@ -70,6 +70,16 @@ def test_sequences(sizes, dtype):
     check((random(T, T, 20) + random(1, 20)).to(dtype), 3, segments)
 
 
+# as many sequences as share the compute units by smaller workgroups and one less, many of them empty or of one token, and a long one; more
+# than one, two and three rounds of a search in 64 places; more experts than a smaller workgroup has
+@pytest.mark.parametrize("S,E", [(64, 9), (65, 9), (511, 20), (512, 20), (700, 300), (1_000, 1_024), (4_097, 17), (65_536, 3)])
+def test_many_sequences(S, E):
+    sizes = np.random.default_rng(S).choice([0, 0, 1, 1, 2, 3], S)
+    sizes[S // 3], sizes[-1] = 300, 2
+    segments = offsets_of(sizes.tolist()) + 5  # some tokens before the first sequence, some behind the last
+    check((random(S, int(sizes.sum()) + 12, E) + random(1, E)).to(torch.bfloat16), 2, segments)
+
+
 def test_tokens_before_the_first_sequence():
     check(random(1, 100, 9), 2, torch.tensor([13, 50, 50, 90], dtype=torch.int32))
 
