@@ -13,8 +13,8 @@
 // its rows.
 //
 // Bound by memory where there are many: 16,384 tokens (a tenth of them one), 65,536 rows of 2,048, bf16: the lookup 16.4 us, 106 MB at
-// 6.5 TB/s; the gradient 75 us: sorting 30, which clears 122 MB, sums 21, which read 67 MB, joins 24, which clear the other half: 339 MB
-// at 4.5 TB/s.  Of few the launches are: 8 rows of 4,096 3.4 us, and 1,498 tokens' gradient in 551 rows of 256 7.6.
+// 6.5 TB/s; the gradient 72 us: sorting 28, which clears 134 MB, sums 21, which read 67 MB, joins 23, which clear the other half: 339 MB
+// at 4.7 TB/s.  Of few the launches are: 8 rows of 4,096 3.4 us, and 1,498 tokens' gradient in 551 rows of 256 7.6.
 #include <algorithm>
 #include <type_traits>
 
