@@ -344,3 +344,45 @@ def test_few_rows_are_exact(G, R, N, K, dtype):
     want, size = grouped_mm(offsets, values(x, xs, K, True), values(w, ws, K, False), "nk", R)
     assert_within(y, want, (K + 8) * EPS * size)
     check(x, xs, w, ws, K, offsets, R, torch.float32)
+
+
+# every kernel of tiles, of 16-bit results, and few rows
+KERNELS = [(11, 300, 500, (0, 16)), (60, 4_000, 4_000, (0, 32)), (700, 1_000, 1_100, (2, 64)), (900, 3_900, 2_200, (2, 128)), (300, 4_000, 300, (1, 64)),
+           (2_000, 4_000, 4_000, (1, 128)), (4_000, 8_100, 530, (1, 256))]
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("R,N,K,kernel", KERNELS)
+def test_products_that_nothing_cuts_off(R, N, K, kernel, dtype):
+    # codes -8 .. 8: products lie within seven powers of two, which 13 bits hold whole, their sums are whole numbers below 2^24, and the
+    # scales powers of two: a result is rounded once
+    assert plan(1, R, K, N, dtype, given=False)[:2] == kernel
+    gen = torch.Generator().manual_seed(R)
+    pad = lambda v: torch.nn.functional.pad(v, (0, -K % BLOCK)).to(F8)  # noqa: E731
+    x, w = (pad(torch.randint(-8, 9, s, generator=gen).float()) for s in ((R, K), (1, N, K)))
+    y = filled(dtype, R, N)
+    binding.sgap_grouped_mm_f8(1, R, K, N, None, x.cuda(), torch.full((R, blocks(K)), 0.25, device="cuda"), w.cuda(),
+                               torch.full((1, blocks(N), blocks(K)), 0.5, device="cuda"), y)
+    want = torch.mm(x.cuda().double(), w[0].cuda().double().t().contiguous()) / 8
+    assert torch.equal(y, want.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("R,N,K,kernel", KERNELS)
+def test_nan_of_codes_stays_in_its_row_and_column(R, N, K, kernel, dtype):
+    # a row that is NaN, a column with one in its last block, and rows that a list leaves out, in whose place the NaN row is read
+    assert plan(1, R, K, N, dtype, given=False, src=True)[:2] == kernel
+    x, xs, w, ws = operands(2, R, 1, N, K)
+    x.view(torch.uint8)[0, :K] = 0x7f
+    x.view(torch.uint8)[7, K - 1] = 0xff
+    w.view(torch.uint8)[0, N - 2, K - 1] = 0x7f
+    src = torch.arange(R, dtype=torch.int32)
+    src[3], src[R - 2] = -1, R
+    y = filled(dtype, R, N)
+    y.zero_()
+    binding.sgap_grouped_mm_f8(1, R, K, N, None, x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), y, src=src.cuda())
+    want = torch.zeros(R, N, dtype=torch.bool)
+    want[0], want[7], want[:, N - 2] = True, True, True
+    want[3], want[R - 2] = False, False
+    assert torch.equal(torch.isnan(y).cpu(), want)
+    assert not y[3].any() and not y[R - 2].any()
