@@ -393,7 +393,8 @@ __global__ __launch_bounds__(kThreads) void balance_mean_kernel(BalanceArgs a, P
     }
 }
 
-// SEQUENCES: there are segments.
+// SEQUENCES: there are segments.  Each workgroup counts those that have a token, which takes longer the more there are (us, 128
+// experts, bf16, 1 / 1,000 / 20,000 / 65,536 sequences: 16,384 tokens 4.6, 6.5, 9.8, 15.2; 65,536 tokens 8.8, 15.2, 24.3, 36.5).
 template <typename T, int LANES, int V, bool SEQUENCES>
 __global__ __launch_bounds__(kThreads) void balance_grad_kernel(BalanceGradArgs a, int64_t row_blocks)
 {

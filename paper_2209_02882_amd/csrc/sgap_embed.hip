@@ -734,7 +734,12 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
     // One launch for a few tokens.  It reads a frequent token's rows by one compute unit, and where a large table is cleared that comes on
     // top.  (us, three launches and one, ids' frequency one over their rank, 16 bits: 92 tokens, 496 rows of 557 15.4, 5.0; 1,498, 551 of
     // 256 19.0, 7.6; 4,096, 32,000 of 1,024 41.2, 20.5; 8,192, 8,000 of 512 35.0, 19.0; 8,192, 65,536 of 2,048 82.9, 88.2, and added up
-    // 64.6, 36.1.  At its worst, all tokens of one id, 4,096 of 1,024 take 34.5, 53.7.)
+    // 64.6, 36.1.)  It is the slower one where one id has a large part of the tokens, since a row's columns are four workgroups' at most with
+    // 64 rows or more: all of 4,096 tokens of 1,024 34.5, 53.7; three launches with 8,193 tokens, one with 8,192 added to 8,000 rows in 16 bits, all / half /
+    // frequency one over rank: of 1,024 42.5, 90.3 / 35.7, 51.2 / 32.5, 21.9; of 4,096 48.6, 176 / 47.1, 142 / 46.5, 46.7; of 8,192 58.5, 328 /
+    // 67.0, 277 / 64.7, 104.  And where the ids have few residues of the number of workgroups across rows, whose list each wavefront looks through for
+    // each row: 8,192 tokens of 1,024, 32,768 rows, ids multiples of 1 / 64 / 256 / 4,096 23.1, 21.2 / 20.3, 537 / 20.6, 929 / 24.1, 153.
+    // The ids are on the device: the host's rule cannot tell.
     if (a.T > 0 && a.T <= kFewTokens && a.V <= 1 << 22 && (ADD || a.T <= 1024 || a.V * a.D * (int64_t)sizeof(G) <= 128 << 20)) {
         // 256 workgroups, by rows first; columns are shared by four of them where there are so many, so that a frequent token's are
         const int64_t pieces = (a.D + 64 * VEC - 1) / (64 * VEC), four = std::min<int64_t>(pieces, 4);
@@ -746,6 +751,8 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t s)
     }
     const Spread sp = spread<VEC>(a.D);
     const Sorted st = sorted_view(a.workspace, a.T, a.V, a.D, kThreads / sp.lanes);
+    // A workgroup of the sort looks at all tokens, so that its time grows with tokens times rows: even ids, floats, 262,144 tokens and rows of 64
+    // 113 us, 1,048,576 of 16 969, 4,194,304 tokens of those 3,597.
     // 256 ranges, one for each compute unit (us of lookup and gradient, 512 and 256: 16,384 tokens, 65,536 rows of 2,048 95.7, 95.0; 16,384
     // rows 62.3, 57.8; 12,000 tokens, 50,001 rows of 64 26.1, 22.1)
     constexpr int64_t ranges = 256;
